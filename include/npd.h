@@ -391,6 +391,112 @@ npd_status npd_policy_lag(int64_t n_tokens, int32_t n_segments, const float* kl_
 npd_status npd_segment_ppl(int32_t n_segments, const float* seg_mean_nll, const int32_t* seg_count, float* seg_ppl,
                            void* stream);
 
+/*
+ * The language-model head with the loss behind it: the calls below take hidden states [T, D] and the head's weights
+ * [V, D] in place of logits [T, V], for programs that would hold the logits for the loss alone.  They share a
+ * descriptor; fields that an entry point has no use for are ignored.
+ */
+#define NPD_HEAD_MAX_VOCAB (1 << 21)  /* largest vocabulary and row stride (elements), beyond: NPD_ERR_UNSUPPORTED */
+#define NPD_HEAD_MAX_WIDTH (1 << 16)  /* largest width, likewise                                                  */
+
+/* npd_head_desc.flags */
+enum {
+  NPD_HEAD_GRAD_HIDDEN = 1u,  /* grad_hidden is given                                                              */
+  NPD_HEAD_GRAD_WEIGHT = 2u,  /* grad_weight is given                                                              */
+  NPD_HEAD_GRAD_BIAS = 4u,    /* grad_bias is given                                                                */
+  NPD_HEAD_ACCUMULATE = 8u,   /* grad_weight and grad_bias are added to (in fp32, rounded once) instead of written */
+  NPD_HEAD_UNALIGNED = 16u    /* hidden, weight or grad_logits begin anywhere, not on 16 bytes                     */
+};
+
+/* which entry point npd_head_workspace_bytes() is asked about */
+enum { NPD_HEAD_LOSS = 0, NPD_HEAD_LOGITS = 1, NPD_HEAD_LOGITS_BWD = 2 };
+
+typedef struct {
+  int64_t n_tokens;           /* T in [1, NPD_MAX_TOKENS]                                            */
+  int32_t vocab;              /* V in [1, NPD_HEAD_MAX_VOCAB]                                        */
+  int32_t width;              /* D in [1, NPD_HEAD_MAX_WIDTH]                                        */
+  int64_t hidden_stride;      /* elements between rows of hidden (>= D)                              */
+  int64_t weight_stride;      /* elements between rows of weight (>= D)                              */
+  int64_t grad_hidden_stride; /* of grad_hidden, with NPD_HEAD_GRAD_HIDDEN (>= D)                    */
+  int64_t grad_weight_stride; /* of grad_weight, with NPD_HEAD_GRAD_WEIGHT (>= D)                    */
+  int64_t logits_stride;      /* of logits and grad_logits, where an entry point has them (>= V)     */
+  int32_t topk;               /* loss: k in [1, min(V, 4096)] entries of the teacher's record, 0: no teacher */
+  uint32_t flags;             /* NPD_HEAD_*                                                          */
+  float tau;                  /* loss: KD temperature, finite, > 0                                   */
+  float grad_scale;           /* loss: finite; multiplies the KD gradient (ignored without a teacher) */
+  float ce_grad_scale;        /* loss: finite; weight of the hard-label CE gradient                  */
+  float softcap;              /* finite, >= 0; 0: none                                               */
+} npd_head_desc;
+
+/*
+ * Bytes of device workspace that an entry point (`op`: NPD_HEAD_LOSS, ...) takes for `desc`: the least, and as many as it
+ * can make use of (rows are worked on in chunks, longer ones with more; results agree to rounding).  Host calls; 0 is a
+ * legal answer and what an invalid desc gets.
+ */
+size_t npd_head_workspace_bytes(const npd_head_desc* desc, int op);
+size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op);
+
+/*
+ * The loss of npd_kd_loss_fwd_bwd against a top-k record (Eq. 2), hard labels, or both (Eq. 1), with
+ *
+ *   x[p, v] = hidden[p, :] . weight[v, :] + bias[v],      with softcap > 0: softcap * tanh(that / softcap)
+ *
+ * in the place of the student's logits, which are never stored: p_S = Softmax(x / tau),
+ *
+ *   kd_tok[p], nll_tok[p], lse_tok[p]   as there (of fp32 logits)
+ *   G[p, v]        = (grad_scale / tau * (p_S(v) - p_T(v) [v in support]) + ce_grad_scale * (p_S(v) - [v == labels[p]]))
+ *                    * dx / d(hidden . weight)                                           at scored positions, else 0
+ *   grad_hidden[p] = sum_v G[p, v] weight[v];   grad_weight[v] = sum_p G[p, v] hidden[p];   grad_bias[v] = sum_p G[p, v]
+ *
+ * Any of the gradients may be asked for by its flag; with none the call is forward only (the scoring pass of Eq. 3).
+ * Positions with loss_mask[p] == 0 cost nothing but their zeros (scalars and grad_hidden rows).
+ *
+ *   hidden       bf16 [T, hidden_stride], required          weight   bf16 [V, weight_stride], required
+ *   bias         bf16 [V] or NULL (-inf: an entry of probability 0, without a soft cap)
+ *   labels       int32 [T]; required iff nll_tok is given or ce_grad_scale != 0 (given without: they must still be ids
+ *                for the call to be fast, and any other value is let pass)
+ *   teacher_idx  int32 [T, k] and teacher_val fp32 [T, k], iff topk > 0: as in npd_kd_loss_fwd_bwd
+ *   loss_mask    uint8 [T], required
+ *   grad_hidden  bf16 [T, grad_hidden_stride]   grad_weight  bf16 [V, grad_weight_stride]   grad_bias  bf16 [V]
+ *   kd_tok (with a teacher), nll_tok, lse_tok   fp32 [T] or NULL
+ *   dev_status   int32 [1] or NULL: a label (if used) or id outside [0, V) gives NaN scalars, a NaN row of grad_hidden and
+ *                no part in grad_weight and grad_bias
+ *   workspace    device, >= npd_head_workspace_bytes(desc, NPD_HEAD_LOSS) bytes, 256-byte aligned; scratch of the call
+ *
+ * NPD_ERR_UNSUPPORTED: tau != 1 together with nll_tok, lse_tok or ce_grad_scale != 0 (quantities at tau = 1: ask for them in
+ * a call of their own), and gradients with grad_scale and ce_grad_scale of opposite sign.  NPD_ERR_VALUE: ce_grad_scale != 0
+ * without a gradient, gradients with neither a teacher nor ce_grad_scale.
+ *
+ * Products are of bf16 operands with fp32 sums (the gradient's operands G and hidden are rounded to bf16 once each, G against
+ * its row's scale); softmax statistics are fp32.  Results are reproducible bit by bit for the same workspace size.
+ */
+npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, const void* weight, const void* bias,
+                                 const int32_t* labels, const int32_t* teacher_idx, const float* teacher_val,
+                                 const uint8_t* loss_mask, void* grad_hidden, void* grad_weight, void* grad_bias,
+                                 float* kd_tok, float* nll_tok, float* lse_tok, int32_t* dev_status, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * The logits themselves, for the calls that take them (dense teachers, other divergences, npd_teacher_topk):
+ * logits[p, v] = x[p, v] as above, rounded to bf16 once; all T positions.  logits bf16 [T, logits_stride]; what lies
+ * between V and the stride is left as it was.
+ */
+npd_status npd_head_logits(const npd_head_desc* desc, const void* hidden, const void* weight, const void* bias,
+                           void* logits, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The backward pass of npd_head_logits from the gradient of its logits (npd_kd_loss_fwd_bwd's grad_out):
+ *
+ *   z[p, v] = grad_logits[p, v] * (softcap > 0 ? 1 - (logits[p, v] / softcap)^2 : 1)
+ *   grad_hidden[p] = sum_v z[p, v] weight[v];  grad_weight[v] = sum_p z[p, v] hidden[p];  grad_bias[v] = sum_p z[p, v]
+ *
+ *   grad_logits bf16 [T, logits_stride], required; logits bf16 [T, logits_stride], required iff softcap > 0, else NULL;
+ *   weight may be NULL without NPD_HEAD_GRAD_HIDDEN, hidden without NPD_HEAD_GRAD_WEIGHT; one gradient at least
+ */
+npd_status npd_head_logits_bwd(const npd_head_desc* desc, const void* grad_logits, const void* logits,
+                               const void* hidden, const void* weight, void* grad_hidden, void* grad_weight,
+                               void* grad_bias, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

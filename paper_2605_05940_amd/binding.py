@@ -24,13 +24,16 @@ NPD_DEV_BAD_LABEL, NPD_DEV_BAD_TOPK_INDEX, NPD_DEV_BAD_CU_SEQLENS, NPD_DEV_GANG_
 NPD_ZONE_DEGENERATE, NPD_ZONE_PROXIMAL, NPD_ZONE_DISCONNECT, NPD_ZONE_INVALID = 0, 1, 2, 3
 NPD_IFD_REQUIRE_TEACHER_LE_1 = 1
 NPD_TOPK_LOG_PROBS = 1
+NPD_HEAD_GRAD_HIDDEN, NPD_HEAD_GRAD_WEIGHT, NPD_HEAD_GRAD_BIAS, NPD_HEAD_ACCUMULATE, NPD_HEAD_UNALIGNED = 1, 2, 4, 8, 16
+NPD_HEAD_LOSS, NPD_HEAD_LOGITS, NPD_HEAD_LOGITS_BWD = 0, 1, 2
 NOALLOC_WORKSPACE_BYTES = 16 << 20   # NPD_NOALLOC_WORKSPACE_BYTES
 
 EXPORTS = ("npd_version", "npd_status_string", "npd_workspace_bytes", "npd_kd_loss_fwd_bwd",
            "npd_segment_reduce", "npd_delta_ifd_score", "npd_teacher_topk", "npd_debug_gang_spin_limit",
            "npd_kd_loss_fwd_bwd_noalloc", "npd_policy_lag", "npd_segment_ppl", "npd_kd_kernel_name",
            "npd_forward_scratch_bytes", "npd_kd_loss_forward", "npd_workspace_bytes_preferred",
-           "npd_kept_workspace_bytes", "npd_kd_loss_fwd_bwd_kept")
+           "npd_kept_workspace_bytes", "npd_kd_loss_fwd_bwd_kept", "npd_head_workspace_bytes",
+           "npd_head_workspace_bytes_preferred", "npd_head_loss_fwd_bwd", "npd_head_logits", "npd_head_logits_bwd")
 
 
 class NpdError(RuntimeError):
@@ -46,6 +49,16 @@ class KdDesc(ctypes.Structure):
                 ("topk", ctypes.c_int32), ("flags", ctypes.c_uint32),
                 ("tau", ctypes.c_float), ("grad_scale", ctypes.c_float), ("ce_grad_scale", ctypes.c_float),
                 ("divergence", ctypes.c_int32), ("skew_alpha", ctypes.c_float)]
+
+
+class HeadDesc(ctypes.Structure):
+    """Mirror of ``npd_head_desc``."""
+    _fields_ = [("n_tokens", ctypes.c_int64), ("vocab", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64),
+                ("grad_hidden_stride", ctypes.c_int64), ("grad_weight_stride", ctypes.c_int64),
+                ("logits_stride", ctypes.c_int64), ("topk", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("tau", ctypes.c_float), ("grad_scale", ctypes.c_float), ("ce_grad_scale", ctypes.c_float),
+                ("softcap", ctypes.c_float)]
 
 
 _lib = None
@@ -95,12 +108,21 @@ def load() -> ctypes.CDLL:
                  "npd_kd_loss_forward": (ctypes.c_int, [_vp] * 12 + [ctypes.c_size_t, _vp])}
         newest = {"npd_kept_workspace_bytes": (ctypes.c_size_t, [_vp]),
                   "npd_kd_loss_fwd_bwd_kept": (ctypes.c_int, [_vp] * 13 + [ctypes.c_size_t, _vp])}
+        head = {"npd_head_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int]),
+                "npd_head_workspace_bytes_preferred": (ctypes.c_size_t, [ctypes.c_int]),
+                "npd_head_loss_fwd_bwd": (ctypes.c_int, [_vp] * 15 + [ctypes.c_size_t, _vp]),
+                "npd_head_logits": (ctypes.c_int, [_vp] * 5 + [ctypes.c_size_t, _vp]),
+                "npd_head_logits_bwd": (ctypes.c_int, [_vp] * 8 + [ctypes.c_size_t, _vp])}
         here = os.path.realpath(LIB_PATH) == os.path.realpath(os.path.join(HERE, "libnpd.so"))
         native = here or all(hasattr(L, name) for name in newer)
         for name, (result, more) in {**newer, **newest}.items():
             if here or hasattr(L, name):
                 getattr(L, name).restype = result
                 getattr(L, name).argtypes = [ctypes.POINTER(KdDesc)] + more
+        for name, (result, more) in head.items():
+            if here or hasattr(L, name):
+                getattr(L, name).restype = result
+                getattr(L, name).argtypes = [ctypes.POINTER(HeadDesc)] + more
         _host = _load_host(L) if native else None
         _lib = L
     return _lib
@@ -415,3 +437,128 @@ def npd_segment_ppl(seg_mean_nll: torch.Tensor, seg_count: torch.Tensor, seg_ppl
         raise ValueError("inconsistent sizes")
     _check(load().npd_segment_ppl(S, _ptr(seg_mean_nll, torch.float32), _ptr(seg_count, torch.int32),
                                   _ptr(seg_ppl, torch.float32), _stream()))
+
+
+# ------------------------------------------------------------------------------------------------------------- the head
+
+def _matrix(name: str, t: Optional[torch.Tensor], shape):
+    """Device pointer of a bf16 matrix of ``shape`` with unit stride along its rows (None if it is absent)."""
+    if t is None:
+        return None
+    if t.shape != shape or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be {list(shape)} with unit stride along its rows")
+    return _ptr(t, torch.bfloat16)
+
+
+def _pitch(t: Optional[torch.Tensor]) -> int:
+    """Elements between the rows of a matrix (of one row, where torch keeps any stride: its width)."""
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, *inputs) -> int:
+    return ((NPD_HEAD_GRAD_HIDDEN if grad_hidden is not None else 0) | (NPD_HEAD_GRAD_WEIGHT if grad_weight is not None else 0) |
+            (NPD_HEAD_GRAD_BIAS if grad_bias is not None else 0) | (NPD_HEAD_ACCUMULATE if accumulate else 0) |
+            (NPD_HEAD_UNALIGNED if any(t is not None and t.data_ptr() & 15 for t in inputs) else 0))
+
+
+def _head_workspace(L, desc, op: int, workspace: Optional[torch.Tensor]):
+    """(pointer, bytes) of a call's workspace: the caller's, or a block from torch's stream-ordered allocator, which it goes
+    back to when the call has been enqueued (smaller where there is no memory for what the call prefers)."""
+    if workspace is not None:
+        return workspace, _ptr(workspace), workspace.numel() * workspace.element_size()
+    want = L.npd_head_workspace_bytes_preferred(desc, op)
+    if not want:
+        return None, None, 0
+    block = _own_block(want)
+    if block is None:
+        want = L.npd_head_workspace_bytes(desc, op)
+        block = torch.empty(want, dtype=torch.uint8, device="cuda")
+    return block, block.data_ptr(), want
+
+
+def _on_current_device(t: torch.Tensor) -> None:
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, kernels run on the current device: make it current first")
+
+
+def npd_head_loss_fwd_bwd(hidden: torch.Tensor, weight: torch.Tensor, loss_mask: torch.Tensor, *,
+                          bias: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                          labels: Optional[torch.Tensor] = None, teacher_idx: Optional[torch.Tensor] = None,
+                          teacher_val: Optional[torch.Tensor] = None, tau: float = 1.0, grad_scale: float = 1.0,
+                          ce_grad_scale: float = 0.0, grad_hidden: Optional[torch.Tensor] = None,
+                          grad_weight: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                          accumulate: bool = False, kd_tok: Optional[torch.Tensor] = None,
+                          nll_tok: Optional[torch.Tensor] = None, lse_tok: Optional[torch.Tensor] = None,
+                          dev_status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Enqueue the loss of ``npd_kd_loss_fwd_bwd`` on logits ``hidden @ weight.T + bias`` that are never stored, with the
+    gradients that are given a tensor (see ``npd_head_loss_fwd_bwd`` in npd.h); with none of them the call is forward only.
+    ``accumulate``: the gradients of weight and bias are added to what their tensors hold.  ``workspace``: a uint8 tensor of
+    at least ``npd_head_workspace_bytes`` bytes; without it the call takes a block from torch's allocator for as long as it
+    is being enqueued.
+    """
+    T, D = hidden.shape
+    V = weight.shape[0]
+    k = 0
+    if teacher_idx is not None:
+        k = teacher_idx.shape[1] if teacher_idx.dim() == 2 else 0
+        if teacher_val is None or k == 0 or not (
+                teacher_idx.is_contiguous() and teacher_val.is_contiguous() and teacher_val.shape == teacher_idx.shape
+                and teacher_idx.shape[0] == T):
+            raise ValueError("teacher_idx / teacher_val must be contiguous [T, k]")
+    _on_current_device(hidden)
+    desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight), 0, k,
+                                 _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, hidden, weight), tau, grad_scale,
+                                 ce_grad_scale, softcap))
+    args = (desc, _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
+            _array("bias", bias, V, torch.bfloat16), _array("labels", labels, T, torch.int32),
+            _ptr(teacher_idx, torch.int32), _ptr(teacher_val, torch.float32),
+            _array("loss_mask", loss_mask, T, torch.uint8), _matrix("grad_hidden", grad_hidden, (T, D)),
+            _matrix("grad_weight", grad_weight, (V, D)), _array("grad_bias", grad_bias, V, torch.bfloat16),
+            _array("kd_tok", kd_tok, T, torch.float32), _array("nll_tok", nll_tok, T, torch.float32),
+            _array("lse_tok", lse_tok, T, torch.float32), _array("dev_status", dev_status, 1, torch.int32))
+    L = load()
+    _block, ws, n = _head_workspace(L, desc, NPD_HEAD_LOSS, workspace)
+    _check(L.npd_head_loss_fwd_bwd(*args, ws, n, _stream()))
+
+
+def npd_head_logits(hidden: torch.Tensor, weight: torch.Tensor, *, logits_out: torch.Tensor,
+                    bias: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                    workspace: Optional[torch.Tensor] = None) -> None:
+    """Enqueue ``logits_out = hidden @ weight.T + bias``, soft-capped, rounded to bf16 once (see ``npd_head_logits`` in npd.h)."""
+    T, D = hidden.shape
+    V = weight.shape[0]
+    _on_current_device(hidden)
+    desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), 0, 0, _pitch(logits_out), 0,
+                                 _head_flags(None, None, None, False, hidden, weight), 1.0, 0.0, 0.0, softcap))
+    args = (desc, _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
+            _array("bias", bias, V, torch.bfloat16), _matrix("logits_out", logits_out, (T, V)))
+    L = load()
+    _block, ws, n = _head_workspace(L, desc, NPD_HEAD_LOGITS, workspace)
+    _check(L.npd_head_logits(*args, ws, n, _stream()))
+
+
+def npd_head_logits_bwd(grad_logits: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, *,
+                        logits: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                        grad_hidden: Optional[torch.Tensor] = None, grad_weight: Optional[torch.Tensor] = None,
+                        grad_bias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                        workspace: Optional[torch.Tensor] = None) -> None:
+    """Enqueue the backward pass of ``npd_head_logits`` from the bf16 gradient of its logits (see ``npd_head_logits_bwd`` in
+    npd.h); ``logits`` are its outputs, needed with a soft cap (and ignored without)."""
+    T, D = hidden.shape
+    V = weight.shape[0]
+    _on_current_device(hidden)
+    if softcap == 0.0:
+        logits = None
+    elif logits is not None and logits.shape == grad_logits.shape and _pitch(logits) != _pitch(grad_logits):
+        raise ValueError("logits must have the row stride of grad_logits")
+    desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight),
+                                 _pitch(grad_logits), 0,
+                                 _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, grad_logits, hidden, weight), 1.0,
+                                 0.0, 0.0, softcap))
+    args = (desc, _matrix("grad_logits", grad_logits, (T, V)), _matrix("logits", logits, (T, V)),
+            _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
+            _matrix("grad_hidden", grad_hidden, (T, D)), _matrix("grad_weight", grad_weight, (V, D)),
+            _array("grad_bias", grad_bias, V, torch.bfloat16))
+    L = load()
+    _block, ws, n = _head_workspace(L, desc, NPD_HEAD_LOGITS_BWD, workspace)
+    _check(L.npd_head_logits_bwd(*args, ws, n, _stream()))

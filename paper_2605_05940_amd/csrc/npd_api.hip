@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "../../include/npd.h"
+#include "npd_check.hpp"
 #include "npd_internal.hpp"
 
 // Scratch of npd_kd_loss_fwd_bwd_noalloc: one copy per GPU, held from the time the library is loaded on that GPU
@@ -15,28 +16,7 @@ static __device__ __align__(256) unsigned char scratch[NPD_NOALLOC_WORKSPACE_BYT
 
 namespace {
 
-struct Range {
-  uintptr_t b, e;
-};
-
-Range range_of(const void* p, size_t bytes) {
-  const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-  return Range{b, b + bytes};
-}
-
-bool overlaps(const Range& x, const Range& y) { return x.b < y.e && y.b < x.e && x.b != x.e && y.b != y.e; }
-
-size_t rows_bytes(int64_t T, int64_t stride, int64_t width, size_t elem) {
-  return (size_t)(((T - 1) * stride + width) * (int64_t)elem);
-}
-
-// a row stride the byte extent of [T, stride] bf16 / fp32 arrays can be computed with in 64 bits
-bool stride_fits(int64_t T, int64_t stride) { return stride <= (INT64_MAX / 8) / T; }
-
-// a pointer that is not a multiple of its element size (NULL counts as aligned)
-bool misaligned(const void* p, uintptr_t elem) { return (reinterpret_cast<uintptr_t>(p) & (elem - 1)) != 0; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+using namespace npd;  // the checks of npd_check.hpp
 
 // two tensors whose rows 0 begin at the same offset from a 16-byte boundary (an absent one agrees with any)
 bool same_offset(const void* p, const void* q) {
@@ -76,20 +56,6 @@ npd_status check_desc(const npd_kd_desc* d) {
   if (d->teacher_kind == NPD_TEACHER_TOPK && d->topk > npd::kTopkMax) return NPD_ERR_UNSUPPORTED;
   return NPD_OK;
 }
-
-// true if an output range overlaps an input range or another output range
-bool any_alias(const Range* in, int n_in, const Range* out, int n_out) {
-  for (int o = 0; o < n_out; ++o) {
-    for (int i = 0; i < n_in; ++i)
-      if (overlaps(out[o], in[i])) return true;
-    for (int o2 = o + 1; o2 < n_out; ++o2)
-      if (overlaps(out[o], out[o2])) return true;
-  }
-  return false;
-}
-
-Range opt_range(const void* p, size_t bytes) { return p ? range_of(p, bytes) : Range{0, 0}; }
-
 
 // Numbers of the launches on records that are not cleared: each is taken once in the life of the process, so no word that an
 // earlier launch left can be taken for one of a later launch.  When they run out such calls are refused.

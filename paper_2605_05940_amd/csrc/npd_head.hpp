@@ -1,0 +1,134 @@
+// Launch interface of the head operators: arguments of their kernels, shared by npd_head_api.hip and the kernel files.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "npd_head_gemm.hpp"
+#include "npd_internal.hpp"
+
+namespace npd {
+
+constexpr int kHeadPart = 128;  // columns of one partial sum of a row: what a wave holds of it
+
+enum HeadForward { kHeadLogits = 0, kHeadSums = 1, kHeadSumsKept = 2 };
+
+// x = (q w^T + bias), soft-capped, of a chunk of rows; then by HeadForward
+//   kHeadLogits     out = x, rounded to bf16
+//   kHeadSums       part[row][v / 128] = (r, z): sum over those 128 columns of 2^(x c - r) is z
+//   kHeadSumsKept   and e[row][v] = 2^(x c - r) (with a soft cap times dx / d(q w^T)), rounded to bf16; 0 for v >= V
+struct HeadForwardArgs {
+  HeadChunk chunk;
+  HeadMatrix q, w;      // q.rows is the chunk's (set on the device)
+  const uint16_t* bias; // or null
+  int32_t K, V;
+  float cap;            // 0: none
+  float c;              // log2(e) / tau
+  const float* r0;      // [rows] a logit of the row times c, whole, or -1e30: the reference of columns not far above it
+  float2* part;
+  int32_t parts;
+  uint16_t* e;
+  int64_t e_stride;
+  uint16_t* out;
+  int64_t out_stride;
+};
+hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream);
+
+// out[position of row m][n] = scale[m] sum_k g[m][k] w[k][n], k < K: the gradient of the hidden states.  splits > 1: k in that
+// many pieces, joined by a second kernel through `partial` [splits][cap][N].
+struct HeadHiddenArgs {
+  HeadChunk chunk;
+  HeadMatrix g, w;
+  const float* scale;    // or null: 1
+  const int32_t* rows;   // positions of the rows, or null: m itself
+  int32_t K, N, splits;
+  float* partial;
+  int64_t partial_rows;
+  uint16_t* out;
+  int64_t out_stride;
+};
+hipError_t launch_head_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream);
+int head_hidden_splits(int64_t rows, int32_t K, int32_t N);
+
+// out[m][n] = sum_k g[k][m] h[k][n] over the rows k of the chunk, on top of the chunks before it (`partial`, fp32 [M][N]): the
+// gradient of the weights.  `out` is written with the last chunk, on top of what it holds if `accumulate`.
+struct HeadWeightArgs {
+  HeadChunk chunk;
+  HeadMatrix g, h;
+  int32_t M, N;
+  float* partial;
+  uint16_t* out;
+  int64_t out_stride;
+  int32_t accumulate;
+};
+hipError_t launch_head_weight(const HeadWeightArgs& a, hipStream_t stream);
+
+// out[m] = sum_k scale[k] g[k][m] likewise: the gradient of the bias
+constexpr int kHeadBiasSplits = 32;
+struct HeadBiasArgs {
+  HeadChunk chunk;
+  HeadMatrix g;
+  const float* scale;
+  int32_t M;
+  float* pieces;   // [kHeadBiasSplits][M]
+  float* partial;  // [M]
+  uint16_t* out;
+  int32_t accumulate;
+};
+hipError_t launch_head_bias(const HeadBiasArgs& a, hipStream_t stream);
+
+// The positions that are scored, in order, their number, and zeros for the outputs of the others.
+struct HeadRowsArgs {
+  int64_t T;
+  const uint8_t* mask;
+  int32_t* rows;
+  int32_t* count;
+  float *kd, *nll, *lse;
+  uint16_t* grad_hidden;
+  int64_t grad_stride;
+  int32_t D;
+};
+hipError_t launch_head_rows(const HeadRowsArgs& a, hipStream_t stream);
+
+// dst[i][0 .. width) = src[rows ? rows[first + i] : first + i][0 .. cols), 0 behind; with `cap` times 1 - (y / cap)^2
+struct HeadPackArgs {
+  HeadChunk chunk;
+  const int32_t* rows;
+  const uint16_t* src;
+  int64_t src_stride;
+  const uint16_t* y;
+  int64_t y_stride;
+  float cap;
+  int32_t cols, width;
+  uint16_t* dst;
+  int64_t dst_stride;
+};
+hipError_t launch_head_pack(const HeadPackArgs& a, int64_t rows, hipStream_t stream);
+
+// What a row of the loss needs besides the sums over the vocabulary: its logits at the label and at the teacher's ids.
+struct HeadLossArgs {
+  HeadChunk chunk;
+  const int32_t* rows;
+  HeadMatrix h, w;       // h: the chunk's rows
+  const uint16_t* bias;
+  int32_t K, V, k;
+  float cap, c;
+  const int32_t* labels;  // null: not used
+  const int32_t* tidx;
+  const float* tval;
+  float* x;       // [cap][1 + k] logits at the label (or column 0) and the ids
+  float* r0;      // [cap]
+  const float2* part;
+  int32_t parts;
+  float *kd, *nll, *lse;
+  int32_t* status;
+  // gradients
+  float kd_weight, ce_weight;  // grad_scale / tau, ce_grad_scale
+  uint16_t* e;                 // null: forward only
+  int64_t e_stride;
+  float* scale;
+  uint16_t* hs;                // scaled rows for the weights' gradient, or null
+};
+hipError_t launch_head_gather(const HeadLossArgs& a, int64_t rows, hipStream_t stream);
+hipError_t launch_head_finish(const HeadLossArgs& a, int64_t rows, hipStream_t stream);
+
+}  // namespace npd

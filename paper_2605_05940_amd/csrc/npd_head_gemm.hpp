@@ -1,0 +1,290 @@
+// The matrix product behind the head operators (npd_head_*.hip): C[m, n] = sum_k Q(m, k) P(n, k) of two bf16 matrices with
+// fp32 sums, one tile of C per workgroup of four waves, and whatever the caller's epilogue makes of the tile.
+//
+// Each operand is read along k (KC: a row of memory holds consecutive k) or across it (KS: a row of memory holds one k), so the
+// three products of a head -- logits = H W^T, dH = G W, dW = G^T H -- need no transposed copy of anything: a KS operand's
+// fragments come out of LDS through ds_read_b64_tr_b16, which hands lane i of 16 the i-th column of a 4 x 16 block.
+//
+// One step is 32 values of k.  Tiles of four steps are in flight or in use in LDS (buffer_load ... lds, 16 bytes per lane, no
+// registers in between); the fragments of step i + 1 are read into registers while the matrix cores work on step i, so a wave
+// waits only for the barrier that ends a step.  With 256 x 256 tiles a wave holds 128 x 128 sums (256 registers) and a step is
+// 64 v_mfma_f32_16x16x32_bf16, 1,024 cycles of its SIMD, against 512 + 256 cycles of LDS (32 KB read twice over by the four waves, 32 KB
+// written): the matrix cores are what bounds it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "npd_device.hpp"
+
+namespace npd {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kHeadStep = 32;      // values of k per step
+constexpr int kHeadStages = 4;     // steps in LDS
+constexpr int kHeadThreads = 256;  // four waves, two by two over the tile
+
+// A bf16 matrix.  KC: `rows` along m (or n), `cols` along k.  KS: `rows` along k, `cols` along m (or n).  Rows begin on 16
+// bytes.  `rows` / `cols` along m or n are limits that addresses are clamped to (what is computed there is not stored); along k
+// the limit is the product's, and what lies behind it counts as 0 without being read.  cols is a multiple of 8.
+struct HeadMatrix {
+  const uint16_t* p;
+  int64_t stride;
+  int32_t rows, cols;
+};
+
+// The rows of a batch are worked on in chunks of at most `cap` (a multiple of 256).  How many rows there are may be known on the
+// device alone (`count`): launches are made for the most there can be, and those of chunks that are not there end at once.
+// The chunks that are there share the rows evenly.
+struct HeadChunk {
+  const int32_t* count;  // null: `total`
+  int64_t total;
+  int32_t cap, index;
+};
+struct HeadSpan {
+  int64_t first;
+  int32_t rows;
+  bool there, last;
+};
+__device__ __forceinline__ HeadSpan head_span(const HeadChunk& c) {
+  const int64_t n = c.count ? (int64_t)*c.count : c.total;
+  const int64_t chunks = n > c.cap ? (n + c.cap - 1) / c.cap : 1;
+  const int64_t each = ((n + chunks - 1) / chunks + 255) / 256 * 256;
+  HeadSpan s;
+  s.first = c.index * each;
+  const int64_t left = n - s.first;
+  s.rows = (int32_t)(left < 0 ? 0 : left < each ? left : each);
+  s.there = c.index < chunks;
+  s.last = c.index == chunks - 1;
+  return s;
+}
+
+// Which tile a workgroup has.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets consecutive
+// tiles, in bands of eight tiles of m, so that the 32 that it runs together share 8 + 4 panels of the operands instead of
+// reading 64.
+struct HeadTile {
+  int m, n;
+  bool there;
+};
+__device__ __forceinline__ HeadTile head_tile(unsigned block, int mt, int nt) {
+  const unsigned total = (unsigned)mt * (unsigned)nt, per = (total + 7) / 8;
+  const unsigned local = block / 8, id = block % 8 * per + local;
+  HeadTile t;
+  t.there = local < per && id < total;
+  const unsigned band = 8u * (unsigned)nt, b = id / band, in = id % band;
+  const unsigned left = (unsigned)mt - b * 8, height = left < 8 ? left : 8;
+  t.m = (int)(b * 8 + in % (height ? height : 1));
+  t.n = (int)(in / (height ? height : 1));
+  return t;
+}
+
+#define NPD_LDS __attribute__((address_space(3)))
+
+// 16-byte groups of a KC tile's rows (64 bytes: four groups) are stored at group ^ kc_swizzle(row): the lanes of a fragment
+// read that are served together (four runs of four lanes of two groups) then hit 16 different groups of the 64 banks, in both
+// row orders below
+__device__ __forceinline__ int kc_swizzle(int row) {
+  const int a = row >> 2;
+  return ((a ^ a >> 2) & 1) << 1 ^ (a >> 1 & 1) * 3;
+}
+// 32-byte granules of a KS tile's rows are stored at granule ^ ks_swizzle(k), so that the eight rows that 32 lanes read
+// together lie in different banks
+__device__ __forceinline__ int ks_swizzle(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
+
+constexpr uint32_t kHeadRecords = 0x80000000u;  // bytes behind a tile's base that loads may reach; at offsets from here on they give 0
+
+// One operand's side of a tile: F fragments of 16 rows (or columns) for each of two waves, 32 F in all.  PAIRED: fragments 2j and
+// 2j + 1 take turns over groups of four rows, so that a lane's sums of the two are eight neighbours.
+template <int F, bool KS, bool PAIRED>
+struct HeadSide {
+  static_assert(F % 2 == 0, "loads are whole waves");
+  static constexpr int kLoads = F / 2;            // 16-byte loads per lane and step
+  static constexpr int kBytes = F * 32 * kHeadStep * 2;  // of a step
+  static constexpr int kGran = 2 * F;             // granules of a KS row
+  const uint16_t* base;  // uniform
+  int64_t step;          // elements between steps
+  uint32_t off[kLoads];
+  int kpos[2];           // KC: k of the lane's loads within a step (of even and odd ones)
+  uint32_t pitch;        // KS: bytes between rows
+  uint32_t rd[KS ? F : 2];  // where this lane's fragments begin within a step's bytes
+  int kend;
+
+  __device__ __forceinline__ void init(const HeadMatrix& x, int64_t tile0, int64_t k0, int64_t k1, int wave, int half) {
+    const int lane = threadIdx.x & 63;
+    kend = (int)(k1 - k0);
+    if constexpr (!KS) {
+      base = x.p + tile0 * x.stride + k0;
+      step = kHeadStep;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int row = (wave * kLoads + j) * 16 + (lane >> 2);
+        const int group = (lane & 3) ^ kc_swizzle(row);
+        const int64_t most = x.rows - 1 - tile0;
+        off[j] = (uint32_t)((row < most ? row : most) * x.stride * 2 + group * 16);
+        if (j < 2) kpos[j] = group * 8;  // (rows of loads j and j + 2 are 32 apart: the same swizzle)
+      }
+      const int i = lane & 15, g = lane >> 4;
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const int row = PAIRED ? 8 * (i >> 2) + 4 * f + (i & 3) : 16 * f + i;
+        rd[f] = (uint32_t)((half * F * 16 + row) * 64 + (g ^ kc_swizzle(row)) * 16);
+      }
+    } else {
+      base = x.p + k0 * x.stride + tile0;
+      step = (int64_t)kHeadStep * x.stride;
+      pitch = (uint32_t)(x.stride * 2);
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int byte = (wave * kLoads + j) * 1024 + lane * 16;
+        const int k = byte / (64 * F), group = byte % (64 * F) / 16;
+        const int gran = (group >> 1) ^ (ks_swizzle(k) & (kGran - 1));
+        const int64_t col = gran * 16 + (group & 1) * 8, most = x.cols - 8 - tile0;
+        off[j] = (uint32_t)(k * x.stride * 2 + (col < most ? col : most) * 2);
+      }
+      const int i = lane & 15, g = lane >> 4, k = 8 * g + (i >> 2);
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+        rd[f] = (uint32_t)(k * 64 * F + ((half * F + f) ^ (ks_swizzle(k) & (kGran - 1))) * 32 + (i & 3) * 8);
+    }
+  }
+
+  // requests load j of step `s` into `to` (this operand's bytes of the stage)
+  __device__ __forceinline__ void load(int j, int s, char* to, int wave) const {
+    const int left = kend - s * kHeadStep;  // uniform
+    uint32_t o = off[j], records = kHeadRecords;
+    if constexpr (KS) {
+      const int rows = left < kHeadStep ? left : kHeadStep;
+      records = __builtin_amdgcn_readfirstlane(rows < 0 ? 0 : rows) * pitch;
+    } else {
+      if (left <= kpos[j & 1]) o = kHeadRecords;
+    }
+    // Written out: a wait that the compiler puts in front of every read of LDS behind such a load (it does in front of the
+    // transposing ones) would undo what the stages are for.  The instruction writes no register; m0 is set for every use of it.
+    const uint64_t at = reinterpret_cast<uint64_t>(base + (left > 0 ? s * step : 0));
+    const i32x4 r = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)records, 0x00020000};
+    const uint32_t lds = (uint32_t)(uintptr_t)(NPD_LDS char*)(to + (wave * kLoads + j) * 1024);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(o), "s"(r) : "memory");
+  }
+
+  __device__ __forceinline__ bf16x8 fragment(int f, const char* from) const {
+    if constexpr (!KS) {
+      return *reinterpret_cast<const bf16x8*>(from + rd[f & 1] + (f >> 1) * 2048);
+    } else {
+      typedef short tr4 __attribute__((ext_vector_type(4)));
+      const tr4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NPD_LDS tr4*)(from + rd[f]));
+      const tr4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NPD_LDS tr4*)(from + rd[f] + 4 * 64 * F));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+// The sums of a tile of 32 MF rows by 32 NF columns.  acc[i][j][e]: row m = 16 i + (lane & 15) of the wave's 16 MF, column
+// 16 j + 4 (lane >> 4) + e of its 16 NF (PAIRED: 32 (j / 2) + 8 (lane >> 4) + 4 (j & 1) + e).
+template <int MF, int NF, bool QKS, bool PKS, bool PAIRED>
+struct HeadProduct {
+  using Q = HeadSide<MF, QKS, false>;
+  using P = HeadSide<NF, PKS, PAIRED>;
+  static constexpr int kLds = kHeadStages * (Q::kBytes + P::kBytes);
+  static constexpr int kTileM = 32 * MF, kTileN = 32 * NF;
+  static constexpr int kLoads = Q::kLoads + P::kLoads;
+  f32x4 acc[MF][NF];
+  Q q;
+  P p;
+  bf16x8 fq[2][MF], fp[2][NF];
+
+  template <int LEFT>
+  static __device__ __forceinline__ void meet() {
+    // LDS reads done, all but LEFT of the wave's loads landed; then every wave's
+    constexpr int imm = 0x70 | (LEFT & 15) | (LEFT >> 4) << 14;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(imm);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  static __device__ __forceinline__ char* q_stage(char* lds, int s) { return lds + s * Q::kBytes; }
+  static __device__ __forceinline__ char* p_stage(char* lds, int s) { return lds + kHeadStages * Q::kBytes + s * P::kBytes; }
+
+  template <int S>
+  __device__ __forceinline__ void phase(int i, char* lds, int wave) {
+    constexpr int cur = S & 1, nxt = cur ^ 1, sn = (S + 1) % kHeadStages;
+    meet<(kHeadStages - 2) * kLoads>();
+    constexpr int kReads = MF + NF, kSteps = MF * NF;
+    int load = 0, read = 0;
+#pragma unroll
+    for (int a = 0; a < MF; ++a) {
+#pragma unroll
+      for (int b = 0; b < NF; ++b) {
+        const int done = a * NF + b;
+        // loads and reads are spread over the first three quarters of the step's matrix instructions
+        while (load < kLoads && load * (kSteps * 3 / 4) <= done * kLoads) {
+          if (load < Q::kLoads)
+            q.load(load, i + kHeadStages, q_stage(lds, S), wave);
+          else
+            p.load(load - Q::kLoads, i + kHeadStages, p_stage(lds, S), wave);
+          ++load;
+        }
+        while (read < kReads && read * (kSteps * 3 / 4) <= done * kReads) {
+          if (read < NF)
+            fp[nxt][read] = p.fragment(read, p_stage(lds, sn));
+          else
+            fq[nxt][read - NF] = q.fragment(read - NF, q_stage(lds, sn));
+          ++read;
+        }
+        multiply(acc[a][b], fp[cur][b], fq[cur][a]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // acc += p q, written out so that the sums stay where they are (256 registers of sums leave the compiler none to move them
+  // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one)
+  static __device__ __forceinline__ void multiply(f32x4& c, const bf16x8& a, const bf16x8& b) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  }
+
+  // adds the products of k in [k0, k1) to acc
+  __device__ __forceinline__ void run(const HeadMatrix& qm, const HeadMatrix& pm, int64_t m0, int64_t n0, int64_t k0, int64_t k1,
+                                      char* lds) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    q.init(qm, m0, k0, k1, wave, wave >> 1);
+    p.init(pm, n0, k0, k1, wave, wave & 1);
+    const int steps = (int)((k1 - k0 + kHeadStep - 1) / kHeadStep);
+    if (steps <= 0) return;
+#pragma unroll
+    for (int s = 0; s < kHeadStages; ++s) {
+#pragma unroll
+      for (int j = 0; j < Q::kLoads; ++j) q.load(j, s, q_stage(lds, s), wave);
+#pragma unroll
+      for (int j = 0; j < P::kLoads; ++j) p.load(j, s, p_stage(lds, s), wave);
+    }
+    // (the sums' first values are in place well before the first product reads them)
+#pragma unroll
+    for (int a = 0; a < MF; ++a)
+#pragma unroll
+      for (int b = 0; b < NF; ++b) asm volatile("" : "+a"(acc[a][b]));
+    meet<(kHeadStages - 1) * kLoads>();
+#pragma unroll
+    for (int b = 0; b < NF; ++b) fp[0][b] = p.fragment(b, p_stage(lds, 0));
+#pragma unroll
+    for (int a = 0; a < MF; ++a) fq[0][a] = q.fragment(a, q_stage(lds, 0));
+    // (up to three steps of zeros behind the last: leaving between the phases costs the loop its registers)
+#pragma unroll 1
+    for (int i = 0; i < steps; i += kHeadStages) {
+      phase<0>(i, lds, wave);
+      phase<1>(i + 1, lds, wave);
+      phase<2>(i + 2, lds, wave);
+      phase<3>(i + 3, lds, wave);
+    }
+    // nothing may still be on its way into LDS when it is used again or given back; the last product takes 8 passes until
+    // its sums can be read
+    meet<0>();
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int a = 0; a < MF; ++a)
+#pragma unroll
+      for (int b = 0; b < NF; ++b) asm volatile("" : "+a"(acc[a][b]));
+  }
+};
+
+}  // namespace npd

@@ -1,0 +1,288 @@
+// What the head operators do row by row around their matrix products: the list of scored positions, packed copies, the logits
+// at labels and teacher ids, and the end of the loss (sums joined, scalars, what the gradient takes away at those ids).
+#include "../../include/npd.h"
+#include "npd_head.hpp"
+
+namespace npd {
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int kScanThreads = 1024;
+
+// One workgroup walks the mask, 16 positions per thread at a time; a position's place is the number of scored ones before it.
+__global__ __launch_bounds__(kScanThreads) void head_scan_kernel(HeadRowsArgs a) {
+  __shared__ int waves[kScanThreads / kWave];
+  constexpr int kEach = 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t before = 0;  // scored positions in front of this stretch (uniform)
+  for (int64_t p0 = 0; p0 < a.T; p0 += kScanThreads * kEach) {
+    const int64_t p = p0 + (int64_t)threadIdx.x * kEach;
+    uint32_t on = 0;
+#pragma unroll
+    for (int t = 0; t < kEach; ++t)
+      if (p + t < a.T && a.mask[p + t]) on |= 1u << t;
+    const int mine = __popc(on);
+    int sum = mine;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const int v = __shfl_up(sum, off, kWave);
+      if (lane >= off) sum += v;
+    }
+    if (lane == 63) waves[wave] = sum;
+    __syncthreads();
+    int64_t at = before + sum - mine;
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kScanThreads / kWave; ++w) {
+      if (w < wave) at += waves[w];
+      all += waves[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kEach; ++t) {
+      if (p + t >= a.T) break;
+      if (on >> t & 1) {
+        a.rows[at++] = (int32_t)(p + t);
+      } else {
+        if (a.kd) a.kd[p + t] = 0.0f;
+        if (a.nll) a.nll[p + t] = 0.0f;
+        if (a.lse) a.lse[p + t] = 0.0f;
+      }
+    }
+    before += all;
+  }
+  if (threadIdx.x == 0) *a.count = (int32_t)before;
+}
+
+// zero rows of the hidden states' gradient at positions that are not scored
+__global__ __launch_bounds__(kRowThreads) void head_zero_kernel(HeadRowsArgs a) {
+  for (int64_t p = blockIdx.x; p < a.T; p += gridDim.x) {
+    if (a.mask[p]) continue;
+    uint16_t* row = a.grad_hidden + p * a.grad_stride;
+    if (((reinterpret_cast<uintptr_t>(row) | (uintptr_t)(2 * a.D)) & 15) == 0) {
+      for (int d = threadIdx.x; d < a.D / 8; d += kRowThreads) reinterpret_cast<uint4*>(row)[d] = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int d = threadIdx.x; d < a.D; d += kRowThreads) row[d] = 0;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kRowThreads) void head_pack_kernel(HeadPackArgs a) {
+  const HeadSpan span = head_span(a.chunk);
+  if (!span.there) return;
+  for (int64_t i = blockIdx.x; i < span.rows; i += gridDim.x) {
+    const int64_t p = a.rows ? (int64_t)a.rows[span.first + i] : span.first + i;
+    const uint16_t* src = a.src + p * a.src_stride;
+    const uint16_t* y = a.y ? a.y + p * a.y_stride : nullptr;
+    uint16_t* dst = a.dst + i * a.dst_stride;
+    const bool vec = !y && (reinterpret_cast<uintptr_t>(src) & 15) == 0;
+    const float inv = a.y ? 1.0f / a.cap : 0.0f;
+    for (int d = threadIdx.x * 8; d < a.width; d += kRowThreads * 8) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (vec && d + 8 <= a.cols) {
+        v = *reinterpret_cast<const uint4*>(src + d);
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          w[t] = d + t < a.cols ? src[d + t] : 0;
+          if (y && d + t < a.cols) {
+            const float f = bf16_one(y[d + t]) * inv;
+            w[t] = one_bf16(bf16_one((uint16_t)w[t]) * __builtin_fmaf(-f, f, 1.0f));
+          }
+        }
+        v = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+      }
+      *reinterpret_cast<uint4*>(dst + d) = v;  // (rows of dst begin on 16 bytes, width is a multiple of eight)
+    }
+  }
+}
+
+// the id that entry j of a row is about: its label (column 0 where there is none), then the teacher's; -1: outside the vocabulary
+__device__ __forceinline__ int entry_id(const HeadLossArgs& a, int64_t p, int j) {
+  const int v = j == 0 ? (a.labels ? a.labels[p] : 0) : a.tidx[p * a.k + j - 1];
+  return v >= 0 && v < a.V ? v : -1;
+}
+
+// Logits at a row's label and ids, a wave per product of two rows, and the row's reference: the largest of them.
+__global__ __launch_bounds__(kRowThreads) void head_gather_kernel(HeadLossArgs a) {
+  __shared__ float tops[kRowThreads / kWave];
+  const HeadSpan span = head_span(a.chunk);
+  const int64_t i = blockIdx.x;
+  if (!span.there || i >= span.rows) return;
+  const int64_t p = a.rows[span.first + i];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint16_t* h = a.h.p + i * a.h.stride;
+  float top = -__builtin_inff();
+  for (int j = wave; j <= a.k; j += kRowThreads / kWave) {
+    const int id = entry_id(a, p, j);
+    float x = __builtin_nanf("");
+    if (id >= 0) {
+      const uint16_t* w = a.w.p + id * a.w.stride;
+      float s = 0.0f;
+      for (int d = lane * 8; d < a.K; d += kWave * 8) {
+        float u[8], v[8];
+        unpack8(*reinterpret_cast<const uint4*>(h + d), u);
+        unpack8(*reinterpret_cast<const uint4*>(w + d), v);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) s = __builtin_fmaf(u[t], v[t], s);
+      }
+      x = wave_sum(s);
+      if (a.bias) x += bf16_one(a.bias[id]);
+      if (a.cap != 0.0f) x = a.cap * tanhf(x / a.cap);
+      top = fmaxf(top, x);
+    }
+    if (lane == 0) a.x[i * (1 + a.k) + j] = x;
+  }
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kRowThreads / kWave; ++w) top = fmaxf(top, tops[w]);
+    const float r = __builtin_rintf(top * a.c);
+    a.r0[i] = r > -1.0e30f && r < 1.0e30f ? r : -1.0e30f;  // (no finite logit: every part takes its own reference)
+  }
+}
+
+// Joins the sums of a row over the vocabulary (part, one pair per 128 columns), writes its scalars, and turns what is kept of it,
+// e = 2^(x c - R), into the gradient up to the row's factor: with w = grad_scale / tau + ce_grad_scale and Z the row's sum
+//   G(v) = w / Z (e(v) - Z / w (grad_scale / tau p_T(v) + ce_grad_scale [v = label])),
+// so that only the entries at the label and the teacher's ids change (they are rounded to bf16 once, from fp32 values).
+__global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a) {
+  __shared__ float fred[3 * kRowThreads / kWave];
+  __shared__ int bad_id;
+  const HeadSpan span = head_span(a.chunk);
+  const int64_t i = blockIdx.x;
+  if (!span.there || i >= span.rows) return;
+  const int64_t p = a.rows[span.first + i];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) bad_id = 0;
+  __syncthreads();
+
+  const float2* part = a.part + i * a.parts;
+  Lse sum[1];
+  sum[0].init();
+  bool apart = false;  // parts with different references
+  const float first = part[0].x;
+  for (int t = threadIdx.x; t < a.parts; t += kRowThreads) {
+    const float2 v = part[t];
+    if (!(v.y == 0.0f)) sum[0].merge(v.x, v.y, 0.0f);
+    apart |= v.x != first;
+  }
+  block_merge<kRowThreads, 1>(sum, fred);
+  const float R = sum[0].r, Z = sum[0].z, lz = __log2f(Z);
+  const bool rescale = a.e && __syncthreads_or(apart || first != R);
+  if (rescale) {  // exact unless it underflows: references are whole numbers
+    for (int t = wave; t < a.parts; t += kRowThreads / kWave) {
+      const float r = part[t].x;
+      if (r == R) continue;
+      const float f = exp2_fast(r - R);
+      uint16_t* e = a.e + i * a.e_stride + t * kHeadPart;
+      const int n = 2 * lane;
+      if (t * kHeadPart + n < a.V) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(e + n);
+        *w = f == 0.0f ? 0u : pack_bf16(bf16_lo(*w) * f, bf16_hi(*w) * f);
+      }
+    }
+    __syncthreads();
+  }
+
+  const float* x = a.x + i * (1 + a.k);
+  const int label = a.labels ? entry_id(a, p, 0) : -1;
+  const bool no_label = a.labels && label < 0;
+  // the teacher's distribution over its ids at this temperature
+  float tmax = -__builtin_inff();
+  for (int j = threadIdx.x; j < a.k; j += kRowThreads) tmax = fmaxf(tmax, a.tval[p * a.k + j]);
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) tmax = fmaxf(tmax, __shfl_xor(tmax, off, kWave));
+  if (lane == 0) fred[wave] = tmax;
+  __syncthreads();
+  tmax = fmaxf(fmaxf(fred[0], fred[1]), fmaxf(fred[2], fred[3]));
+  __syncthreads();
+  float tz = 0.0f;
+  for (int j = threadIdx.x; j < a.k; j += kRowThreads) {
+    tz += exp2_fast((a.tval[p * a.k + j] - tmax) * a.c);
+    if (entry_id(a, p, 1 + j) < 0) bad_id = 1;
+  }
+  tz = block_sum<kRowThreads>(tz, fred);
+  const bool no_id = bad_id != 0;
+  const float ltz = a.k ? __log2f(tz) : 0.0f;
+  const float w = (a.k ? a.kd_weight : 0.0f) + a.ce_weight;
+  const float take = w != 0.0f ? Z / w : 0.0f;
+  float kd = 0.0f;
+  bool at_label = false;
+  for (int j = threadIdx.x; j < a.k; j += kRowThreads) {
+    const int id = entry_id(a, p, 1 + j);
+    if (id < 0) continue;
+    const float lp = __builtin_fmaf(a.tval[p * a.k + j] - tmax, a.c, -ltz), pt = exp2_fast(lp);
+    const float xe = __builtin_fmaf(x[1 + j], a.c, -R);  // log2 of e here
+    // p_T log(p_T / p_S): an id of probability 0 contributes nothing
+    if (pt > 0.0f) kd = __builtin_fmaf(pt, lp - xe + lz, kd);
+    if (a.e) {
+      const bool here = id == label;
+      at_label |= here;
+      float g = exp2_fast(xe) - take * (a.kd_weight * pt + (here ? a.ce_weight : 0.0f));
+      if (a.cap != 0.0f) {
+        const float f = x[1 + j] / a.cap;
+        g *= __builtin_fmaf(-f, f, 1.0f);
+      }
+      a.e[i * a.e_stride + id] = one_bf16(g);
+    }
+  }
+  const bool label_done = __syncthreads_or(at_label);
+  kd = block_sum<kRowThreads>(kd, fred);
+  const bool bad = (no_label && (a.nll || a.ce_weight != 0.0f)) || no_id;
+  if (threadIdx.x == 0) {
+    const float nan = __builtin_nanf("");
+    if (a.e && label >= 0 && !label_done && a.ce_weight != 0.0f) {
+      float g = exp2_fast(__builtin_fmaf(x[0], a.c, -R)) - take * a.ce_weight;
+      if (a.cap != 0.0f) {
+        const float f = x[0] / a.cap;
+        g *= __builtin_fmaf(-f, f, 1.0f);
+      }
+      a.e[i * a.e_stride + label] = one_bf16(g);
+    }
+    if (a.lse) a.lse[p] = (R + lz) * kLn2;
+    if (a.nll) a.nll[p] = no_label ? nan : (__builtin_fmaf(-x[0], a.c, R) + lz) * kLn2;
+    if (a.kd) a.kd[p] = no_id ? nan : kd * kLn2;
+    if (a.status && bad) atomicOr(a.status, (no_label ? NPD_DEV_BAD_LABEL : 0) | (no_id ? NPD_DEV_BAD_TOPK_INDEX : 0));
+    if (a.scale) a.scale[i] = bad ? nan : w / Z;
+  }
+  if (a.hs) {
+    // Rounded to bf16 as an operand of the matrix cores (half a step, like e itself): the row's factor is not known when e is
+    // stored.  A position with a bad label or id is left out of the weights' gradient.
+    const float s = bad ? 0.0f : w / Z;
+    const uint16_t* h = a.h.p + i * a.h.stride;
+    uint16_t* hs = a.hs + i * a.h.stride;
+    for (int d = threadIdx.x * 8; d < a.K; d += kRowThreads * 8) {
+      float v[8];
+      unpack8(*reinterpret_cast<const uint4*>(h + d), v);
+      *reinterpret_cast<uint4*>(hs + d) = bad ? make_uint4(0, 0, 0, 0)
+                                              : make_uint4(pack_bf16(v[0] * s, v[1] * s), pack_bf16(v[2] * s, v[3] * s),
+                                                           pack_bf16(v[4] * s, v[5] * s), pack_bf16(v[6] * s, v[7] * s));
+    }
+  }
+}
+
+unsigned few(int64_t rows) { return (unsigned)(rows < 65536 ? rows : 65536); }
+
+}  // namespace
+
+hipError_t launch_head_rows(const HeadRowsArgs& a, hipStream_t stream) {
+  const hipError_t e = launch_kernel(head_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+  if (e != hipSuccess || !a.grad_hidden) return e;
+  return launch_kernel(head_zero_kernel, dim3(few(a.T)), dim3(kRowThreads), 0, stream, a);
+}
+
+hipError_t launch_head_pack(const HeadPackArgs& a, int64_t rows, hipStream_t stream) {
+  return launch_kernel(head_pack_kernel, dim3(few(rows)), dim3(kRowThreads), 0, stream, a);
+}
+
+hipError_t launch_head_gather(const HeadLossArgs& a, int64_t rows, hipStream_t stream) {
+  return launch_kernel(head_gather_kernel, dim3((unsigned)rows), dim3(kRowThreads), 0, stream, a);
+}
+
+hipError_t launch_head_finish(const HeadLossArgs& a, int64_t rows, hipStream_t stream) {
+  return launch_kernel(head_finish_kernel, dim3((unsigned)rows), dim3(kRowThreads), 0, stream, a);
+}
+
+}  // namespace npd
