@@ -10,6 +10,13 @@ namespace npd {
 
 constexpr int kHeadPart = 128;  // columns of one partial sum of a row: what a wave holds of it
 
+// Workgroups of a kernel whose workgroups take one tile after the other: one per compute unit, whose LDS the stages fill (a
+// multiple of eight, see head_tile).
+inline unsigned head_grid(int64_t tiles) {
+  const int64_t units = compute_units() / 8 * 8;
+  return (unsigned)(tiles < units || units == 0 ? tiles : units);
+}
+
 enum HeadForward { kHeadLogits = 0, kHeadSums = 1, kHeadSumsKept = 2 };
 
 // x = (q w^T + bias), soft-capped, of a chunk of rows; then by HeadForward
@@ -20,7 +27,7 @@ struct HeadForwardArgs {
   HeadChunk chunk;
   HeadMatrix q, w;      // q.rows is the chunk's (set on the device)
   const uint16_t* bias; // or null
-  int32_t K, V;
+  int32_t D, K, V;      // K: D rounded up to eight
   float cap;            // 0: none
   float c;              // log2(e) / tau
   const float* r0;      // [rows] a logit of the row times c, whole, or -1e30: the reference of columns not far above it
@@ -33,24 +40,29 @@ struct HeadForwardArgs {
 };
 hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream);
 
-// out[position of row m][n] = scale[m] sum_k g[m][k] w[k][n], k < K: the gradient of the hidden states.  splits > 1: k in that
-// many pieces, joined by a second kernel through `partial` [splits][cap][N].
+// Rows that are so few that reading the weights is all the time: the weights go straight into registers, at any alignment.
+constexpr int64_t kHeadFewRows = 64;
+hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream);
+
+// out[position of row m][n] = scale[m] sum_k g[m][k] w[k][n], k < K: the gradient of the hidden states.  k may be split into
+// up to `most_splits` pieces, joined by a second kernel through `partial` [splits][rows][up(N, 4)].
 struct HeadHiddenArgs {
   HeadChunk chunk;
   HeadMatrix g, w;
   const float* scale;    // or null: 1
   const int32_t* rows;   // positions of the rows, or null: m itself
-  int32_t K, N, splits;
+  int32_t K, N, most_splits;
   float* partial;
-  int64_t partial_rows;
   uint16_t* out;
   int64_t out_stride;
 };
 hipError_t launch_head_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream);
+// the most pieces that a chunk of up to so many rows is split into, and the floats that they take
 int head_hidden_splits(int64_t rows, int32_t K, int32_t N);
+size_t head_hidden_floats(int64_t rows, int32_t N, int splits);
 
-// out[m][n] = sum_k g[k][m] h[k][n] over the rows k of the chunk, on top of the chunks before it (`partial`, fp32 [M][N]): the
-// gradient of the weights.  `out` is written with the last chunk, on top of what it holds if `accumulate`.
+// out[m][n] = sum_k g[k][m] h[k][n] over the rows k of the chunk, on top of the chunks before it (`partial`, fp32 [M][up(N, 4)]):
+// the gradient of the weights.  `out` is written with the last chunk, on top of what it holds if `accumulate`.
 struct HeadWeightArgs {
   HeadChunk chunk;
   HeadMatrix g, h;
@@ -60,7 +72,7 @@ struct HeadWeightArgs {
   int64_t out_stride;
   int32_t accumulate;
 };
-hipError_t launch_head_weight(const HeadWeightArgs& a, hipStream_t stream);
+hipError_t launch_head_weight(const HeadWeightArgs& a, int64_t chunks, hipStream_t stream);
 
 // out[m] = sum_k scale[k] g[k][m] likewise: the gradient of the bias
 constexpr int kHeadBiasSplits = 32;
@@ -108,9 +120,13 @@ hipError_t launch_head_pack(const HeadPackArgs& a, int64_t rows, hipStream_t str
 struct HeadLossArgs {
   HeadChunk chunk;
   const int32_t* rows;
-  HeadMatrix h, w;       // h: the chunk's rows
+  const uint16_t* src;   // hidden states and weights as the caller has them
+  int64_t src_stride;
+  const uint16_t* weight;
+  int64_t weight_stride;
+  HeadMatrix h;          // packed rows of the chunk
   const uint16_t* bias;
-  int32_t K, V, k;
+  int32_t D, K, V, k;    // K: D rounded up to eight
   float cap, c;
   const int32_t* labels;  // null: not used
   const int32_t* tidx;
@@ -128,6 +144,7 @@ struct HeadLossArgs {
   float* scale;
   uint16_t* hs;                // scaled rows for the weights' gradient, or null
 };
+hipError_t launch_head_prepare(const HeadRowsArgs& r, const HeadLossArgs& a, hipStream_t stream);
 hipError_t launch_head_gather(const HeadLossArgs& a, int64_t rows, hipStream_t stream);
 hipError_t launch_head_finish(const HeadLossArgs& a, int64_t rows, hipStream_t stream);
 

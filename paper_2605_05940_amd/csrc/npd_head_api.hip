@@ -62,6 +62,7 @@ struct Plan {
   int32_t K = 0;          // width, a multiple of eight
   int64_t e_stride = 0;
   int32_t parts = 0, splits = 1;
+  bool few = false;       // rows that head_few_kernel takes
   bool pack_w = false, pack_h = false, pack_g = false;
   size_t rows = 0, count = 0, h = 0, hs = 0, x = 0, r0 = 0, part = 0, e = 0, scale = 0, w = 0, dw = 0, dh = 0, pieces = 0, db = 0;
   size_t bytes = 0;
@@ -73,11 +74,12 @@ Plan make_plan(const npd_head_desc& d, int op, int32_t cap) {
   const int64_t T = d.n_tokens;
   p.K = (int32_t)up(d.width, 8);
   const bool odd = d.width % 8 != 0 || (d.flags & NPD_HEAD_UNALIGNED);
-  p.pack_w = (odd || d.weight_stride % 8 != 0) && (op != NPD_HEAD_LOGITS_BWD || gh);
+  p.few = op != NPD_HEAD_LOGITS_BWD && T <= kHeadFewRows;  // these read weights at any alignment
+  p.pack_w = (odd || d.weight_stride % 8 != 0) && (gh || (op != NPD_HEAD_LOGITS_BWD && !p.few));
   p.pack_g = op == NPD_HEAD_LOGITS_BWD &&
              (d.vocab % 8 != 0 || d.logits_stride % 8 != 0 || (d.flags & NPD_HEAD_UNALIGNED) || d.softcap != 0.0f);
   p.pack_h = op == NPD_HEAD_LOSS ||
-             ((op == NPD_HEAD_LOGITS || gw) && (odd || d.hidden_stride % 8 != 0 || p.pack_g));
+             (((op == NPD_HEAD_LOGITS && !p.few) || gw) && (odd || d.hidden_stride % 8 != 0 || p.pack_g));
   const bool chunked = op == NPD_HEAD_LOSS || p.pack_g;
   p.cap = chunked ? cap : kWhole;
   p.chunk_rows = chunked && T > cap ? cap : T;
@@ -105,8 +107,8 @@ Plan make_plan(const npd_head_desc& d, int op, int32_t cap) {
     if (gw) p.hs = take(C * p.K * 2);
   }
   if (p.pack_g || (op == NPD_HEAD_LOSS && (gh || gw || gb))) p.e = take(C * p.e_stride * 2);
-  if (gw && p.chunks > 1) p.dw = take(V * D * 4);
-  if (gh && p.splits > 1) p.dh = take(p.splits * C * D * 4);
+  if (gw && p.chunks > 1) p.dw = take(V * (size_t)up(D, 4) * 4);
+  if (gh) p.dh = take(head_hidden_floats(p.chunk_rows, d.width, p.splits) * 4);
   if (gb) {
     p.pieces = take(kHeadBiasSplits * V * 4);
     p.db = take(V * 4);
@@ -163,9 +165,8 @@ npd_status gradients(const npd_head_desc& d, const Plan& p, const HeadChunk& chu
     a.rows = rows;
     a.K = d.vocab;
     a.N = d.width;
-    a.splits = p.splits;
+    a.most_splits = p.splits;
     a.partial = reinterpret_cast<float*>(ws + p.dh);
-    a.partial_rows = p.chunk_rows;
     a.out = static_cast<uint16_t*>(grad_hidden);
     a.out_stride = d.grad_hidden_stride;
     NPD_TRY(launch_head_hidden(a, p.chunk_rows, stream));
@@ -181,7 +182,7 @@ npd_status gradients(const npd_head_desc& d, const Plan& p, const HeadChunk& chu
     a.out = static_cast<uint16_t*>(grad_weight);
     a.out_stride = d.grad_weight_stride;
     a.accumulate = accumulate;
-    NPD_TRY(launch_head_weight(a, stream));
+    NPD_TRY(launch_head_weight(a, p.chunks, stream));
   }
   if (grad_bias) {
     HeadBiasArgs a{};
@@ -281,10 +282,15 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   rows.grad_hidden = static_cast<uint16_t*>(grad_hidden);
   rows.grad_stride = d.grad_hidden_stride;
   rows.D = D;
-  NPD_TRY(launch_head_rows(rows, on));
 
+  HeadMatrix w;
+  if ((st = pack_weight(d, p, static_cast<const uint16_t*>(weight), ws, on, &w)) != NPD_OK) return st;
   HeadLossArgs l{};
-  if ((st = pack_weight(d, p, static_cast<const uint16_t*>(weight), ws, on, &l.w)) != NPD_OK) return st;
+  l.src = static_cast<const uint16_t*>(hidden);
+  l.src_stride = d.hidden_stride;
+  l.weight = static_cast<const uint16_t*>(weight);
+  l.weight_stride = d.weight_stride;
+  l.D = D;
   uint16_t* h = reinterpret_cast<uint16_t*>(ws + p.h);
   l.rows = rows.rows;
   l.h = HeadMatrix{h, p.K, (int32_t)p.chunk_rows, p.K};
@@ -315,7 +321,8 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
 
   HeadForwardArgs f{};
   f.q = l.h;
-  f.w = l.w;
+  f.D = D;
+  f.w = w;
   f.bias = l.bias;
   f.K = p.K;
   f.V = V;
@@ -327,26 +334,21 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   f.e = l.e;
   f.e_stride = p.e_stride;
 
-  HeadPackArgs pack{};
-  pack.rows = rows.rows;
-  pack.src = static_cast<const uint16_t*>(hidden);
-  pack.src_stride = d.hidden_stride;
-  pack.cols = D;
-  pack.width = p.K;
-  pack.dst = h;
-  pack.dst_stride = p.K;
-
   const HeadMatrix e = {l.e, p.e_stride, (int32_t)p.chunk_rows, (int32_t)p.e_stride};
   const HeadMatrix hs = {l.hs, p.K, (int32_t)p.chunk_rows, p.K};
   for (int64_t c = 0; c < p.chunks; ++c) {
     const HeadChunk chunk = {rows.count, T, p.cap, (int32_t)c};
-    pack.chunk = l.chunk = f.chunk = chunk;
-    NPD_TRY(launch_head_pack(pack, p.chunk_rows, on));
-    NPD_TRY(launch_head_gather(l, p.chunk_rows, on));
-    NPD_TRY(launch_head_forward(f, grads ? kHeadSumsKept : kHeadSums, p.chunk_rows, on));
+    l.chunk = f.chunk = chunk;
+    if (p.chunks == 1) {
+      NPD_TRY(launch_head_prepare(rows, l, on));
+    } else {
+      if (c == 0) NPD_TRY(launch_head_rows(rows, on));
+      NPD_TRY(launch_head_gather(l, p.chunk_rows, on));
+    }
+    NPD_TRY((p.few ? launch_head_few : launch_head_forward)(f, grads ? kHeadSumsKept : kHeadSums, p.chunk_rows, on));
     NPD_TRY(launch_head_finish(l, p.chunk_rows, on));
     if (!grads) continue;
-    st = gradients(d, p, chunk, e, l.w, hs, l.scale, rows.rows, grad_hidden, grad_weight, grad_bias, ws, on);
+    st = gradients(d, p, chunk, e, w, hs, l.scale, rows.rows, grad_hidden, grad_weight, grad_bias, ws, on);
     if (st != NPD_OK) return st;
   }
   return NPD_OK;
@@ -390,12 +392,13 @@ npd_status npd_head_logits(const npd_head_desc* desc, const void* hidden, const 
     f.q.stride = p.K;
   }
   f.bias = static_cast<const uint16_t*>(bias);
+  f.D = d.width;
   f.K = p.K;
   f.V = d.vocab;
   f.cap = d.softcap;
   f.out = static_cast<uint16_t*>(logits);
   f.out_stride = d.logits_stride;
-  NPD_TRY(launch_head_forward(f, kHeadLogits, T, on));
+  NPD_TRY((p.few ? launch_head_few : launch_head_forward)(f, kHeadLogits, T, on));
   return NPD_OK;
 }
 

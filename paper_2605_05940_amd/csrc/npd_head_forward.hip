@@ -27,15 +27,21 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
   __shared__ __attribute__((aligned(1024))) char lds[Product::kLds];
   const HeadSpan span = head_span(a.chunk);
   if (!span.there || span.rows == 0) return;
-  const HeadTile tile = head_tile(blockIdx.x, (span.rows + Product::kTileM - 1) / Product::kTileM,
-                                  (a.V + Product::kTileN - 1) / Product::kTileN);
+  const int mt = (span.rows + Product::kTileM - 1) / Product::kTileM, nt = (a.V + Product::kTileN - 1) / Product::kTileN;
+  HeadTile tile = head_tile(blockIdx.x, mt, nt);
   if (!tile.there) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  HeadMatrix q = a.q;
+  q.rows = span.rows;
+  Product x;
+  x.start(q, a.w, (int64_t)tile.m * Product::kTileM, (int64_t)tile.n * Product::kTileN, 0, a.K, lds);
+  for (unsigned block = blockIdx.x + gridDim.x; tile.there; block += gridDim.x) {
+  const HeadTile next = head_tile(block, mt, nt);
   const int64_t m0 = (int64_t)tile.m * Product::kTileM;
   const int n0 = tile.n * Product::kTileN;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t mw = m0 + (wave >> 1) * 16 * MF + (lane & 15);  // + 16 i
-  const int nw = n0 + (wave & 1) * 16 * NF + 8 * (lane >> 4);   // + 32 j + 0 .. 7, fragments 2 j and 2 j + 1
-  Product x;
+  const int columns = n0 + (x.wave & 1) * 16 * NF;              // of the wave
+  const int nw = columns + 8 * (lane >> 4);                     // + 32 j + 0 .. 7, fragments 2 j and 2 j + 1
 #pragma unroll
   for (int j = 0; j < NF; ++j) {
     f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -47,14 +53,14 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
 #pragma unroll
     for (int i = 0; i < MF; ++i) x.acc[i][j] = b;
   }
-  HeadMatrix q = a.q;
-  q.rows = span.rows;
-  x.run(q, a.w, m0, n0, 0, a.K, lds);
+  x.run(q, a.w, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, a.K, lds);
+  tile = next;
 
   const SoftCap soft(CAP ? a.cap : 1.0f);
   const bool edge = n0 + Product::kTileN > a.V;  // uniform
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
+    __builtin_amdgcn_sched_barrier(0);  // (a row's sums at a time: the fragments of the next tile are in registers already)
     const int64_t m = mw + 16 * i;
     const bool row = m < span.rows;
     if constexpr (WHAT == kHeadLogits) {
@@ -73,8 +79,8 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
           v[t] = pack_bf16(lo, hi);
         }
         if (!row) continue;
-        if (n + 8 <= a.V && (reinterpret_cast<uintptr_t>(out + n) & 15) == 0) {
-          *reinterpret_cast<uint4*>(out + n) = make_uint4(v[0], v[1], v[2], v[3]);
+        if (columns + 16 * j + 32 <= a.V) {
+          stream8(out + n, make_uint4(v[0], v[1], v[2], v[3]));
         } else {
 #pragma unroll
           for (int t = 0; t < 8; ++t)
@@ -94,11 +100,18 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
             y = soft.cap * th;
             d[4 * j + t] = __builtin_fmaf(-th, th, 1.0f);
           }
-          if (edge && nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) y = -__builtin_inff();
           v[4 * j + t] = y;
-          top = fmaxf(top, y);
         }
       }
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = -__builtin_inff();
+      }
+#pragma unroll
+      for (int p = 0; p < 4 * NF; p += 2) top = max3(top, v[p], v[p + 1]);
       top = fmaxf(top, __shfl_xor(top, 16, kWave));
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
       const float r0 = a.r0[row ? m : 0];
@@ -124,7 +137,7 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
         if constexpr (WHAT == kHeadSumsKept) {
           const int n = nw + 16 * j;
           // (rows of e begin on 16 bytes, n is a multiple of 8)
-          if (row && n < a.e_stride) *reinterpret_cast<uint4*>(e + n) = make_uint4(w[0], w[1], w[2], w[3]);
+          if (row && (columns + 16 * j + 32 <= a.V || n < a.e_stride)) stream8(e + n, make_uint4(w[0], w[1], w[2], w[3]));
         }
       }
       z += __shfl_xor(z, 16, kWave);
@@ -133,6 +146,223 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
       if (lane < 16 && row && part < a.parts) a.part[m * a.parts + part] = make_float2(r, z);
     }
   }
+  }
+}
+
+// The end of a workgroup's 128 columns of up to 64 rows, which lie in LDS as [row][kHeadPart]: a wave per row, two columns per
+// lane.
+template <HeadForward WHAT, bool CAP>
+__device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const float* x, int rows) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const SoftCap soft(CAP ? a.cap : 1.0f);
+  const int n = blockIdx.x * kHeadPart + 2 * lane;
+  float bias[2] = {0.0f, 0.0f};
+  if (a.bias) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) bias[e] = n + e < a.V ? bf16_one(a.bias[n + e]) : 0.0f;
+  }
+  for (int m = wave; m < rows; m += kHeadThreads / kWave) {
+    float y[2], slope[2] = {1.0f, 1.0f};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      y[e] = x[m * kHeadPart + 2 * lane + e] + bias[e];
+      if constexpr (CAP) {
+        const float th = soft.tanh_of(y[e]);
+        y[e] = soft.cap * th;
+        slope[e] = __builtin_fmaf(-th, th, 1.0f);
+      }
+    }
+    if constexpr (WHAT == kHeadLogits) {
+      uint16_t* out = a.out + m * a.out_stride + n;
+      const uint32_t v = pack_bf16(y[0], y[1]);
+      if (n + 2 <= a.V)
+        __builtin_memcpy(out, &v, 4);
+      else if (n < a.V)
+        *out = (uint16_t)v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (n + e >= a.V) y[e] = -__builtin_inff();
+      float top = fmaxf(y[0], y[1]);
+#pragma unroll
+      for (int off = kWave / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+      const float r0 = a.r0[m], u = top * a.c;
+      const float r = u > r0 + kHeadHeadroom ? __builtin_rintf(u) : r0;
+      float g[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) g[e] = exp2_fast(__builtin_fmaf(y[e], a.c, -r));
+      const float z = wave_sum(g[0] + g[1]);
+      if constexpr (WHAT == kHeadSumsKept) {
+        // (a part's columns end within the row: its pitch is a multiple of 64 that covers V)
+        if (n < a.e_stride) *reinterpret_cast<uint32_t*>(a.e + m * a.e_stride + n) = pack_bf16(g[0] * slope[0], g[1] * slope[1]);
+      }
+      if (lane == 0) a.part[(int64_t)m * a.parts + blockIdx.x] = make_float2(r, z);
+    }
+  }
+}
+
+// Up to 4 NT rows, where reading the weights is all the time.  v_mfma_f32_4x4x4_16b_bf16 is 16 products of 4 x 4 at once; here they
+// are 16 pieces of k of the same four columns and four rows, added up at the end, so that one load of a wave is 256 consecutive
+// bytes of each of four rows of the weights.  That is what decides: reading 151,936 x 2,048 alone (MI355X) takes 126 us in pieces of 64 bytes
+// of 16 rows, 105 in pieces of 256 of four, 91 if the caches are told that nothing is read twice, as here; waves begin at
+// different places of their rows and wrap around, since rows of a power of two of bytes would else be read out of few memory
+// channels (126 us: 145).  A workgroup has 128 columns, a wave 4 G of them at a time.
+template <int NT, int G, HeadForward WHAT, bool CAP>
+__global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_kernel(HeadForwardArgs a) {
+  __shared__ __attribute__((aligned(16))) float x[4 * NT][kHeadPart];
+  const HeadSpan span = head_span(a.chunk);
+  if (span.rows == 0) return;
+  typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 3, b = lane >> 2;
+  constexpr int kBlock = 128;  // values of k per load
+  const int blocks = a.D / kBlock, tail = blocks * kBlock + 8 * b;
+  const uint16_t* h[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int m = 4 * t + i;
+    h[t] = a.q.p + (int64_t)(m < span.rows ? m : span.rows - 1) * a.q.stride;
+  }
+  for (int part = 0; part < 32 / (4 * G); ++part) {
+    const int c0 = wave * 32 + part * 4 * G;  // of the workgroup's columns
+    const uint16_t* w[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int v = blockIdx.x * kHeadPart + c0 + 4 * g + i;
+      w[g] = a.w.p + (int64_t)(v < a.V ? v : a.V - 1) * a.w.stride;
+    }
+    f32x4 acc[G][NT];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[g][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](const uint4 (&wv)[G], const uint4 (&hv)[NT]) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          acc[g][t] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, make_uint2(wv[g].x, wv[g].y)),
+                                                             __builtin_bit_cast(s16x4, make_uint2(hv[t].x, hv[t].y)), acc[g][t], 0, 0, 0);
+          acc[g][t] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, make_uint2(wv[g].z, wv[g].w)),
+                                                             __builtin_bit_cast(s16x4, make_uint2(hv[t].z, hv[t].w)), acc[g][t], 0, 0, 0);
+        }
+    };
+    int at = blocks ? (int)((blockIdx.x * 4 + wave) % (unsigned)blocks) : 0;
+    for (int n = 0; n < blocks; ++n) {
+      const int d = at * kBlock + 8 * b;
+      at = at + 1 == blocks ? 0 : at + 1;
+      uint4 wv[G], hv[NT];
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const words v = __builtin_nontemporal_load(reinterpret_cast<const words*>(w[g] + d));
+        wv[g] = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) hv[t] = load8(h[t] + d);
+      multiply(wv, hv);
+    }
+    if (tail - 8 * b < a.D) {  // uniform
+      uint4 wv[G], hv[NT];
+#pragma unroll
+      for (int g = 0; g < G; ++g) wv[g] = load8_of(w[g], tail, a.D);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) hv[t] = load8_of(h[t], tail, a.D);
+      multiply(wv, hv);
+    }
+    // acc[g][t][e] of lane (b, i): column 4 g + e, row 4 t + i, piece b of k
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int off = 4; off < kWave; off <<= 1)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[g][t][e] += __shfl_xor(acc[g][t][e], off, kWave);
+        if (b == g) *reinterpret_cast<f32x4*>(&x[4 * t + i][c0 + 4 * g]) = acc[g][t];
+      }
+  }
+  __syncthreads();
+  finish_columns<WHAT, CAP>(a, &x[0][0], span.rows);
+}
+
+// The same for up to 16 RT rows: a wave reads the weights of 32 columns straight into the fragments of 16 x 16 x 32 products (64
+// bytes of 16 rows per load, the next 64 with the one after it: 5 TB/s).
+template <int RT, HeadForward WHAT, bool CAP>
+__global__ __launch_bounds__(kHeadThreads, RT == 2 ? 4 : 3) void head_few_kernel(HeadForwardArgs a) {
+  __shared__ __attribute__((aligned(16))) float x[16 * RT][kHeadPart];
+  const HeadSpan span = head_span(a.chunk);
+  if (span.rows == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int v0 = blockIdx.x * kHeadPart + wave * 32;
+  constexpr int kAhead = 4;  // steps requested together
+  const uint16_t* w[2];
+  const uint16_t* h[RT];
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    const int v = v0 + 16 * f + i;
+    w[f] = a.w.p + (int64_t)(v < a.V ? v : a.V - 1) * a.w.stride;
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int m = 16 * t + i;
+    h[t] = a.q.p + (int64_t)(m < span.rows ? m : span.rows - 1) * a.q.stride;
+  }
+  f32x4 acc[2][RT];
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int blocks = a.D / (kAhead * kHeadStep);
+  int at = blocks ? (int)((blockIdx.x * 4 + wave) % (unsigned)blocks) : 0;
+  for (int b = 0; b < blocks; ++b) {
+    const int d = at * kAhead * kHeadStep + 8 * g;
+    at = at + 1 == blocks ? 0 : at + 1;
+    bf16x8 wv[kAhead][2], y[kAhead][RT];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8(w[f] + d + s * kHeadStep));
+    }
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) y[s][t] = __builtin_bit_cast(bf16x8, load8(h[t] + d + s * kHeadStep));
+    }
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s][f], y[s][t], acc[f][t], 0, 0, 0);
+  }
+  for (int d = blocks * kAhead * kHeadStep + 8 * g; d - 8 * g < a.D; d += kHeadStep) {
+    bf16x8 wv[2], y[RT];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) wv[f] = __builtin_bit_cast(bf16x8, load8_of(w[f], d, a.D));
+#pragma unroll
+    for (int t = 0; t < RT; ++t) y[t] = __builtin_bit_cast(bf16x8, load8_of(h[t], d, a.D));
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[f], y[t], acc[f][t], 0, 0, 0);
+  }
+
+  // acc[f][t][e]: row 16 t + i, column v0 + 16 f + 4 g + e
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<f32x4*>(&x[16 * t + i][wave * 32 + 16 * f + 4 * g]) = acc[f][t];
+  __syncthreads();
+  finish_columns<WHAT, CAP>(a, &x[0][0], span.rows);
+}
+
+template <HeadForward WHAT, bool CAP>
+hipError_t launch_few(const HeadForwardArgs& a, int64_t rows, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.V + kHeadPart - 1) / kHeadPart)), block(kHeadThreads);
+  if (rows <= 4) return launch_kernel(head_tokens_kernel<1, 8, WHAT, CAP>, grid, block, 0, stream, a);
+  if (rows <= 8) return launch_kernel(head_tokens_kernel<2, 8, WHAT, CAP>, grid, block, 0, stream, a);
+  if (rows <= 16) return launch_kernel(head_tokens_kernel<4, 4, WHAT, CAP>, grid, block, 0, stream, a);
+  if (rows <= 32) return launch_kernel(head_few_kernel<2, WHAT, CAP>, grid, block, 0, stream, a);
+  return launch_kernel(head_few_kernel<4, WHAT, CAP>, grid, block, 0, stream, a);
 }
 
 template <int MF, HeadForward WHAT, bool CAP>
@@ -141,7 +371,7 @@ hipError_t launch(const HeadForwardArgs& a, int64_t rows, hipStream_t stream) {
   const int64_t mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.V + Product::kTileN - 1) / Product::kTileN;
   const int64_t blocks = (mt * nt + 7) / 8 * 8;
   if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-  return launch_kernel(head_forward_kernel<MF, 8, WHAT, CAP>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
+  return launch_kernel(head_forward_kernel<MF, 8, WHAT, CAP>, dim3(head_grid(blocks)), dim3(kHeadThreads), 0, stream, a);
 }
 
 template <int MF>
@@ -156,8 +386,16 @@ hipError_t launch_rows(const HeadForwardArgs& a, HeadForward what, int64_t rows,
 
 }  // namespace
 
+hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream) {
+  const bool cap = a.cap != 0.0f;
+  switch (what) {
+    case kHeadLogits: return cap ? launch_few<kHeadLogits, true>(a, rows, stream) : launch_few<kHeadLogits, false>(a, rows, stream);
+    case kHeadSums: return cap ? launch_few<kHeadSums, true>(a, rows, stream) : launch_few<kHeadSums, false>(a, rows, stream);
+    default: return cap ? launch_few<kHeadSumsKept, true>(a, rows, stream) : launch_few<kHeadSumsKept, false>(a, rows, stream);
+  }
+}
+
 hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream) {
-  if (rows <= 64) return launch_rows<2>(a, what, rows, stream);
   if (rows <= 128) return launch_rows<4>(a, what, rows, stream);
   return launch_rows<8>(a, what, rows, stream);
 }

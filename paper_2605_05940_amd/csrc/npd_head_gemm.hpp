@@ -19,6 +19,7 @@
 namespace npd {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kHeadStep = 32;      // values of k per step
@@ -81,6 +82,29 @@ __device__ __forceinline__ HeadTile head_tile(unsigned block, int mt, int nt) {
 
 #define NPD_LDS __attribute__((address_space(3)))
 
+// Eight or four bf16 values at any even address: one access of 16 or 8 bytes, which global memory takes at any alignment.
+__device__ __forceinline__ uint4 load8(const uint16_t* p) {
+  uint4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+__device__ __forceinline__ void store8(uint16_t* p, const uint4& v) { __builtin_memcpy(p, &v, 16); }
+// the same for what is not read again soon: it does not push the operands of the products out of the L2
+__device__ __forceinline__ void stream8(uint16_t* p, const uint4& v) {
+  typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+  __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, reinterpret_cast<words*>(p));
+}
+__device__ __forceinline__ void store4(uint16_t* p, const uint2& v) { __builtin_memcpy(p, &v, 8); }
+// values [d, d + 8) of a row of `cols`, 0 behind its end
+__device__ __forceinline__ uint4 load8_of(const uint16_t* row, int d, int cols) {
+  if (d + 8 <= cols) return load8(row + d);
+  uint32_t w[4] = {};
+#pragma unroll
+  for (int t = 0; t < 8; ++t)
+    if (d + t < cols) w[t >> 1] |= (uint32_t)row[d + t] << (16 * (t & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // 16-byte groups of a KC tile's rows (64 bytes: four groups) are stored at group ^ kc_swizzle(row): the lanes of a fragment
 // read that are served together (four runs of four lanes of two groups) then hit 16 different groups of the 64 banks, in both
 // row orders below
@@ -94,23 +118,21 @@ __device__ __forceinline__ int ks_swizzle(int k) { return (k & 3) | ((k >> 3) & 
 
 constexpr uint32_t kHeadRecords = 0x80000000u;  // bytes behind a tile's base that loads may reach; at offsets from here on they give 0
 
-// One operand's side of a tile: F fragments of 16 rows (or columns) for each of two waves, 32 F in all.  PAIRED: fragments 2j and
-// 2j + 1 take turns over groups of four rows, so that a lane's sums of the two are eight neighbours.
-template <int F, bool KS, bool PAIRED>
-struct HeadSide {
+// Where one operand's values of a tile come from: F fragments of 16 rows (or columns) for each of two waves, 32 F in all.
+template <int F, bool KS>
+struct HeadSource {
   static_assert(F % 2 == 0, "loads are whole waves");
-  static constexpr int kLoads = F / 2;            // 16-byte loads per lane and step
+  static constexpr int kLoads = F / 2;                   // 16-byte loads per lane and step
   static constexpr int kBytes = F * 32 * kHeadStep * 2;  // of a step
-  static constexpr int kGran = 2 * F;             // granules of a KS row
+  static constexpr int kGran = 2 * F;                    // granules of a KS row
   const uint16_t* base;  // uniform
   int64_t step;          // elements between steps
   uint32_t off[kLoads];
   int kpos[2];           // KC: k of the lane's loads within a step (of even and odd ones)
   uint32_t pitch;        // KS: bytes between rows
-  uint32_t rd[KS ? F : 2];  // where this lane's fragments begin within a step's bytes
   int kend;
 
-  __device__ __forceinline__ void init(const HeadMatrix& x, int64_t tile0, int64_t k0, int64_t k1, int wave, int half) {
+  __device__ __forceinline__ void init(const HeadMatrix& x, int64_t tile0, int64_t k0, int64_t k1, int wave) {
     const int lane = threadIdx.x & 63;
     kend = (int)(k1 - k0);
     if constexpr (!KS) {
@@ -124,12 +146,6 @@ struct HeadSide {
         off[j] = (uint32_t)((row < most ? row : most) * x.stride * 2 + group * 16);
         if (j < 2) kpos[j] = group * 8;  // (rows of loads j and j + 2 are 32 apart: the same swizzle)
       }
-      const int i = lane & 15, g = lane >> 4;
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int row = PAIRED ? 8 * (i >> 2) + 4 * f + (i & 3) : 16 * f + i;
-        rd[f] = (uint32_t)((half * F * 16 + row) * 64 + (g ^ kc_swizzle(row)) * 16);
-      }
     } else {
       base = x.p + k0 * x.stride + tile0;
       step = (int64_t)kHeadStep * x.stride;
@@ -142,14 +158,10 @@ struct HeadSide {
         const int64_t col = gran * 16 + (group & 1) * 8, most = x.cols - 8 - tile0;
         off[j] = (uint32_t)(k * x.stride * 2 + (col < most ? col : most) * 2);
       }
-      const int i = lane & 15, g = lane >> 4, k = 8 * g + (i >> 2);
-#pragma unroll
-      for (int f = 0; f < F; ++f)
-        rd[f] = (uint32_t)(k * 64 * F + ((half * F + f) ^ (ks_swizzle(k) & (kGran - 1))) * 32 + (i & 3) * 8);
     }
   }
 
-  // requests load j of step `s` into `to` (this operand's bytes of the stage)
+  // requests load j of step `s` into `to` (this operand's bytes of the stage); zeros behind the last step
   __device__ __forceinline__ void load(int j, int s, char* to, int wave) const {
     const int left = kend - s * kHeadStep;  // uniform
     uint32_t o = off[j], records = kHeadRecords;
@@ -166,6 +178,29 @@ struct HeadSide {
     const uint32_t lds = (uint32_t)(uintptr_t)(NPD_LDS char*)(to + (wave * kLoads + j) * 1024);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(o), "s"(r) : "memory");
   }
+};
+
+// Where a wave's fragments lie in a step's bytes.  PAIRED: fragments 2j and 2j + 1 take turns over groups of four rows, so that a
+// lane's sums of the two are eight neighbours.
+template <int F, bool KS, bool PAIRED>
+struct HeadReader {
+  uint32_t rd[KS ? F : 2];
+
+  __device__ __forceinline__ void init(int half) {
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    if constexpr (!KS) {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const int row = PAIRED ? 8 * (i >> 2) + 4 * f + (i & 3) : 16 * f + i;
+        rd[f] = (uint32_t)((half * F * 16 + row) * 64 + (g ^ kc_swizzle(row)) * 16);
+      }
+    } else {
+      const int k = 8 * g + (i >> 2);
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+        rd[f] = (uint32_t)(k * 64 * F + ((half * F + f) ^ (ks_swizzle(k) & (2 * F - 1))) * 32 + (i & 3) * 8);
+    }
+  }
 
   __device__ __forceinline__ bf16x8 fragment(int f, const char* from) const {
     if constexpr (!KS) {
@@ -179,19 +214,24 @@ struct HeadSide {
   }
 };
 
-// The sums of a tile of 32 MF rows by 32 NF columns.  acc[i][j][e]: row m = 16 i + (lane & 15) of the wave's 16 MF, column
-// 16 j + 4 (lane >> 4) + e of its 16 NF (PAIRED: 32 (j / 2) + 8 (lane >> 4) + 4 (j & 1) + e).
+// The sums of tiles of 32 MF rows by 32 NF columns, one after the other: start() with the first, then for every tile run(), which
+// requests the next one's first steps while it works on its own last ones, so that they are there when the tile's sums
+// have been dealt with.  acc[i][j][e]: row m = 16 i + (lane & 15) of the wave's 16 MF, column 16 j + 4 (lane >> 4) + e of its
+// 16 NF (PAIRED: 32 (j / 2) + 8 (lane >> 4) + 4 (j & 1) + e).
 template <int MF, int NF, bool QKS, bool PKS, bool PAIRED>
 struct HeadProduct {
-  using Q = HeadSide<MF, QKS, false>;
-  using P = HeadSide<NF, PKS, PAIRED>;
+  using Q = HeadSource<MF, QKS>;
+  using P = HeadSource<NF, PKS>;
   static constexpr int kLds = kHeadStages * (Q::kBytes + P::kBytes);
   static constexpr int kTileM = 32 * MF, kTileN = 32 * NF;
   static constexpr int kLoads = Q::kLoads + P::kLoads;
   f32x4 acc[MF][NF];
   Q q;
   P p;
+  HeadReader<MF, QKS, false> qr;
+  HeadReader<NF, PKS, PAIRED> pr;
   bf16x8 fq[2][MF], fp[2][NF];
+  int steps, wave;
 
   template <int LEFT>
   static __device__ __forceinline__ void meet() {
@@ -205,8 +245,15 @@ struct HeadProduct {
   static __device__ __forceinline__ char* q_stage(char* lds, int s) { return lds + s * Q::kBytes; }
   static __device__ __forceinline__ char* p_stage(char* lds, int s) { return lds + kHeadStages * Q::kBytes + s * P::kBytes; }
 
+  // acc += p q, written out so that the sums stay where they are (256 registers of sums leave the compiler none to move them
+  // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one)
+  static __device__ __forceinline__ void multiply(f32x4& c, const bf16x8& a, const bf16x8& b) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  }
+
+  // One step, in stage S; requests step `ahead` of (nq, np) into the same stage.
   template <int S>
-  __device__ __forceinline__ void phase(int i, char* lds, int wave) {
+  __device__ __forceinline__ void phase(const Q& nq, const P& np, int ahead, char* lds) {
     constexpr int cur = S & 1, nxt = cur ^ 1, sn = (S + 1) % kHeadStages;
     meet<(kHeadStages - 2) * kLoads>();
     constexpr int kReads = MF + NF, kSteps = MF * NF;
@@ -219,16 +266,16 @@ struct HeadProduct {
         // loads and reads are spread over the first three quarters of the step's matrix instructions
         while (load < kLoads && load * (kSteps * 3 / 4) <= done * kLoads) {
           if (load < Q::kLoads)
-            q.load(load, i + kHeadStages, q_stage(lds, S), wave);
+            nq.load(load, ahead, q_stage(lds, S), wave);
           else
-            p.load(load - Q::kLoads, i + kHeadStages, p_stage(lds, S), wave);
+            np.load(load - Q::kLoads, ahead, p_stage(lds, S), wave);
           ++load;
         }
         while (read < kReads && read * (kSteps * 3 / 4) <= done * kReads) {
           if (read < NF)
-            fp[nxt][read] = p.fragment(read, p_stage(lds, sn));
+            fp[nxt][read] = pr.fragment(read, p_stage(lds, sn));
           else
-            fq[nxt][read - NF] = q.fragment(read - NF, q_stage(lds, sn));
+            fq[nxt][read - NF] = qr.fragment(read - NF, q_stage(lds, sn));
           ++read;
         }
         multiply(acc[a][b], fp[cur][b], fq[cur][a]);
@@ -237,20 +284,15 @@ struct HeadProduct {
     }
   }
 
-  // acc += p q, written out so that the sums stay where they are (256 registers of sums leave the compiler none to move them
-  // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one)
-  static __device__ __forceinline__ void multiply(f32x4& c, const bf16x8& a, const bf16x8& b) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
-  }
-
-  // adds the products of k in [k0, k1) to acc
-  __device__ __forceinline__ void run(const HeadMatrix& qm, const HeadMatrix& pm, int64_t m0, int64_t n0, int64_t k0, int64_t k1,
-                                      char* lds) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    q.init(qm, m0, k0, k1, wave, wave >> 1);
-    p.init(pm, n0, k0, k1, wave, wave & 1);
-    const int steps = (int)((k1 - k0 + kHeadStep - 1) / kHeadStep);
-    if (steps <= 0) return;
+  // the first tile: rows m0, columns n0, k in [k0, k1)
+  __device__ __forceinline__ void start(const HeadMatrix& qm, const HeadMatrix& pm, int64_t m0, int64_t n0, int64_t k0, int64_t k1,
+                                        char* lds) {
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    steps = (int)((k1 - k0 + kHeadStep - 1) / kHeadStep);
+    q.init(qm, m0, k0, k1, wave);
+    p.init(pm, n0, k0, k1, wave);
+    qr.init(wave >> 1);
+    pr.init(wave & 1);
 #pragma unroll
     for (int s = 0; s < kHeadStages; ++s) {
 #pragma unroll
@@ -258,27 +300,42 @@ struct HeadProduct {
 #pragma unroll
       for (int j = 0; j < P::kLoads; ++j) p.load(j, s, p_stage(lds, s), wave);
     }
+    meet<(kHeadStages - 1) * kLoads>();
+#pragma unroll
+    for (int b = 0; b < NF; ++b) fp[0][b] = pr.fragment(b, p_stage(lds, 0));
+#pragma unroll
+    for (int a = 0; a < MF; ++a) fq[0][a] = qr.fragment(a, q_stage(lds, 0));
+  }
+
+  // adds the current tile's products to acc; the tile at (m0, n0) of the same k is the next one if `more`
+  __device__ __forceinline__ void run(const HeadMatrix& qm, const HeadMatrix& pm, bool more, int64_t m0, int64_t n0, int64_t k0,
+                                      int64_t k1, char* lds) {
     // (the sums' first values are in place well before the first product reads them)
 #pragma unroll
     for (int a = 0; a < MF; ++a)
 #pragma unroll
       for (int b = 0; b < NF; ++b) asm volatile("" : "+a"(acc[a][b]));
-    meet<(kHeadStages - 1) * kLoads>();
-#pragma unroll
-    for (int b = 0; b < NF; ++b) fp[0][b] = p.fragment(b, p_stage(lds, 0));
-#pragma unroll
-    for (int a = 0; a < MF; ++a) fq[0][a] = q.fragment(a, q_stage(lds, 0));
     // (up to three steps of zeros behind the last: leaving between the phases costs the loop its registers)
+    int i = 0;
 #pragma unroll 1
-    for (int i = 0; i < steps; i += kHeadStages) {
-      phase<0>(i, lds, wave);
-      phase<1>(i + 1, lds, wave);
-      phase<2>(i + 2, lds, wave);
-      phase<3>(i + 3, lds, wave);
+    for (; i + kHeadStages < steps; i += kHeadStages) {
+      phase<0>(q, p, i + kHeadStages, lds);
+      phase<1>(q, p, i + kHeadStages + 1, lds);
+      phase<2>(q, p, i + kHeadStages + 2, lds);
+      phase<3>(q, p, i + kHeadStages + 3, lds);
     }
-    // nothing may still be on its way into LDS when it is used again or given back; the last product takes 8 passes until
-    // its sums can be read
-    meet<0>();
+    if (more) {
+      q.init(qm, m0, k0, k1, wave);
+      p.init(pm, n0, k0, k1, wave);
+    } else {
+      q.kend = p.kend = 0;  // (zeros, so that the waits count alike)
+    }
+    phase<0>(q, p, 0, lds);
+    phase<1>(q, p, 1, lds);
+    phase<2>(q, p, 2, lds);
+    phase<3>(q, p, 3, lds);
+    // nothing may still be on its way into LDS when it is given back; the last product takes 8 passes until its sums can be read
+    if (!more) meet<0>();
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
     for (int a = 0; a < MF; ++a)

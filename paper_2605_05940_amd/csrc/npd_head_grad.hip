@@ -5,14 +5,66 @@
 namespace npd {
 namespace {
 
-__device__ __forceinline__ void store4(uint16_t* out, int n, int N, const float v[4]) {
-  if (n + 4 <= N && (reinterpret_cast<uintptr_t>(out + n) & 7) == 0) {
-    *reinterpret_cast<uint2*>(out + n) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+// four neighbouring columns of a row of N
+__device__ __forceinline__ void store_columns(uint16_t* out, int n, int N, const f32x4& v) {
+  if (n + 4 <= N) {
+    store4(out + n, make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])));
   } else {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
       if (n + t < N) out[n + t] = one_bf16(v[t]);
   }
+}
+// the same of fragments j and j + 1 (columns n and n + 16 of this lane, neighbours' between them): lanes 16 apart exchange halves,
+// so that each stores eight neighbouring columns and the four lanes of a row 64 bytes
+// (`whole`, the same for the wave: all 32 columns are there)
+__device__ __forceinline__ void store_two(uint16_t* out, int n, int N, bool whole, const f32x4& a, const f32x4& b) {
+  const uint32_t a0 = pack_bf16(a[0], a[1]), a1 = pack_bf16(a[2], a[3]), b0 = pack_bf16(b[0], b[1]), b1 = pack_bf16(b[2], b[3]);
+  const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a0, b0, false, false));
+  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a1, b1, false, false));
+  const int at = n + (threadIdx.x & 16 ? 12 : 0);
+  const uint32_t v[4] = {x[0], y[0], x[1], y[1]};
+  if (whole) {
+    store8(out + at, make_uint4(v[0], v[1], v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (at + t < N) out[at + t] = (uint16_t)(v[t >> 1] >> (16 * (t & 1)));
+  }
+}
+__device__ __forceinline__ f32x4 load_columns(const uint16_t* in, int n, int N) {
+  f32x4 v;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) v[t] = n + t < N ? bf16_one(in[n + t]) : 0.0f;
+  return v;
+}
+
+// How many pieces the contraction over K is split into.  A compute unit has one tile at a time, so `tiles` in s pieces take
+// ceil(tiles s / 256) rounds of K / s and what a tile costs besides (about 14 steps of 32, of which a step takes 0.8 us); the pieces are written and
+// read once more, at about 4 bytes per ns.  130 tiles of 1,152 columns over 262,144 (6,554 rows): 5.0 ms in one piece.
+constexpr int kUnits = 256;
+__host__ __device__ inline int hidden_pieces(int tiles, int64_t rows, int K, int N, int most) {
+  const int steps = (K + kHeadStep - 1) / kHeadStep;
+  const int64_t join = rows * N * 8 / 3200 + 4000;  // of one piece, in 1/1000 steps
+  int best = 1;
+  int64_t least = (int64_t)((tiles + kUnits - 1) / kUnits) * (steps + 14) * 1000;
+  for (int s = 2; s <= most; s += s < 8 ? 1 : s < 16 ? 2 : s < 64 ? 8 : 32) {
+    if (steps / s < 4) break;
+    const int64_t t = ((int64_t)tiles * s + kUnits - 1) / kUnits * ((steps + s - 1) / s + 14) * 1000 + join * s + 5000;
+    if (t < least) {
+      least = t;
+      best = s;
+    }
+  }
+  return best;
+}
+__host__ __device__ inline int pitch4(int n) { return (n + 3) / 4 * 4; }
+
+template <int MF, int NF>
+__device__ __forceinline__ int pieces_of(const HeadHiddenArgs& a, int rows) {
+  using Product = HeadProduct<MF, NF, false, true, false>;
+  const int mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
+  return hidden_pieces(mt * nt, rows, a.K, a.N, a.most_splits);
 }
 
 template <int MF, int NF>
@@ -23,9 +75,10 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHidden
   if (!span.there || span.rows == 0) return;
   const int mt = (span.rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
   // a piece of k after the other (tiles of one piece share its rows of w)
+  const int pieces = hidden_pieces(mt * nt, span.rows, a.K, a.N, a.most_splits);
   const unsigned per = (unsigned)(mt * nt + 7) / 8 * 8;
   const int split = (int)(blockIdx.x / per);
-  if (split >= a.splits) return;
+  if (split >= pieces) return;
   const HeadTile tile = head_tile(blockIdx.x % per, mt, nt);
   if (!tile.there) return;
   const int64_t m0 = (int64_t)tile.m * Product::kTileM;
@@ -34,7 +87,7 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHidden
   // pieces of whole rounds of the stages
   constexpr int kRound = kHeadStep * kHeadStages;
   const int rounds = (a.K + kRound - 1) / kRound;
-  const int64_t k0 = (int64_t)rounds * split / a.splits * kRound, k1 = (int64_t)rounds * (split + 1) / a.splits * kRound;
+  const int64_t k0 = (int64_t)rounds * split / pieces * kRound, k1 = (int64_t)rounds * (split + 1) / pieces * kRound;
   Product x;
 #pragma unroll
   for (int i = 0; i < MF; ++i)
@@ -42,92 +95,99 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHidden
     for (int j = 0; j < NF; ++j) x.acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   HeadMatrix g = a.g;
   g.rows = span.rows;
-  x.run(g, a.w, m0, n0, k0, k1 < a.K ? k1 : a.K, lds);
+  x.start(g, a.w, m0, n0, k0, k1 < a.K ? k1 : a.K, lds);
+  x.run(g, a.w, false, 0, 0, 0, 0, lds);
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
     const int64_t m = m0 + (wave >> 1) * 16 * MF + 16 * i + (lane & 15);
     if (m >= span.rows) continue;
-    const int nw = n0 + (wave & 1) * 16 * NF + 4 * (lane >> 4);
-    if (a.splits > 1) {
-      float* out = a.partial + (split * a.partial_rows + m) * a.N;
+    const int columns = n0 + (x.wave & 1) * 16 * NF, nw = columns + 4 * (lane >> 4);
+    if (pieces > 1) {
+      float* out = a.partial + ((int64_t)split * span.rows + m) * pitch4(a.N);
 #pragma unroll
       for (int j = 0; j < NF; ++j)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (nw + 16 * j + t < a.N) out[nw + 16 * j + t] = x.acc[i][j][t];
+        if (columns + 16 * j + 16 <= a.N || nw + 16 * j < a.N) *reinterpret_cast<f32x4*>(out + nw + 16 * j) = x.acc[i][j];
     } else {
       const float s = a.scale ? a.scale[m] : 1.0f;
       uint16_t* out = a.out + (a.rows ? (int64_t)a.rows[span.first + m] : span.first + m) * a.out_stride;
 #pragma unroll
-      for (int j = 0; j < NF; ++j) {
-        const float v[4] = {x.acc[i][j][0] * s, x.acc[i][j][1] * s, x.acc[i][j][2] * s, x.acc[i][j][3] * s};
-        store4(out, nw + 16 * j, a.N, v);
-      }
+      for (int j = 0; j < NF; j += 2) store_two(out, nw + 16 * j, a.N, columns + 16 * j + 32 <= a.N, x.acc[i][j] * s, x.acc[i][j + 1] * s);
     }
   }
 }
 
 // joins the pieces of head_hidden_kernel in their order
+template <int MF, int NF>
 __global__ __launch_bounds__(256) void head_join_kernel(HeadHiddenArgs a) {
   const HeadSpan span = head_span(a.chunk);
-  if (!span.there) return;
-  for (int64_t m = blockIdx.x; m < span.rows; m += gridDim.x) {
+  if (!span.there || span.rows == 0) return;
+  const int pieces = pieces_of<MF, NF>(a, span.rows);
+  if (pieces == 1) return;
+  const int pitch = pitch4(a.N), quads = pitch / 4;
+  const int64_t all = (int64_t)span.rows * quads;
+  for (int64_t q = blockIdx.x * 256ll + threadIdx.x; q < all; q += gridDim.x * 256ll) {
+    const int64_t m = q / quads;
+    const int n = (int)(q - m * quads) * 4;
+    const float* at = a.partial + m * pitch + n;
+    f32x4 v = *reinterpret_cast<const f32x4*>(at);
+#pragma unroll 4
+    for (int p = 1; p < pieces; ++p) v += *reinterpret_cast<const f32x4*>(at + (int64_t)p * span.rows * pitch);
     const float s = a.scale ? a.scale[m] : 1.0f;
-    uint16_t* out = a.out + (a.rows ? (int64_t)a.rows[span.first + m] : span.first + m) * a.out_stride;
-    for (int n = threadIdx.x; n < a.N; n += 256) {
-      float v = 0.0f;
-      for (int p = 0; p < a.splits; ++p) v += a.partial[(p * a.partial_rows + m) * a.N + n];
-      out[n] = one_bf16(v * s);
-    }
+    store_columns(a.out + (a.rows ? (int64_t)a.rows[span.first + m] : span.first + m) * a.out_stride, n, a.N, v * s);
   }
 }
 
-template <int MF, int NF>
+// ADD: on top of the chunks before this one.  Whether a chunk is the last one is known on the device: both forms are launched, and
+// the one that does not apply ends at once (a kernel of both would spill: the sums and the next tile's fragments are 384 registers).
+template <int MF, int NF, bool ADD, bool LAST, bool ACCUMULATE>
 __global__ __launch_bounds__(kHeadThreads, 1) void head_weight_kernel(HeadWeightArgs a) {
   using Product = HeadProduct<MF, NF, true, true, false>;
   __shared__ __attribute__((aligned(1024))) char lds[Product::kLds];
   const HeadSpan span = head_span(a.chunk);
-  if (!span.there) return;
-  const HeadTile tile = head_tile(blockIdx.x, (a.M + Product::kTileM - 1) / Product::kTileM, (a.N + Product::kTileN - 1) / Product::kTileN);
+  if (!span.there || span.last != LAST) return;
+  const int mt = (a.M + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
+  HeadTile tile = head_tile(blockIdx.x, mt, nt);
   if (!tile.there) return;
-  const int64_t m0 = (int64_t)tile.m * Product::kTileM;
-  const int n0 = tile.n * Product::kTileN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Product x;
+  // rows of the chunk: behind the last one nothing is read
+  x.start(a.g, a.h, (int64_t)tile.m * Product::kTileM, (int64_t)tile.n * Product::kTileN, 0, span.rows, lds);
+  for (unsigned block = blockIdx.x + gridDim.x; tile.there; block += gridDim.x) {
+  const HeadTile next = head_tile(block, mt, nt);
+  const int64_t m0 = (int64_t)tile.m * Product::kTileM;
+  const int n0 = tile.n * Product::kTileN;
 #pragma unroll
   for (int i = 0; i < MF; ++i)
 #pragma unroll
     for (int j = 0; j < NF; ++j) x.acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  // rows of the chunk: behind the last one nothing is read
-  x.run(a.g, a.h, m0, n0, 0, span.rows, lds);
+  x.run(a.g, a.h, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, span.rows, lds);
+  tile = next;
+  const int64_t mw = m0 + (wave >> 1) * 16 * MF + (lane & 15);
+  const int columns = n0 + (x.wave & 1) * 16 * NF, nw = columns + 4 * (lane >> 4);
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
-    const int64_t m = m0 + (wave >> 1) * 16 * MF + 16 * i + (lane & 15);
+    __builtin_amdgcn_sched_barrier(0);  // (a row's sums at a time)
+    const int64_t m = mw + 16 * i;
     if (m >= a.M) continue;
+    f32x4* partial = reinterpret_cast<f32x4*>(a.partial + m * pitch4(a.N));
+    uint16_t* out = a.out + m * a.out_stride;
 #pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      const int n = n0 + (wave & 1) * 16 * NF + 16 * j + 4 * (lane >> 4);
-      float v[4] = {x.acc[i][j][0], x.acc[i][j][1], x.acc[i][j][2], x.acc[i][j][3]};
-      float* partial = a.partial + m * a.N;
-      if (a.chunk.index > 0) {
+    for (int j = 0; j < NF; j += 2) {
+      f32x4 v[2] = {x.acc[i][j], x.acc[i][j + 1]};
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (n + t < a.N) v[t] += partial[n + t];
-      }
-      if (span.last) {
-        uint16_t* out = a.out + m * a.out_stride;
-        if (a.accumulate) {
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-            if (n + t < a.N) v[t] += bf16_one(out[n + t]);
+      for (int t = 0; t < 2; ++t) {
+        const int n = nw + 16 * (j + t);
+        if constexpr (ADD) {
+          if (columns + 16 * (j + t) + 16 <= a.N || n < a.N) v[t] += partial[n / 4];
         }
-        store4(out, n, a.N, v);
-      } else {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (n + t < a.N) partial[n + t] = v[t];
+        if constexpr (ACCUMULATE) v[t] += load_columns(out, n, a.N);
+        if constexpr (!LAST) {
+          if (columns + 16 * (j + t) + 16 <= a.N || n < a.N) partial[n / 4] = v[t];
+        }
       }
+      if constexpr (LAST) store_two(out, nw + 16 * j, a.N, columns + 16 * j + 32 <= a.N, v[0], v[1]);
     }
+  }
   }
 }
 
@@ -171,9 +231,13 @@ template <int MF>
 hipError_t launch_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
   using Product = HeadProduct<MF, 8, false, true, false>;
   const int64_t mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
-  const int64_t blocks = (mt * nt + 7) / 8 * 8 * a.splits;
+  // (fewer rows than the most may be split further: tiles and pieces together never need more workgroups than this)
+  const int64_t blocks = a.most_splits == 1 ? (mt * nt + 7) / 8 * 8 : (mt * nt + 7) / 8 * 8 * a.most_splits;
   if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-  return launch_kernel(head_hidden_kernel<MF, 8>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
+  const hipError_t e = launch_kernel(head_hidden_kernel<MF, 8>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
+  if (e != hipSuccess || a.most_splits == 1) return e;
+  const int64_t quads = rows * ((a.N + 3) / 4), join = (quads + 255) / 256;
+  return launch_kernel(head_join_kernel<MF, 8>, dim3((unsigned)(join < 8192 ? join : 8192)), dim3(256), 0, stream, a);
 }
 
 int hidden_tile_rows(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
@@ -181,23 +245,34 @@ int hidden_tile_rows(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 
 }  // namespace
 
 int head_hidden_splits(int64_t rows, int32_t K, int32_t N) {
+  // the pieces that this many rows are split into, and half as many again for a chunk that turns out to have fewer
   const int64_t tiles = (rows + hidden_tile_rows(rows) - 1) / hidden_tile_rows(rows) * ((N + 255) / 256);
-  const int64_t most = K / 512 > 1 ? K / 512 : 1;  // a piece pays from 16 steps on
-  const int64_t fit = 256 / tiles;
-  return (int)(fit < 2 ? 1 : fit < most ? fit : most);
+  if (tiles > 4 * kUnits) return 1;
+  const int s = hidden_pieces((int)tiles, rows, K, N, kUnits);
+  return s + s / 2 < 4 ? 4 : s + s / 2;
 }
+
+size_t head_hidden_floats(int64_t rows, int32_t N, int splits) { return splits > 1 ? (size_t)splits * rows * pitch4(N) : 0; }
 
 hipError_t launch_head_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
   const int tile = hidden_tile_rows(rows);
-  const hipError_t e = tile == 64 ? launch_hidden<2>(a, rows, stream) : tile == 128 ? launch_hidden<4>(a, rows, stream) : launch_hidden<8>(a, rows, stream);
-  if (e != hipSuccess || a.splits == 1) return e;
-  return launch_kernel(head_join_kernel, dim3((unsigned)(rows < 4096 ? rows : 4096)), dim3(256), 0, stream, a);
+  return tile == 64 ? launch_hidden<2>(a, rows, stream) : tile == 128 ? launch_hidden<4>(a, rows, stream) : launch_hidden<8>(a, rows, stream);
 }
 
-hipError_t launch_head_weight(const HeadWeightArgs& a, hipStream_t stream) {
-  const int64_t tiles = (int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256), blocks = (tiles + 7) / 8 * 8;
-  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-  return launch_kernel(head_weight_kernel<8, 8>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
+template <bool ADD, bool LAST, bool ACCUMULATE>
+static hipError_t launch_weight(const HeadWeightArgs& a, int64_t tiles, hipStream_t stream) {
+  return launch_kernel(head_weight_kernel<8, 8, ADD, LAST, ACCUMULATE>, dim3(head_grid(tiles)), dim3(kHeadThreads), 0, stream, a);
+}
+
+hipError_t launch_head_weight(const HeadWeightArgs& a, int64_t chunks, hipStream_t stream) {
+  const int64_t tiles = ((int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256) + 7) / 8 * 8;
+  const bool add = a.chunk.index > 0;
+  if (chunks > 1) {
+    const hipError_t e = add ? launch_weight<true, false, false>(a, tiles, stream) : launch_weight<false, false, false>(a, tiles, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (a.accumulate) return add ? launch_weight<true, true, true>(a, tiles, stream) : launch_weight<false, true, true>(a, tiles, stream);
+  return add ? launch_weight<true, true, false>(a, tiles, stream) : launch_weight<false, true, false>(a, tiles, stream);
 }
 
 hipError_t launch_head_bias(const HeadBiasArgs& a, hipStream_t stream) {
