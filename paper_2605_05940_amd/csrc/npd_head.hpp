@@ -8,7 +8,14 @@
 
 namespace npd {
 
-constexpr int kHeadPart = 128;  // columns of one partial sum of a row: what a wave holds of it
+// Columns of one partial sum of a row: what a wave of the forward product holds of it, 128, or 64 with the small tiles.
+constexpr int kHeadPart = 128, kHeadSmallPart = 64;
+
+// Tiles of 128 x 128 in place of 256 x 256: where there are so few that each has a compute unit to itself either way, a tile's own
+// time decides (MI355X, 512 positions of a 1,024-entry vocabulary, width 256: LATER).
+inline bool head_small(int64_t rows, int64_t columns) {
+  return (rows + 255) / 256 * ((columns + 255) / 256) <= 64;
+}
 
 // Workgroups of a kernel whose workgroups take one tile after the other: one per compute unit, whose LDS the stages fill (a
 // multiple of eight, see head_tile).
@@ -21,7 +28,7 @@ enum HeadForward { kHeadLogits = 0, kHeadSums = 1, kHeadSumsKept = 2 };
 
 // x = (q w^T + bias), soft-capped, of a chunk of rows; then by HeadForward
 //   kHeadLogits     out = x, rounded to bf16
-//   kHeadSums       part[row][v / 128] = (r, z): sum over those 128 columns of 2^(x c - r) is z
+//   kHeadSums       part[row][v / 128 or 64] = (r, z): sum over those columns of 2^(x c - r) is z
 //   kHeadSumsKept   and e[row][v] = 2^(x c - r) (with a soft cap times dx / d(q w^T)), rounded to bf16; 0 for v >= V
 struct HeadForwardArgs {
   HeadChunk chunk;
@@ -33,6 +40,7 @@ struct HeadForwardArgs {
   const float* r0;      // [rows] a logit of the row times c, whole, or -1e30: the reference of columns not far above it
   float2* part;
   int32_t parts;
+  int32_t small;        // head_small(): parts of 64 columns
   uint16_t* e;
   int64_t e_stride;
   uint16_t* out;
@@ -101,10 +109,9 @@ struct HeadRowsArgs {
 };
 hipError_t launch_head_rows(const HeadRowsArgs& a, hipStream_t stream);
 
-// dst[i][0 .. width) = src[rows ? rows[first + i] : first + i][0 .. cols), 0 behind; with `cap` times 1 - (y / cap)^2
+// dst[i][0 .. width) = src[first + i][0 .. cols), 0 behind; with y times 1 - (y / cap)^2
 struct HeadPackArgs {
   HeadChunk chunk;
-  const int32_t* rows;
   const uint16_t* src;
   int64_t src_stride;
   const uint16_t* y;
@@ -134,7 +141,7 @@ struct HeadLossArgs {
   float* x;       // [cap][1 + k] logits at the label (or column 0) and the ids
   float* r0;      // [cap]
   const float2* part;
-  int32_t parts;
+  int32_t parts, part_columns;
   float *kd, *nll, *lse;
   int32_t* status;
   // gradients

@@ -61,7 +61,8 @@ struct Plan {
   int64_t chunks = 1;
   int32_t K = 0;          // width, a multiple of eight
   int64_t e_stride = 0;
-  int32_t parts = 0, splits = 1;
+  int32_t parts = 0, part_columns = 0, splits = 1;
+  bool small = false;     // head_small()
   bool few = false;       // rows that head_few_kernel takes
   bool pack_w = false, pack_h = false, pack_g = false;
   size_t rows = 0, count = 0, h = 0, hs = 0, x = 0, r0 = 0, part = 0, e = 0, scale = 0, w = 0, dw = 0, dh = 0, pieces = 0, db = 0;
@@ -87,7 +88,9 @@ Plan make_plan(const npd_head_desc& d, int op, int32_t cap) {
   // an odd number of 128-byte lines between rows: a tile reads 256 rows at one column, which would else come from few channels
   p.e_stride = up(d.vocab, 64);
   if (p.e_stride / 64 % 2 == 0) p.e_stride += 64;
-  p.parts = (d.vocab + kHeadPart - 1) / kHeadPart;
+  p.small = !p.few && head_small(p.chunk_rows, d.vocab);
+  p.part_columns = p.small ? kHeadSmallPart : kHeadPart;
+  p.parts = (d.vocab + p.part_columns - 1) / p.part_columns;
   if (gh) p.splits = head_hidden_splits(p.chunk_rows, d.vocab, d.width);
   auto take = [&p](size_t bytes) {
     const size_t at = p.bytes;
@@ -308,6 +311,7 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   float2* part = reinterpret_cast<float2*>(ws + p.part);
   l.part = part;
   l.parts = p.parts;
+  l.part_columns = p.part_columns;
   l.kd = kd_tok;
   l.nll = nll_tok;
   l.lse = lse_tok;
@@ -331,6 +335,7 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   f.r0 = l.r0;
   f.part = part;
   f.parts = p.parts;
+  f.small = p.small;
   f.e = l.e;
   f.e_stride = p.e_stride;
 
@@ -396,6 +401,7 @@ npd_status npd_head_logits(const npd_head_desc* desc, const void* hidden, const 
   f.K = p.K;
   f.V = d.vocab;
   f.cap = d.softcap;
+  f.small = p.small;
   f.out = static_cast<uint16_t*>(logits);
   f.out_stride = d.logits_stride;
   NPD_TRY((p.few ? launch_head_few : launch_head_forward)(f, kHeadLogits, T, on));

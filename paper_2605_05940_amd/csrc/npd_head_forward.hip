@@ -23,7 +23,7 @@ struct SoftCap {
 template <int MF, int NF, HeadForward WHAT, bool CAP>
 __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwardArgs a) {
   using Product = HeadProduct<MF, NF, false, false, true>;
-  static_assert(16 * NF == kHeadPart, "a wave's columns are one partial sum");
+  constexpr int kPart = 16 * NF;  // a wave's columns are one partial sum
   __shared__ __attribute__((aligned(1024))) char lds[Product::kLds];
   const HeadSpan span = head_span(a.chunk);
   if (!span.there || span.rows == 0) return;
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
       }
       z += __shfl_xor(z, 16, kWave);
       z += __shfl_xor(z, 32, kWave);
-      const int part = (n0 + (wave & 1) * 16 * NF) / kHeadPart;
+      const int part = columns / kPart;
       if (lane < 16 && row && part < a.parts) a.part[m * a.parts + part] = make_float2(r, z);
     }
   }
@@ -285,25 +285,32 @@ __global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_ker
 }
 
 // The same for up to 16 RT rows: a wave reads the weights of 32 columns straight into the fragments of 16 x 16 x 32 products (64
-// bytes of 16 rows per load, the next 64 with the one after it: 5 TB/s).
+// bytes of 16 rows per load, the next 64 with the one after it: 5 TB/s), 8 KB at a time; the hidden states go through LDS, 128
+// values of k of all rows at a time, so that a compute unit reads them once and not once per wave.
 template <int RT, HeadForward WHAT, bool CAP>
-__global__ __launch_bounds__(kHeadThreads, RT == 2 ? 4 : 3) void head_few_kernel(HeadForwardArgs a) {
-  __shared__ __attribute__((aligned(16))) float x[16 * RT][kHeadPart];
+__global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardArgs a) {
+  constexpr int kBlock = 128, kSteps = kBlock / kHeadStep;
+  constexpr int kPitch = kBlock + 8;  // (rows 17 groups of 16 bytes apart: 16 rows' reads lie in 16 different ones of 256 bytes)
+  __shared__ __attribute__((aligned(16))) union {
+    uint16_t h[2][16 * RT][kPitch];
+    float x[16 * RT][kHeadPart];
+  } lds;
   const HeadSpan span = head_span(a.chunk);
   if (span.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
   const int v0 = blockIdx.x * kHeadPart + wave * 32;
-  constexpr int kAhead = 4;  // steps requested together
   const uint16_t* w[2];
-  const uint16_t* h[RT];
 #pragma unroll
   for (int f = 0; f < 2; ++f) {
     const int v = v0 + 16 * f + i;
     w[f] = a.w.p + (int64_t)(v < a.V ? v : a.V - 1) * a.w.stride;
   }
+  // this thread's share of a block of the hidden states: group threadIdx.x % 16 of rows threadIdx.x / 16 + 16 t
+  const int hg = threadIdx.x & 15;
+  const uint16_t* h[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int m = 16 * t + i;
+    const int m = 16 * t + (threadIdx.x >> 4);
     h[t] = a.q.p + (int64_t)(m < span.rows ? m : span.rows - 1) * a.q.stride;
   }
   f32x4 acc[2][RT];
@@ -311,48 +318,54 @@ __global__ __launch_bounds__(kHeadThreads, RT == 2 ? 4 : 3) void head_few_kernel
   for (int f = 0; f < 2; ++f)
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int blocks = a.D / (kAhead * kHeadStep);
-  int at = blocks ? (int)((blockIdx.x * 4 + wave) % (unsigned)blocks) : 0;
-  for (int b = 0; b < blocks; ++b) {
-    const int d = at * kAhead * kHeadStep + 8 * g;
-    at = at + 1 == blocks ? 0 : at + 1;
-    bf16x8 wv[kAhead][2], y[kAhead][RT];
+  const int whole = a.D / kBlock, blocks = (a.D + kBlock - 1) / kBlock;
+  int at = whole ? (int)((blockIdx.x * 5) % (unsigned)whole) : 0;  // (where the workgroup begins, see above)
+  uint4 hv[RT];
+  auto request = [&](int block) {
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) {
+    for (int t = 0; t < RT; ++t)
+      hv[t] = block < whole ? load8(h[t] + block * kBlock + 8 * hg) : load8_of(h[t], block * kBlock + 8 * hg, a.D);
+  };
+  request(whole ? at : 0);
+  for (int n = 0; n < blocks; ++n) {
+    const int block = n < whole ? at : whole;
+    if (n < whole) at = at + 1 == whole ? 0 : at + 1;
+    bf16x8 wv[kSteps][2];
+    const int d = block * kBlock + 8 * g;
+    if (block < whole) {
 #pragma unroll
-      for (int f = 0; f < 2; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8(w[f] + d + s * kHeadStep));
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8(w[f] + d + s * kHeadStep));
+    } else {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8_of(w[f], d + s * kHeadStep, a.D));
     }
+    // (two buffers: what is written here was last read before the barrier of the block before)
 #pragma unroll
-    for (int s = 0; s < kAhead; ++s) {
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<uint4*>(&lds.h[n & 1][16 * t + (threadIdx.x >> 4)][8 * hg]) = hv[t];
+    __syncthreads();
+    if (n + 1 < blocks) request(n + 1 < whole ? at : whole);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) y[s][t] = __builtin_bit_cast(bf16x8, load8(h[t] + d + s * kHeadStep));
+    for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const bf16x8 y = *reinterpret_cast<const bf16x8*>(&lds.h[n & 1][16 * t + i][8 * g + s * kHeadStep]);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s][f], y, acc[f][t], 0, 0, 0);
+      }
     }
-#pragma unroll
-    for (int s = 0; s < kAhead; ++s)
-#pragma unroll
-      for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s][f], y[s][t], acc[f][t], 0, 0, 0);
   }
-  for (int d = blocks * kAhead * kHeadStep + 8 * g; d - 8 * g < a.D; d += kHeadStep) {
-    bf16x8 wv[2], y[RT];
-#pragma unroll
-    for (int f = 0; f < 2; ++f) wv[f] = __builtin_bit_cast(bf16x8, load8_of(w[f], d, a.D));
-#pragma unroll
-    for (int t = 0; t < RT; ++t) y[t] = __builtin_bit_cast(bf16x8, load8_of(h[t], d, a.D));
-#pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-      for (int t = 0; t < RT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[f], y[t], acc[f][t], 0, 0, 0);
-  }
-
+  __syncthreads();
   // acc[f][t][e]: row 16 t + i, column v0 + 16 f + 4 g + e
 #pragma unroll
   for (int f = 0; f < 2; ++f)
 #pragma unroll
-    for (int t = 0; t < RT; ++t) *reinterpret_cast<f32x4*>(&x[16 * t + i][wave * 32 + 16 * f + 4 * g]) = acc[f][t];
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<f32x4*>(&lds.x[16 * t + i][wave * 32 + 16 * f + 4 * g]) = acc[f][t];
   __syncthreads();
-  finish_columns<WHAT, CAP>(a, &x[0][0], span.rows);
+  finish_columns<WHAT, CAP>(a, &lds.x[0][0], span.rows);
 }
 
 template <HeadForward WHAT, bool CAP>
@@ -365,22 +378,22 @@ hipError_t launch_few(const HeadForwardArgs& a, int64_t rows, hipStream_t stream
   return launch_kernel(head_few_kernel<4, WHAT, CAP>, grid, block, 0, stream, a);
 }
 
-template <int MF, HeadForward WHAT, bool CAP>
+template <int MF, int NF, HeadForward WHAT, bool CAP>
 hipError_t launch(const HeadForwardArgs& a, int64_t rows, hipStream_t stream) {
-  using Product = HeadProduct<MF, 8, false, false, true>;
+  using Product = HeadProduct<MF, NF, false, false, true>;
   const int64_t mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.V + Product::kTileN - 1) / Product::kTileN;
   const int64_t blocks = (mt * nt + 7) / 8 * 8;
-  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-  return launch_kernel(head_forward_kernel<MF, 8, WHAT, CAP>, dim3(head_grid(blocks)), dim3(kHeadThreads), 0, stream, a);
+  if (blocks >= (int64_t)1 << 30) return hipErrorInvalidConfiguration;
+  return launch_kernel(head_forward_kernel<MF, NF, WHAT, CAP>, dim3(head_grid(blocks)), dim3(kHeadThreads), 0, stream, a);
 }
 
-template <int MF>
-hipError_t launch_rows(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream) {
+template <int MF, int NF>
+hipError_t launch_tiles(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream) {
   const bool cap = a.cap != 0.0f;
   switch (what) {
-    case kHeadLogits: return cap ? launch<MF, kHeadLogits, true>(a, rows, stream) : launch<MF, kHeadLogits, false>(a, rows, stream);
-    case kHeadSums: return cap ? launch<MF, kHeadSums, true>(a, rows, stream) : launch<MF, kHeadSums, false>(a, rows, stream);
-    default: return cap ? launch<MF, kHeadSumsKept, true>(a, rows, stream) : launch<MF, kHeadSumsKept, false>(a, rows, stream);
+    case kHeadLogits: return cap ? launch<MF, NF, kHeadLogits, true>(a, rows, stream) : launch<MF, NF, kHeadLogits, false>(a, rows, stream);
+    case kHeadSums: return cap ? launch<MF, NF, kHeadSums, true>(a, rows, stream) : launch<MF, NF, kHeadSums, false>(a, rows, stream);
+    default: return cap ? launch<MF, NF, kHeadSumsKept, true>(a, rows, stream) : launch<MF, NF, kHeadSumsKept, false>(a, rows, stream);
   }
 }
 
@@ -396,8 +409,9 @@ hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t r
 }
 
 hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream) {
-  if (rows <= 128) return launch_rows<4>(a, what, rows, stream);
-  return launch_rows<8>(a, what, rows, stream);
+  if (a.small) return launch_tiles<4, 4>(a, what, rows, stream);
+  if (rows <= 128) return launch_tiles<4, 8>(a, what, rows, stream);
+  return launch_tiles<8, 8>(a, what, rows, stream);
 }
 
 }  // namespace npd

@@ -227,26 +227,35 @@ __global__ __launch_bounds__(256) void head_bias_join_kernel(HeadBiasArgs a) {
   }
 }
 
-template <int MF>
+template <int MF, int NF>
 hipError_t launch_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
-  using Product = HeadProduct<MF, 8, false, true, false>;
+  using Product = HeadProduct<MF, NF, false, true, false>;
   const int64_t mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
   // (fewer rows than the most may be split further: tiles and pieces together never need more workgroups than this)
-  const int64_t blocks = a.most_splits == 1 ? (mt * nt + 7) / 8 * 8 : (mt * nt + 7) / 8 * 8 * a.most_splits;
+  const int64_t blocks = (mt * nt + 7) / 8 * 8 * a.most_splits;
   if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-  const hipError_t e = launch_kernel(head_hidden_kernel<MF, 8>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
+  const hipError_t e = launch_kernel(head_hidden_kernel<MF, NF>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
   if (e != hipSuccess || a.most_splits == 1) return e;
   const int64_t quads = rows * ((a.N + 3) / 4), join = (quads + 255) / 256;
-  return launch_kernel(head_join_kernel<MF, 8>, dim3((unsigned)(join < 8192 ? join : 8192)), dim3(256), 0, stream, a);
+  return launch_kernel(head_join_kernel<MF, NF>, dim3((unsigned)(join < 8192 ? join : 8192)), dim3(256), 0, stream, a);
 }
 
-int hidden_tile_rows(int64_t rows) { return rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// rows and columns of a tile for a chunk of up to so many rows
+struct HiddenTile {
+  int rows, columns;
+};
+HiddenTile hidden_tile(int64_t rows, int32_t K, int32_t N) {
+  // (K: small products are those whose vocabulary is small as well, so that splitting it cannot fill the chip with large tiles)
+  if (head_small(rows, N) && K <= 8192) return HiddenTile{128, 128};
+  return HiddenTile{rows <= 64 ? 64 : rows <= 128 ? 128 : 256, 256};
+}
 
 }  // namespace
 
 int head_hidden_splits(int64_t rows, int32_t K, int32_t N) {
   // the pieces that this many rows are split into, and half as many again for a chunk that turns out to have fewer
-  const int64_t tiles = (rows + hidden_tile_rows(rows) - 1) / hidden_tile_rows(rows) * ((N + 255) / 256);
+  const HiddenTile t = hidden_tile(rows, K, N);
+  const int64_t tiles = (rows + t.rows - 1) / t.rows * ((N + t.columns - 1) / t.columns);
   if (tiles > 4 * kUnits) return 1;
   const int s = hidden_pieces((int)tiles, rows, K, N, kUnits);
   return s + s / 2 < 4 ? 4 : s + s / 2;
@@ -255,24 +264,32 @@ int head_hidden_splits(int64_t rows, int32_t K, int32_t N) {
 size_t head_hidden_floats(int64_t rows, int32_t N, int splits) { return splits > 1 ? (size_t)splits * rows * pitch4(N) : 0; }
 
 hipError_t launch_head_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
-  const int tile = hidden_tile_rows(rows);
-  return tile == 64 ? launch_hidden<2>(a, rows, stream) : tile == 128 ? launch_hidden<4>(a, rows, stream) : launch_hidden<8>(a, rows, stream);
+  const HiddenTile t = hidden_tile(rows, a.K, a.N);
+  if (t.columns == 128) return launch_hidden<4, 4>(a, rows, stream);
+  return t.rows == 64 ? launch_hidden<2, 8>(a, rows, stream) : t.rows == 128 ? launch_hidden<4, 8>(a, rows, stream) : launch_hidden<8, 8>(a, rows, stream);
 }
 
-template <bool ADD, bool LAST, bool ACCUMULATE>
-static hipError_t launch_weight(const HeadWeightArgs& a, int64_t tiles, hipStream_t stream) {
-  return launch_kernel(head_weight_kernel<8, 8, ADD, LAST, ACCUMULATE>, dim3(head_grid(tiles)), dim3(kHeadThreads), 0, stream, a);
+namespace {
+
+template <int MF, int NF, bool ADD, bool LAST, bool ACCUMULATE>
+hipError_t launch_weight(const HeadWeightArgs& a, hipStream_t stream) {
+  using Product = HeadProduct<MF, NF, true, true, false>;
+  const int64_t mt = (a.M + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
+  return launch_kernel(head_weight_kernel<MF, NF, ADD, LAST, ACCUMULATE>, dim3(head_grid((mt * nt + 7) / 8 * 8)), dim3(kHeadThreads), 0, stream, a);
 }
+
+}  // namespace
 
 hipError_t launch_head_weight(const HeadWeightArgs& a, int64_t chunks, hipStream_t stream) {
-  const int64_t tiles = ((int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256) + 7) / 8 * 8;
   const bool add = a.chunk.index > 0;
   if (chunks > 1) {
-    const hipError_t e = add ? launch_weight<true, false, false>(a, tiles, stream) : launch_weight<false, false, false>(a, tiles, stream);
+    const hipError_t e = add ? launch_weight<8, 8, true, false, false>(a, stream) : launch_weight<8, 8, false, false, false>(a, stream);
     if (e != hipSuccess) return e;
   }
-  if (a.accumulate) return add ? launch_weight<true, true, true>(a, tiles, stream) : launch_weight<false, true, true>(a, tiles, stream);
-  return add ? launch_weight<true, true, false>(a, tiles, stream) : launch_weight<false, true, false>(a, tiles, stream);
+  if (chunks == 1 && head_small(a.M, a.N))
+    return a.accumulate ? launch_weight<4, 4, false, true, true>(a, stream) : launch_weight<4, 4, false, true, false>(a, stream);
+  if (a.accumulate) return add ? launch_weight<8, 8, true, true, true>(a, stream) : launch_weight<8, 8, false, true, true>(a, stream);
+  return add ? launch_weight<8, 8, true, true, false>(a, stream) : launch_weight<8, 8, false, true, false>(a, stream);
 }
 
 hipError_t launch_head_bias(const HeadBiasArgs& a, hipStream_t stream) {

@@ -72,29 +72,42 @@ __global__ __launch_bounds__(kRowThreads) void head_zero_kernel(HeadRowsArgs a) 
   }
 }
 
+// (blockIdx.y: stretches of a row, four groups of eight per thread, requested together)
+constexpr int kPackGroups = 4;
 __global__ __launch_bounds__(kRowThreads) void head_pack_kernel(HeadPackArgs a) {
   const HeadSpan span = head_span(a.chunk);
   if (!span.there) return;
+  const float inv = a.y ? 1.0f / a.cap : 0.0f;
+  const int d0 = blockIdx.y * (kRowThreads * 8 * kPackGroups) + threadIdx.x * 8;
   for (int64_t i = blockIdx.x; i < span.rows; i += gridDim.x) {
-    const int64_t p = a.rows ? (int64_t)a.rows[span.first + i] : span.first + i;
+    const int64_t p = span.first + i;
     const uint16_t* src = a.src + p * a.src_stride;
-    const uint16_t* y = a.y ? a.y + p * a.y_stride : nullptr;
     uint16_t* dst = a.dst + i * a.dst_stride;
-    const float inv = a.y ? 1.0f / a.cap : 0.0f;
-    for (int d = threadIdx.x * 8; d < a.width; d += kRowThreads * 8) {
-      uint4 v = load8_of(src, d, a.cols);
-      if (y) {
+    uint4 v[kPackGroups];
+#pragma unroll
+    for (int u = 0; u < kPackGroups; ++u) v[u] = load8_of(src, d0 + u * kRowThreads * 8, a.cols);
+    if (a.y) {
+      const uint16_t* y = a.y + p * a.y_stride;
+      uint4 w[kPackGroups];
+#pragma unroll
+      for (int u = 0; u < kPackGroups; ++u) w[u] = load8_of(y, d0 + u * kRowThreads * 8, a.cols);
+#pragma unroll
+      for (int u = 0; u < kPackGroups; ++u) {
         float g[8], f[8];
-        unpack8(v, g);
-        unpack8(load8_of(y, d, a.cols), f);
+        unpack8(v[u], g);
+        unpack8(w[u], f);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-          const float u = f[t] * inv;
-          g[t] *= __builtin_fmaf(-u, u, 1.0f);
+          const float x = f[t] * inv;
+          g[t] *= __builtin_fmaf(-x, x, 1.0f);
         }
-        v = make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7]));
+        v[u] = make_uint4(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]), pack_bf16(g[4], g[5]), pack_bf16(g[6], g[7]));
       }
-      *reinterpret_cast<uint4*>(dst + d) = v;  // (rows of dst begin on 16 bytes, width is a multiple of eight)
+    }
+#pragma unroll
+    for (int u = 0; u < kPackGroups; ++u) {
+      const int d = d0 + u * kRowThreads * 8;
+      if (d < a.width) *reinterpret_cast<uint4*>(dst + d) = v[u];  // (rows of dst begin on 16 bytes, width is a multiple of eight)
     }
   }
 }
@@ -189,7 +202,7 @@ __global__ __launch_bounds__(kRowThreads) void head_prepare_kernel(HeadRowsArgs 
   if (r.grad_hidden) zero_row(r.grad_hidden + p * r.grad_stride, r.D);
 }
 
-// Joins the sums of a row over the vocabulary (part, one pair per 128 columns), writes its scalars, and turns what is kept of it,
+// Joins the sums of a row over the vocabulary (part, one pair per 128 or 64 columns), writes its scalars, and turns what is kept of it,
 // e = 2^(x c - R), into the gradient up to the row's factor: with w = grad_scale / tau + ce_grad_scale and Z the row's sum
 //   G(v) = w / Z (e(v) - Z / w (grad_scale / tau p_T(v) + ce_grad_scale [v = label])),
 // so that only the entries at the label and the teacher's ids change (they are rounded to bf16 once, from fp32 values).
@@ -222,9 +235,9 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
       const float r = part[t].x;
       if (r == R) continue;
       const float f = exp2_fast(r - R);
-      uint16_t* e = a.e + i * a.e_stride + t * kHeadPart;
+      uint16_t* e = a.e + i * a.e_stride + t * a.part_columns;
       const int n = 2 * lane;
-      if (t * kHeadPart + n < a.V) {
+      if (n < a.part_columns && t * a.part_columns + n < a.V) {
         uint32_t* w = reinterpret_cast<uint32_t*>(e + n);
         *w = f == 0.0f ? 0u : pack_bf16(bf16_lo(*w) * f, bf16_hi(*w) * f);
       }
@@ -320,7 +333,8 @@ hipError_t launch_head_rows(const HeadRowsArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_head_pack(const HeadPackArgs& a, int64_t rows, hipStream_t stream) {
-  return launch_kernel(head_pack_kernel, dim3(few(rows)), dim3(kRowThreads), 0, stream, a);
+  const unsigned stretch = kRowThreads * 8 * kPackGroups;
+  return launch_kernel(head_pack_kernel, dim3(few(rows), ((unsigned)a.width + stretch - 1) / stretch), dim3(kRowThreads), 0, stream, a);
 }
 
 hipError_t launch_head_prepare(const HeadRowsArgs& r, const HeadLossArgs& a, hipStream_t stream) {
