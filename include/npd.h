@@ -396,8 +396,9 @@ npd_status npd_segment_ppl(int32_t n_segments, const float* seg_mean_nll, const 
  * [V, D] in place of logits [T, V], for programs that would hold the logits for the loss alone.  They share a
  * descriptor; fields that an entry point has no use for are ignored.
  */
-#define NPD_HEAD_MAX_VOCAB (1 << 21)  /* largest vocabulary and row stride (elements), beyond: NPD_ERR_UNSUPPORTED */
-#define NPD_HEAD_MAX_WIDTH (1 << 16)  /* largest width, likewise                                                  */
+#define NPD_HEAD_MAX_TOKENS (1 << 30) /* most positions, beyond: NPD_ERR_UNSUPPORTED                    */
+#define NPD_HEAD_MAX_VOCAB (1 << 21)  /* largest vocabulary and row stride (elements), likewise           */
+#define NPD_HEAD_MAX_WIDTH (1 << 16)  /* largest width, likewise                                          */
 
 /* npd_head_desc.flags */
 enum {
@@ -412,7 +413,7 @@ enum {
 enum { NPD_HEAD_LOSS = 0, NPD_HEAD_LOGITS = 1, NPD_HEAD_LOGITS_BWD = 2 };
 
 typedef struct {
-  int64_t n_tokens;           /* T in [1, NPD_MAX_TOKENS]                                            */
+  int64_t n_tokens;           /* T in [1, NPD_HEAD_MAX_TOKENS]                                       */
   int32_t vocab;              /* V in [1, NPD_HEAD_MAX_VOCAB]                                        */
   int32_t width;              /* D in [1, NPD_HEAD_MAX_WIDTH]                                        */
   int64_t hidden_stride;      /* elements between rows of hidden (>= D)                              */

@@ -19,7 +19,7 @@ npd_status check_head(const npd_head_desc* d, int op) {
   if (!d) return NPD_ERR_NULL;
   if (op != NPD_HEAD_LOSS && op != NPD_HEAD_LOGITS && op != NPD_HEAD_LOGITS_BWD) return NPD_ERR_VALUE;
   if (d->n_tokens <= 0 || d->vocab <= 0 || d->width <= 0) return NPD_ERR_SHAPE;
-  if (d->n_tokens > NPD_MAX_TOKENS || d->vocab > NPD_HEAD_MAX_VOCAB || d->width > NPD_HEAD_MAX_WIDTH)
+  if (d->n_tokens > NPD_HEAD_MAX_TOKENS || d->vocab > NPD_HEAD_MAX_VOCAB || d->width > NPD_HEAD_MAX_WIDTH)
     return NPD_ERR_UNSUPPORTED;
   const uint32_t known = op == NPD_HEAD_LOGITS ? (uint32_t)NPD_HEAD_UNALIGNED
                                                : kGradFlags | NPD_HEAD_ACCUMULATE | NPD_HEAD_UNALIGNED;

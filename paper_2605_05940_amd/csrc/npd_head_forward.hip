@@ -53,10 +53,16 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
 #pragma unroll
     for (int i = 0; i < MF; ++i) x.acc[i][j] = b;
   }
+  float r0[MF];  // (requested here: there is no time to wait for them once the products are done)
+  if constexpr (WHAT != kHeadLogits) {
+#pragma unroll
+    for (int i = 0; i < MF; ++i) r0[i] = a.r0[mw + 16 * i < span.rows ? mw + 16 * i : 0];
+  }
   x.run(q, a.w, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, a.K, lds);
   tile = next;
 
   const SoftCap soft(CAP ? a.cap : 1.0f);
+  const float c = CAP ? a.cap * a.c : a.c;
   const bool edge = n0 + Product::kTileN > a.V;  // uniform
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
@@ -88,35 +94,26 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
         }
       }
     } else {
-      float v[4 * NF], d[CAP ? 4 * NF : 1];
+      // logits, or with a soft cap their tanh: that times cap is the logit, and one less its square the slope
+      float v[4 * NF];
       float top = -__builtin_inff();
 #pragma unroll
-      for (int j = 0; j < NF; ++j) {
+      for (int j = 0; j < NF; ++j)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          float y = x.acc[i][j][t];
-          if constexpr (CAP) {
-            const float th = soft.tanh_of(y);
-            y = soft.cap * th;
-            d[4 * j + t] = __builtin_fmaf(-th, th, 1.0f);
-          }
-          v[4 * j + t] = y;
-        }
-      }
-      if (edge) {
+        for (int t = 0; t < 4; ++t) v[4 * j + t] = CAP ? soft.tanh_of(x.acc[i][j][t]) : x.acc[i][j][t];
+      if (edge) {  // (columns that are not there: e is 0, and with a finite slope e times it)
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
           for (int t = 0; t < 4; ++t)
-            if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = -__builtin_inff();
+            if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = CAP ? -1.0e18f : -__builtin_inff();
       }
 #pragma unroll
       for (int p = 0; p < 4 * NF; p += 2) top = max3(top, v[p], v[p + 1]);
       top = fmaxf(top, __shfl_xor(top, 16, kWave));
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float r0 = a.r0[row ? m : 0];
-      const float u = top * a.c;
-      const float r = u > r0 + kHeadHeadroom ? __builtin_rintf(u) : r0;
+      const float u = top * c;
+      const float r = u > r0[i] + kHeadHeadroom ? __builtin_rintf(u) : r0[i];
       float z = 0.0f;
       uint16_t* e = WHAT == kHeadSumsKept ? a.e + (row ? m : 0) * a.e_stride : nullptr;
 #pragma unroll
@@ -125,12 +122,12 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int p = 4 * j + 2 * t;
-          float lo = exp2_fast(__builtin_fmaf(v[p], a.c, -r)), hi = exp2_fast(__builtin_fmaf(v[p + 1], a.c, -r));
+          float lo = exp2_fast(__builtin_fmaf(v[p], c, -r)), hi = exp2_fast(__builtin_fmaf(v[p + 1], c, -r));
           z += lo;
           z += hi;
           if constexpr (CAP && WHAT == kHeadSumsKept) {
-            lo *= d[p];
-            hi *= d[p + 1];
+            lo *= __builtin_fmaf(-v[p], v[p], 1.0f);
+            hi *= __builtin_fmaf(-v[p + 1], v[p + 1], 1.0f);
           }
           if constexpr (WHAT == kHeadSumsKept) w[t] = pack_bf16(lo, hi);
         }

@@ -196,20 +196,20 @@ __global__ __launch_bounds__(256) void head_bias_kernel(HeadBiasArgs a) {
   if (!span.there) return;
   const int m = (blockIdx.x * 256 + threadIdx.x) * 8;  // rows of g begin on 16 bytes and are padded to eight
   if (m >= a.M) return;
-  const int s = blockIdx.y;
-  const int64_t b = (int64_t)span.rows * s / kHeadBiasSplits, e = (int64_t)span.rows * (s + 1) / kHeadBiasSplits;
+  const int piece = blockIdx.y;
+  const int64_t b = (int64_t)span.rows * piece / kHeadBiasSplits, e = (int64_t)span.rows * (piece + 1) / kHeadBiasSplits;
   float sum[8] = {};
   for (int64_t r = b; r < e; ++r) {
     float x[8];
     unpack8(*reinterpret_cast<const uint4*>(a.g.p + r * a.g.stride + m), x);
-    const float w = a.scale ? a.scale[r] : 1.0f;
-    if (w != w) continue;  // a position with a bad label or id: no part of the shared gradients
+    // (a position with a bad label or id has no part in the shared gradients; one that holds a NaN itself makes them NaN)
+    const float s = a.scale ? a.scale[r] : 1.0f, w = s != s ? 0.0f : s;
 #pragma unroll
     for (int t = 0; t < 8; ++t) sum[t] = __builtin_fmaf(x[t], w, sum[t]);
   }
 #pragma unroll
   for (int t = 0; t < 8; ++t)
-    if (m + t < a.M) a.pieces[(int64_t)s * a.M + m + t] = sum[t];
+    if (m + t < a.M) a.pieces[(int64_t)piece * a.M + m + t] = sum[t];
 }
 
 __global__ __launch_bounds__(256) void head_bias_join_kernel(HeadBiasArgs a) {
