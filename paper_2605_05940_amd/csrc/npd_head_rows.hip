@@ -205,7 +205,11 @@ __global__ __launch_bounds__(kRowThreads) void head_prepare_kernel(HeadRowsArgs 
 // Joins the sums of a row over the vocabulary (part, one pair per 128 or 64 columns), writes its scalars, and turns what is kept of it,
 // e = 2^(x c - R), into the gradient up to the row's factor: with w = grad_scale / tau + ce_grad_scale and Z the row's sum
 //   G(v) = w / Z (e(v) - Z / w (grad_scale / tau p_T(v) + ce_grad_scale [v = label])),
-// so that only the entries at the label and the teacher's ids change (they are rounded to bf16 once, from fp32 values).
+// so that only the entries at the label and the teacher's ids change (they are rounded to bf16 once, from fp32 values).  Those are
+// where most of a row's gradient is, and their roundings are known: the row's factor takes up as much of them as one factor can (by
+// least squares, half a bf16 step at most).  Error of the weights' gradient against 64 bits, as a share of its norm: hard labels
+// .00289 without, .00245 with it, a record of 64 .00288 / .00262; of the hidden states' .00238 / .00182 and .00235 / .00203
+// (rounding the result alone: .00166).
 __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a) {
   __shared__ float fred[3 * kRowThreads / kWave];
   __shared__ int bad_id;
@@ -268,6 +272,20 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
   const float w = (a.k ? a.kd_weight : 0.0f) + a.ce_weight;
   const float take = w != 0.0f ? Z / w : 0.0f;
   float kd = 0.0f;
+  float off = 0.0f, size = 0.0f;  // of the entries' roundings, over Z
+  const float per = 1.0f / Z;
+  auto put = [&](int id, float x, float taken) {
+    float g = exp2_fast(__builtin_fmaf(x, a.c, -R)) - taken;
+    if (a.cap != 0.0f) {
+      const float f = x / a.cap;
+      g *= __builtin_fmaf(-f, f, 1.0f);
+    }
+    const uint16_t rounded = one_bf16(g);
+    a.e[i * a.e_stride + id] = rounded;
+    const float u = bf16_one(rounded) * per;
+    off = __builtin_fmaf(u, __builtin_fmaf(g, per, -u), off);
+    size = __builtin_fmaf(u, u, size);
+  };
   bool at_label = false;
   for (int j = threadIdx.x; j < a.k; j += kRowThreads) {
     const int id = entry_id(a, p, 1 + j);
@@ -279,12 +297,7 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
     if (a.e) {
       const bool here = id == label;
       at_label |= here;
-      float g = exp2_fast(xe) - take * (a.kd_weight * pt + (here ? a.ce_weight : 0.0f));
-      if (a.cap != 0.0f) {
-        const float f = x[1 + j] / a.cap;
-        g *= __builtin_fmaf(-f, f, 1.0f);
-      }
-      a.e[i * a.e_stride + id] = one_bf16(g);
+      put(id, x[1 + j], take * (a.kd_weight * pt + (here ? a.ce_weight : 0.0f)));
     }
   }
   const bool label_done = __syncthreads_or(at_label);
@@ -292,32 +305,28 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
   const bool bad = (no_label && (a.nll || a.ce_weight != 0.0f)) || no_id;
   if (threadIdx.x == 0) {
     const float nan = __builtin_nanf("");
-    if (a.e && label >= 0 && !label_done && a.ce_weight != 0.0f) {
-      float g = exp2_fast(__builtin_fmaf(x[0], a.c, -R)) - take * a.ce_weight;
-      if (a.cap != 0.0f) {
-        const float f = x[0] / a.cap;
-        g *= __builtin_fmaf(-f, f, 1.0f);
-      }
-      a.e[i * a.e_stride + label] = one_bf16(g);
-    }
+    if (a.e && label >= 0 && !label_done && a.ce_weight != 0.0f) put(label, x[0], take * a.ce_weight);
     if (a.lse) a.lse[p] = (R + lz) * kLn2;
     if (a.nll) a.nll[p] = no_label ? nan : (__builtin_fmaf(-x[0], a.c, R) + lz) * kLn2;
     if (a.kd) a.kd[p] = no_id ? nan : kd * kLn2;
     if (a.status && bad) atomicOr(a.status, (no_label ? NPD_DEV_BAD_LABEL : 0) | (no_id ? NPD_DEV_BAD_TOPK_INDEX : 0));
-    if (a.scale) a.scale[i] = bad ? nan : w / Z;
   }
+  if (!a.e) return;
+  off = block_sum<kRowThreads>(off, fred);
+  size = block_sum<kRowThreads>(size, fred);
+  const float factor = w / Z * (size > 0.0f ? 1.0f + off / size : 1.0f);
+  if (threadIdx.x == 0) a.scale[i] = bad ? __builtin_nanf("") : factor;
   if (a.hs) {
     // Rounded to bf16 as an operand of the matrix cores (half a step, like e itself): the row's factor is not known when e is
     // stored.  A position with a bad label or id is left out of the weights' gradient.
-    const float s = bad ? 0.0f : w / Z;
     const uint16_t* h = a.h.p + i * a.h.stride;
     uint16_t* hs = a.hs + i * a.h.stride;
     for (int d = threadIdx.x * 8; d < a.K; d += kRowThreads * 8) {
       float v[8];
       unpack8(*reinterpret_cast<const uint4*>(h + d), v);
       *reinterpret_cast<uint4*>(hs + d) = bad ? make_uint4(0, 0, 0, 0)
-                                              : make_uint4(pack_bf16(v[0] * s, v[1] * s), pack_bf16(v[2] * s, v[3] * s),
-                                                           pack_bf16(v[4] * s, v[5] * s), pack_bf16(v[6] * s, v[7] * s));
+                                              : make_uint4(pack_bf16(v[0] * factor, v[1] * factor), pack_bf16(v[2] * factor, v[3] * factor),
+                                                           pack_bf16(v[4] * factor, v[5] * factor), pack_bf16(v[6] * factor, v[7] * factor));
     }
   }
 }

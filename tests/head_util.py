@@ -11,7 +11,8 @@ Tolerances, from the arithmetic alone.  B = 2^-8 is the largest relative error o
             term counts, 128 u ln 2 each), the exponential and the sums (32 terms per lane, then trees and V / 128 / 256
             partials) give less than 2^-16 of the sum together; two roundings of the result.
   kd        the same, and each of its terms p_T (log p_T - log p_S) once more 2^-20 relative.
-  G         kept as bf16 (B |G|); where it is a difference its parts w p, gs p_T, cs 1 carry the errors of the scalars.
+  G         kept as bf16 (B |G|), times a factor of the row that is off by a weighted mean of the roundings of its entries at
+            the label and the teacher's ids (B |G| at most again); where it is a difference its parts w p, gs p_T, cs 1 carry the errors of the scalars.
             A soft cap's slope 1 - (x / cap)^2 changes by 2 dx / cap relative with x, and is a difference from 1 of a square
             that is off by 2^-20 at most.
   grads     |dG| passes through the second product, whose fp32 sums of n terms add (n / 32 + 8) 2 u sum |G| |w|; hidden
@@ -96,7 +97,7 @@ def loss64(s, *, cap=0.0, tau=1.0, grad_scale=1.0, ce=0.0):
         G[rows, y] -= ce
         parts[rows, y] += abs(ce)
     G, parts, flat = G * slope * on[:, None], parts * slope * on[:, None], parts * on[:, None]
-    dG = B * G.abs() + (2 * d[:, None] + 2.0 ** -18) * parts
+    dG = 2 * B * G.abs() + (2 * d[:, None] + 2.0 ** -18) * parts
     if cap:
         dG = dG + 2 * d[:, None] * tau / cap * parts + 2.0 ** -20 * flat
     h, w = s["hidden"].double(), s["weight"].double()
