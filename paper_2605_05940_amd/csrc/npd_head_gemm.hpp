@@ -62,20 +62,26 @@ __device__ __forceinline__ HeadSpan head_span(const HeadChunk& c) {
 }
 
 // Which tile a workgroup has.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets consecutive
-// tiles, in bands of eight tiles of m, so that the 32 that it runs together share 8 + 4 panels of the operands instead of
-// reading 64.
+// tiles, in bands of four tiles of m, so that the 32 that it runs together share 4 + 8 panels of the operands instead of
+// reading 64; with fewer than eight tiles of n in bands of 32 over those.  Measured (MI355X, TFLOP/s), 8,192^3 along k / 8,192 x
+// 2,048 x 65,536 / 32,768 x 2,048 x 8,192 across it: bands of 2 1,250 / 1,326 / 1,431, of 4 1,378 / 1,344 / 1,431, of 8 1,350 / 1,284
+// / 1,380, of 16 1,232 / 1,110 / 1,317; 50,003 x 1,000 (four tiles of n) over 333 rows: of 4 93 us, of 8 76.
+__device__ __forceinline__ unsigned head_band(int nt) { return nt >= 8 ? 4u : 32u / (unsigned)nt; }
 struct HeadTile {
-  int m, n;
+  int m, n, piece;
   bool there;
 };
-__device__ __forceinline__ HeadTile head_tile(unsigned block, int mt, int nt) {
-  const unsigned total = (unsigned)mt * (unsigned)nt, per = (total + 7) / 8;
-  const unsigned local = block / 8, id = block % 8 * per + local;
+// (pieces of k: all tiles of a piece, then those of the next one)
+__device__ __forceinline__ HeadTile head_tile(unsigned block, int mt, int nt, int pieces = 1) {
+  const unsigned tiles = (unsigned)mt * (unsigned)nt, total = tiles * (unsigned)pieces, per = (total + 7) / 8;
+  const unsigned local = block / 8, all = block % 8 * per + local;
   HeadTile t;
-  t.there = local < per && id < total;
-  const unsigned band = 8u * (unsigned)nt, b = id / band, in = id % band;
-  const unsigned left = (unsigned)mt - b * 8, height = left < 8 ? left : 8;
-  t.m = (int)(b * 8 + in % (height ? height : 1));
+  t.there = local < per && all < total;
+  const unsigned piece = pieces > 1 ? all / tiles : 0, id = all - piece * tiles;
+  t.piece = (int)piece;
+  const unsigned most = head_band(nt), band = most * (unsigned)nt, b = id / band, in = id % band;
+  const unsigned left = (unsigned)mt - b * most, height = left < most ? left : most;
+  t.m = (int)(b * most + in % (height ? height : 1));
   t.n = (int)(in / (height ? height : 1));
   return t;
 }
@@ -263,15 +269,16 @@ struct HeadProduct {
 #pragma unroll
       for (int b = 0; b < NF; ++b) {
         const int done = a * NF + b;
-        // loads and reads are spread over the first three quarters of the step's matrix instructions
-        while (load < kLoads && load * (kSteps * 3 / 4) <= done * kLoads) {
+        // loads are spread over the step's matrix instructions (they wait for one another otherwise: a compute unit takes 64 bytes per
+        // cycle), reads over the first half of them
+        while (load < kLoads && load * kSteps <= done * kLoads) {
           if (load < Q::kLoads)
             nq.load(load, ahead, q_stage(lds, S), wave);
           else
             np.load(load - Q::kLoads, ahead, p_stage(lds, S), wave);
           ++load;
         }
-        while (read < kReads && read * (kSteps * 3 / 4) <= done * kReads) {
+        while (read < kReads && read * (kSteps / 2) <= done * kReads) {
           if (read < NF)
             fp[nxt][read] = pr.fragment(read, p_stage(lds, sn));
           else

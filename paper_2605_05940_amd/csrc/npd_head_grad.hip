@@ -74,13 +74,10 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHidden
   const HeadSpan span = head_span(a.chunk);
   if (!span.there || span.rows == 0) return;
   const int mt = (span.rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
-  // a piece of k after the other (tiles of one piece share its rows of w)
   const int pieces = hidden_pieces(mt * nt, span.rows, a.K, a.N, a.most_splits);
-  const unsigned per = (unsigned)(mt * nt + 7) / 8 * 8;
-  const int split = (int)(blockIdx.x / per);
-  if (split >= pieces) return;
-  const HeadTile tile = head_tile(blockIdx.x % per, mt, nt);
+  const HeadTile tile = head_tile(blockIdx.x, mt, nt, pieces);
   if (!tile.there) return;
+  const int split = tile.piece;
   const int64_t m0 = (int64_t)tile.m * Product::kTileM;
   const int n0 = tile.n * Product::kTileN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
