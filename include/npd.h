@@ -442,7 +442,8 @@ size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op);
  *
  *   x[p, v] = hidden[p, :] . weight[v, :] + bias[v],      with softcap > 0: softcap * tanh(that / softcap)
  *
- * in the place of the student's logits, which are never stored: p_S = Softmax(x / tau),
+ * in the place of the student's logits, which are not stored (with gradients one bf16 value per logit of at most 8,192 scored
+ * positions at a time is, in the workspace): p_S = Softmax(x / tau),
  *
  *   kd_tok[p], nll_tok[p], lse_tok[p]   as there (of fp32 logits)
  *   G[p, v]        = (grad_scale / tau * (p_S(v) - p_T(v) [v in support]) + ce_grad_scale * (p_S(v) - [v == labels[p]]))
@@ -454,8 +455,7 @@ size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op);
  *
  *   hidden       bf16 [T, hidden_stride], required          weight   bf16 [V, weight_stride], required
  *   bias         bf16 [V] or NULL (-inf: an entry of probability 0, without a soft cap)
- *   labels       int32 [T]; required iff nll_tok is given or ce_grad_scale != 0 (given without: they must still be ids
- *                for the call to be fast, and any other value is let pass)
+ *   labels       int32 [T]; required iff nll_tok is given or ce_grad_scale != 0 (given without: not checked)
  *   teacher_idx  int32 [T, k] and teacher_val fp32 [T, k], iff topk > 0: as in npd_kd_loss_fwd_bwd
  *   loss_mask    uint8 [T], required
  *   grad_hidden  bf16 [T, grad_hidden_stride]   grad_weight  bf16 [V, grad_weight_stride]   grad_bias  bf16 [V]
@@ -468,8 +468,10 @@ size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op);
  * a call of their own), and gradients with grad_scale and ce_grad_scale of opposite sign.  NPD_ERR_VALUE: ce_grad_scale != 0
  * without a gradient, gradients with neither a teacher nor ce_grad_scale.
  *
- * Products are of bf16 operands with fp32 sums (the gradient's operands G and hidden are rounded to bf16 once each, G against
- * its row's scale); softmax statistics are fp32.  Results are reproducible bit by bit for the same workspace size.
+ * Products are of bf16 operands with fp32 sums (for the gradients each row of G is rounded to bf16 once, up to a factor of the
+ * row, and hidden times that factor once); softmax statistics are fp32.  Results are reproducible bit by bit for the same sizes
+ * and workspace bytes (no floating-point atomics).  NaN or +inf in the hidden state of a position make its own outputs, and the
+ * gradients that positions share, non-finite.
  */
 npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, const void* weight, const void* bias,
                                  const int32_t* labels, const int32_t* teacher_idx, const float* teacher_val,

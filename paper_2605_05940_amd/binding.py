@@ -491,7 +491,7 @@ def npd_head_loss_fwd_bwd(hidden: torch.Tensor, weight: torch.Tensor, loss_mask:
                           accumulate: bool = False, kd_tok: Optional[torch.Tensor] = None,
                           nll_tok: Optional[torch.Tensor] = None, lse_tok: Optional[torch.Tensor] = None,
                           dev_status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
-    """Enqueue the loss of ``npd_kd_loss_fwd_bwd`` on logits ``hidden @ weight.T + bias`` that are never stored, with the
+    """Enqueue the loss of ``npd_kd_loss_fwd_bwd`` on logits ``hidden @ weight.T + bias`` that are not stored, with the
     gradients that are given a tensor (see ``npd_head_loss_fwd_bwd`` in npd.h); with none of them the call is forward only.
     ``accumulate``: the gradients of weight and bias are added to what their tensors hold.  ``workspace``: a uint8 tensor of
     at least ``npd_head_workspace_bytes`` bytes; without it the call takes a block from torch's allocator for as long as it
