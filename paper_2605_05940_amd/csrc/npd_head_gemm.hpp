@@ -49,15 +49,21 @@ struct HeadSpan {
   bool there, last;
 };
 __device__ __forceinline__ HeadSpan head_span(const HeadChunk& c) {
-  const int64_t n = c.count ? (int64_t)*c.count : c.total;
-  const int64_t chunks = n > c.cap ? (n + c.cap - 1) / c.cap : 1;
-  const int64_t each = ((n + chunks - 1) / chunks + 255) / 256 * 256;
+  // (at most 2^30 rows: 32 bits, whose division is short, and none where one chunk is all; every workgroup begins with this)
+  const uint32_t n = c.count ? (uint32_t)*c.count : (uint32_t)c.total, cap = (uint32_t)c.cap;
   HeadSpan s;
-  s.first = c.index * each;
-  const int64_t left = n - s.first;
-  s.rows = (int32_t)(left < 0 ? 0 : left < each ? left : each);
-  s.there = c.index < chunks;
-  s.last = c.index == chunks - 1;
+  if (n <= cap) {
+    s.first = 0;
+    s.rows = c.index == 0 ? (int32_t)n : 0;
+    s.there = s.last = c.index == 0;
+    return s;
+  }
+  const uint32_t chunks = (n + cap - 1) / cap, each = ((n + chunks - 1) / chunks + 255) / 256 * 256, index = (uint32_t)c.index;
+  s.there = index < chunks;
+  const uint32_t first = s.there ? index * each : n;
+  s.first = first;
+  s.rows = (int32_t)(first >= n ? 0 : n - first < each ? n - first : each);
+  s.last = index == chunks - 1;
   return s;
 }
 

@@ -43,14 +43,13 @@ __device__ __forceinline__ f32x4 load_columns(const uint16_t* in, int n, int N) 
 // ceil(tiles s / 256) rounds of K / s and what a tile costs besides (about 14 steps of 32, of which a step takes 0.8 us); the pieces are written and
 // read once more, at about 4 bytes per ns.  130 tiles of 1,152 columns over 262,144 (6,554 rows): 5.0 ms in one piece.
 constexpr int kUnits = 256;
-__host__ __device__ inline int hidden_pieces(int tiles, int64_t rows, int K, int N, int most) {
+__host__ __device__ inline int hidden_pieces(int tiles, int rows, int K, int N, int most) {
   const int steps = (K + kHeadStep - 1) / kHeadStep;
-  const int64_t join = rows * N * 8 / 3200 + 4000;  // of one piece, in 1/1000 steps
+  const float join = (float)rows * (float)N * (8.0f / 3.2e6f);  // of one piece, in steps
   int best = 1;
-  int64_t least = (int64_t)((tiles + kUnits - 1) / kUnits) * (steps + 14) * 1000;
-  for (int s = 2; s <= most; s += s < 8 ? 1 : s < 16 ? 2 : s < 64 ? 8 : 32) {
-    if (steps / s < 4) break;
-    const int64_t t = ((int64_t)tiles * s + kUnits - 1) / kUnits * ((steps + s - 1) / s + 14) * 1000 + join * s + 5000;
+  float least = (float)((tiles + kUnits - 1) / kUnits) * (float)(steps + 14);
+  for (int s = 2; s <= most && s * 4 <= steps; s += s < 8 ? 1 : s < 16 ? 2 : s < 64 ? 8 : 32) {
+    const float t = (float)((tiles * s + kUnits - 1) / kUnits) * ((float)steps / (float)s + 14.0f) + join * (float)s + 9.0f;
     if (t < least) {
       least = t;
       best = s;
@@ -254,7 +253,7 @@ int head_hidden_splits(int64_t rows, int32_t K, int32_t N) {
   const HiddenTile t = hidden_tile(rows, K, N);
   const int64_t tiles = (rows + t.rows - 1) / t.rows * ((N + t.columns - 1) / t.columns);
   if (tiles > 4 * kUnits) return 1;
-  const int s = hidden_pieces((int)tiles, rows, K, N, kUnits);
+  const int s = hidden_pieces((int)tiles, (int)rows, K, N, kUnits);
   return s + s / 2 < 4 ? 4 : s + s / 2;
 }
 

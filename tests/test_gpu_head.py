@@ -142,6 +142,39 @@ def test_loss_in_chunks(T):
     check_loss(s, grad_scale=0.9, ce=0.1, workspace=torch.empty(least, dtype=torch.uint8, device=dev()))
 
 
+@pytest.mark.parametrize("scored", [2500, 200, 0])
+def test_loss_in_chunks_accumulates(scored):
+    T, V, D = 2500, 700, 72
+    s = inputs(T, V, D, 6, True)
+    s["mask"].fill_(1)
+    s["mask"][scored:] = 0
+    d = binding.HeadDesc(T, V, D, D, D, D, D, 0, 6, 15, 1.0, 0.9, 0.1, 0.0)
+    ws = torch.empty(binding.load().npd_head_workspace_bytes(d, binding.NPD_HEAD_LOSS), dtype=torch.uint8, device=dev())
+    start = dict(grad_weight=torch.randn((V, D), device=dev()).to(torch.bfloat16),
+                 grad_bias=torch.randn(V, device=dev()).to(torch.bfloat16))
+    want = loss64(s, grad_scale=0.9, ce=0.1)
+    got = run_loss(s, grad_scale=0.9, ce=0.1, accumulate=start, workspace=ws)
+    for n, a in start.items():
+        v, t = want[n]
+        v = v + a.double()
+        near(got[n], (v, t + 2.0 ** -8 * v.abs()), n)
+    near(got["grad_hidden"], want["grad_hidden"], "grad_hidden")
+
+
+def test_a_workspace_of_every_size_between():
+    """Chunks of 1,024, 2,048, 4,096 and 8,192 rows: the same results to rounding, nothing written behind the bytes asked for."""
+    T, V, D = 9000, 200, 24
+    s = inputs(T, V, D, 3, True, mask=0.9)
+    d = binding.HeadDesc(T, V, D, D, D, D, D, 0, 3, 7, 1.0, 0.9, 0.1, 0.0)
+    least = binding.load().npd_head_workspace_bytes(d, binding.NPD_HEAD_LOSS)
+    most = binding.load().npd_head_workspace_bytes_preferred(d, binding.NPD_HEAD_LOSS)
+    assert least < most
+    for n in {least, (least + most) // 2, most - 1, most}:
+        full = torch.full((n + 512,), 0x5a, dtype=torch.uint8, device=dev())
+        check_loss(s, grad_scale=0.9 / T, ce=0.1 / T, workspace=full[:n])
+        assert bool((full[n:] == 0x5a).all())
+
+
 def test_loss_more_rows_than_a_preferred_chunk():
     s = inputs(9000, 300, 40, 4, mask=0.97)
     check_loss(s, grad_scale=0.9 / 9000, ce=0.1 / 9000)
