@@ -159,33 +159,33 @@ npd_status gradients(const npd_head_desc& d, const Plan& p, const HeadChunk& chu
                      const HeadMatrix& h, const float* scale, const int32_t* rows, void* grad_hidden, void* grad_weight,
                      void* grad_bias, char* ws, hipStream_t stream) {
   const int32_t accumulate = (d.flags & NPD_HEAD_ACCUMULATE) != 0;
-  if (grad_hidden) {
-    HeadHiddenArgs a{};
-    a.chunk = chunk;
-    a.g = g;
-    a.w = w;
-    a.scale = scale;
-    a.rows = rows;
-    a.K = d.vocab;
-    a.N = d.width;
-    a.most_splits = p.splits;
-    a.partial = reinterpret_cast<float*>(ws + p.dh);
-    a.out = static_cast<uint16_t*>(grad_hidden);
-    a.out_stride = d.grad_hidden_stride;
-    NPD_TRY(launch_head_hidden(a, p.chunk_rows, stream));
-  }
-  if (grad_weight) {
-    HeadWeightArgs a{};
-    a.chunk = chunk;
-    a.g = g;
-    a.h = h;
-    a.M = d.vocab;
-    a.N = d.width;
-    a.partial = reinterpret_cast<float*>(ws + p.dw);
-    a.out = static_cast<uint16_t*>(grad_weight);
-    a.out_stride = d.grad_weight_stride;
-    a.accumulate = accumulate;
-    NPD_TRY(launch_head_weight(a, p.chunks, stream));
+  HeadHiddenArgs gh{};
+  gh.chunk = chunk;
+  gh.g = g;
+  gh.w = w;
+  gh.scale = scale;
+  gh.rows = rows;
+  gh.K = d.vocab;
+  gh.N = d.width;
+  gh.most_splits = p.splits;
+  gh.partial = reinterpret_cast<float*>(ws + p.dh);
+  gh.out = static_cast<uint16_t*>(grad_hidden);
+  gh.out_stride = d.grad_hidden_stride;
+  HeadWeightArgs gw{};
+  gw.chunk = chunk;
+  gw.g = g;
+  gw.h = h;
+  gw.M = d.vocab;
+  gw.N = d.width;
+  gw.partial = reinterpret_cast<float*>(ws + p.dw);
+  gw.out = static_cast<uint16_t*>(grad_weight);
+  gw.out_stride = d.grad_weight_stride;
+  gw.accumulate = accumulate;
+  if (grad_hidden && grad_weight && head_both_small(gh, gw, p.chunk_rows, p.chunks)) {
+    NPD_TRY(launch_head_both(gh, gw, p.chunk_rows, stream));
+  } else {
+    if (grad_hidden) NPD_TRY(launch_head_hidden(gh, p.chunk_rows, stream));
+    if (grad_weight) NPD_TRY(launch_head_weight(gw, p.chunks, stream));
   }
   if (grad_bias) {
     HeadBiasArgs a{};

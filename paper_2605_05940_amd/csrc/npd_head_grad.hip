@@ -67,14 +67,13 @@ __device__ __forceinline__ int pieces_of(const HeadHiddenArgs& a, int rows) {
 }
 
 template <int MF, int NF>
-__global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHiddenArgs a) {
+__device__ __forceinline__ void hidden_tile_of(const HeadHiddenArgs& a, unsigned block, char* lds) {
   using Product = HeadProduct<MF, NF, false, true, false>;
-  __shared__ __attribute__((aligned(1024))) char lds[Product::kLds];
   const HeadSpan span = head_span(a.chunk);
   if (!span.there || span.rows == 0) return;
   const int mt = (span.rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
   const int pieces = hidden_pieces(mt * nt, span.rows, a.K, a.N, a.most_splits);
-  const HeadTile tile = head_tile(blockIdx.x, mt, nt, pieces);
+  const HeadTile tile = head_tile(block, mt, nt, pieces);
   if (!tile.there) return;
   const int split = tile.piece;
   const int64_t m0 = (int64_t)tile.m * Product::kTileM;
@@ -112,6 +111,12 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHidden
   }
 }
 
+template <int MF, int NF>
+__global__ __launch_bounds__(kHeadThreads, 1) void head_hidden_kernel(HeadHiddenArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[HeadProduct<MF, NF, false, true, false>::kLds];
+  hidden_tile_of<MF, NF>(a, blockIdx.x, lds);
+}
+
 // joins the pieces of head_hidden_kernel in their order
 template <int MF, int NF>
 __global__ __launch_bounds__(256) void head_join_kernel(HeadHiddenArgs a) {
@@ -135,20 +140,20 @@ __global__ __launch_bounds__(256) void head_join_kernel(HeadHiddenArgs a) {
 
 // ADD: on top of the chunks before this one.  Whether a chunk is the last one is known on the device: both forms are launched, and
 // the one that does not apply ends at once (a kernel of both would spill: the sums and the next tile's fragments are 384 registers).
+// `block` of `blocks` workgroups that take one tile after the other.
 template <int MF, int NF, bool ADD, bool LAST, bool ACCUMULATE>
-__global__ __launch_bounds__(kHeadThreads, 1) void head_weight_kernel(HeadWeightArgs a) {
+__device__ __forceinline__ void weight_tiles_of(const HeadWeightArgs& a, unsigned block0, unsigned blocks, char* lds) {
   using Product = HeadProduct<MF, NF, true, true, false>;
-  __shared__ __attribute__((aligned(1024))) char lds[Product::kLds];
   const HeadSpan span = head_span(a.chunk);
   if (!span.there || span.last != LAST) return;
   const int mt = (a.M + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
-  HeadTile tile = head_tile(blockIdx.x, mt, nt);
+  HeadTile tile = head_tile(block0, mt, nt);
   if (!tile.there) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Product x;
   // rows of the chunk: behind the last one nothing is read
   x.start(a.g, a.h, (int64_t)tile.m * Product::kTileM, (int64_t)tile.n * Product::kTileN, 0, span.rows, lds);
-  for (unsigned block = blockIdx.x + gridDim.x; tile.there; block += gridDim.x) {
+  for (unsigned block = block0 + blocks; tile.there; block += blocks) {
   const HeadTile next = head_tile(block, mt, nt);
   const int64_t m0 = (int64_t)tile.m * Product::kTileM;
   const int n0 = tile.n * Product::kTileN;
@@ -185,6 +190,24 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_weight_kernel(HeadWeight
     }
   }
   }
+}
+
+template <int MF, int NF, bool ADD, bool LAST, bool ACCUMULATE>
+__global__ __launch_bounds__(kHeadThreads, 1) void head_weight_kernel(HeadWeightArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[HeadProduct<MF, NF, true, true, false>::kLds];
+  weight_tiles_of<MF, NF, ADD, LAST, ACCUMULATE>(a, blockIdx.x, gridDim.x, lds);
+}
+
+// Both gradients of a small call in one launch: the first `hidden` workgroups (a multiple of eight) have the hidden states'.
+template <bool ACCUMULATE>
+__global__ __launch_bounds__(kHeadThreads, 1) void head_small_kernel(HeadHiddenArgs h, HeadWeightArgs w, unsigned hidden) {
+  constexpr int kLds = HeadProduct<4, 4, false, true, false>::kLds;
+  static_assert(kLds == HeadProduct<4, 4, true, true, false>::kLds, "one array for both");
+  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+  if (blockIdx.x < hidden)
+    hidden_tile_of<4, 4>(h, blockIdx.x, lds);
+  else
+    weight_tiles_of<4, 4, false, true, ACCUMULATE>(w, blockIdx.x - hidden, gridDim.x - hidden, lds);
 }
 
 __global__ __launch_bounds__(256) void head_bias_kernel(HeadBiasArgs a) {
@@ -224,16 +247,26 @@ __global__ __launch_bounds__(256) void head_bias_join_kernel(HeadBiasArgs a) {
 }
 
 template <int MF, int NF>
-hipError_t launch_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
+int64_t hidden_blocks(const HeadHiddenArgs& a, int64_t rows) {
   using Product = HeadProduct<MF, NF, false, true, false>;
   const int64_t mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.N + Product::kTileN - 1) / Product::kTileN;
   // (fewer rows than the most may be split further: tiles and pieces together never need more workgroups than this)
-  const int64_t blocks = (mt * nt + 7) / 8 * 8 * a.most_splits;
-  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
-  const hipError_t e = launch_kernel(head_hidden_kernel<MF, NF>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
-  if (e != hipSuccess || a.most_splits == 1) return e;
+  return (mt * nt + 7) / 8 * 8 * a.most_splits;
+}
+
+template <int MF, int NF>
+hipError_t launch_join(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
+  if (a.most_splits == 1) return hipSuccess;
   const int64_t quads = rows * ((a.N + 3) / 4), join = (quads + 255) / 256;
   return launch_kernel(head_join_kernel<MF, NF>, dim3((unsigned)(join < 8192 ? join : 8192)), dim3(256), 0, stream, a);
+}
+
+template <int MF, int NF>
+hipError_t launch_hidden(const HeadHiddenArgs& a, int64_t rows, hipStream_t stream) {
+  const int64_t blocks = hidden_blocks<MF, NF>(a, rows);
+  if (blocks >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;
+  const hipError_t e = launch_kernel(head_hidden_kernel<MF, NF>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, stream, a);
+  return e == hipSuccess ? launch_join<MF, NF>(a, rows, stream) : e;
 }
 
 // rows and columns of a tile for a chunk of up to so many rows
@@ -286,6 +319,20 @@ hipError_t launch_head_weight(const HeadWeightArgs& a, int64_t chunks, hipStream
     return a.accumulate ? launch_weight<4, 4, false, true, true>(a, stream) : launch_weight<4, 4, false, true, false>(a, stream);
   if (a.accumulate) return add ? launch_weight<8, 8, true, true, true>(a, stream) : launch_weight<8, 8, false, true, true>(a, stream);
   return add ? launch_weight<8, 8, true, true, false>(a, stream) : launch_weight<8, 8, false, true, false>(a, stream);
+}
+
+bool head_both_small(const HeadHiddenArgs& h, const HeadWeightArgs& w, int64_t rows, int64_t chunks) {
+  return chunks == 1 && hidden_tile(rows, h.K, h.N).columns == 128 && head_small(w.M, w.N);
+}
+
+hipError_t launch_head_both(const HeadHiddenArgs& h, const HeadWeightArgs& w, int64_t rows, hipStream_t stream) {
+  using Product = HeadProduct<4, 4, true, true, false>;
+  const unsigned hidden = (unsigned)hidden_blocks<4, 4>(h, rows);
+  const int64_t mt = (w.M + Product::kTileM - 1) / Product::kTileM, nt = (w.N + Product::kTileN - 1) / Product::kTileN;
+  const dim3 grid(hidden + head_grid((mt * nt + 7) / 8 * 8));
+  const hipError_t e = w.accumulate ? launch_kernel(head_small_kernel<true>, grid, dim3(kHeadThreads), 0, stream, h, w, hidden)
+                                    : launch_kernel(head_small_kernel<false>, grid, dim3(kHeadThreads), 0, stream, h, w, hidden);
+  return e == hipSuccess ? launch_join<4, 4>(h, rows, stream) : e;
 }
 
 hipError_t launch_head_bias(const HeadBiasArgs& a, hipStream_t stream) {

@@ -127,25 +127,45 @@ __device__ __forceinline__ void gather_row(const HeadLossArgs& a, int64_t i, int
   uint16_t* h = const_cast<uint16_t*>(a.h.p) + i * a.h.stride;
   for (int d = threadIdx.x * 8; d < a.K; d += kRowThreads * 8) *reinterpret_cast<uint4*>(h + d) = load8_of(src, d, a.D);
   float top = -__builtin_inff();
-  for (int j = wave; j <= a.k; j += kRowThreads / kWave) {
-    const int id = entry_id(a, p, j);
-    float x = __builtin_nanf("");
-    if (id >= 0) {
-      const uint16_t* w = a.weight + id * a.weight_stride;
-      float s = 0.0f;
-      for (int d = lane * 8; d < a.D; d += kWave * 8) {
-        float u[8], v[8];
-        unpack8(load8_of(src, d, a.D), u);
-        unpack8(load8_of(w, d, a.D), v);
+  constexpr int kWaves = kRowThreads / kWave, kTogether = 4;  // rows of the weights requested together
+  for (int j0 = wave; j0 <= a.k; j0 += kWaves * kTogether) {
+    const uint16_t* w[kTogether];
+    int id[kTogether];
+    float sum[kTogether] = {};
 #pragma unroll
-        for (int t = 0; t < 8; ++t) s = __builtin_fmaf(u[t], v[t], s);
-      }
-      x = wave_sum(s);
-      if (a.bias) x += bf16_one(a.bias[id]);
-      if (a.cap != 0.0f) x = a.cap * tanhf(x / a.cap);
-      top = fmaxf(top, x);
+    for (int u = 0; u < kTogether; ++u) {
+      const int j = j0 + kWaves * u;
+      id[u] = j <= a.k ? entry_id(a, p, j) : -1;
+      w[u] = a.weight + (int64_t)(id[u] < 0 ? 0 : id[u]) * a.weight_stride;
     }
-    if (lane == 0) a.x[i * (1 + a.k) + j] = x;
+    for (int d = lane * 8; d < a.D; d += kWave * 8) {
+      float x[8];
+      unpack8(load8_of(src, d, a.D), x);
+      uint4 v[kTogether];
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) v[u] = id[u] < 0 ? make_uint4(0, 0, 0, 0) : load8_of(w[u], d, a.D);
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        float y[8];
+        unpack8(v[u], y);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) sum[u] = __builtin_fmaf(x[t], y[t], sum[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) {
+      const int j = j0 + kWaves * u;
+      if (j > a.k) break;
+      float x = wave_sum(sum[u]);
+      if (id[u] < 0) {
+        x = __builtin_nanf("");
+      } else {
+        if (a.bias) x += bf16_one(a.bias[id[u]]);
+        if (a.cap != 0.0f) x = a.cap * tanhf(x / a.cap);
+        top = fmaxf(top, x);
+      }
+      if (lane == 0) a.x[i * (1 + a.k) + j] = x;
+    }
   }
   if (lane == 0) tops[wave] = top;
   __syncthreads();
