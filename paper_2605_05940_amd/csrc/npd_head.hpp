@@ -41,7 +41,7 @@ struct HeadForwardArgs {
   const float* r0;      // [rows] a logit of the row times c, whole, or -1e30: the reference of columns not far above it
   float2* part;
   int32_t parts;
-  int32_t small;        // head_small(): parts of 64 columns
+  int32_t small;        // head_small(), head_few_small(): parts of 64 columns
   uint16_t* e;
   int64_t e_stride;
   uint16_t* out;
@@ -51,6 +51,10 @@ hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64
 
 // Rows that are so few that reading the weights is all the time: the weights go straight into registers, at any alignment.
 constexpr int64_t kHeadFewRows = 64;
+// 17 and more of them, and a vocabulary of less than a workgroup of 128 columns per compute unit: of 64 columns.  Measured (MI355X, us,
+// 20 / 48 rows, of 128 and of 64): 16,000 x 2,048 27.5, 20.5 / 42.6, 27.8; 50,048 x 1,024 22.7, 26.2 / 32.0, 30.5; 98,000 x 1,024 39.6,
+// 40.6 / 46.7, 57.8.
+inline bool head_few_small(int64_t rows, int64_t columns) { return rows > 16 && columns < 256 * 128; }
 hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream);
 
 // out[position of row m][n] = scale[m] sum_k g[m][k] w[k][n], k < K: the gradient of the hidden states.  k may be split into

@@ -62,7 +62,7 @@ struct Plan {
   int32_t K = 0;          // width, a multiple of eight
   int64_t e_stride = 0;
   int32_t parts = 0, part_columns = 0, splits = 1;
-  bool small = false;     // head_small()
+  bool small = false;     // head_small(), head_few_small()
   bool few = false;       // rows that head_few_kernel takes
   bool pack_w = false, pack_h = false, pack_g = false;
   size_t rows = 0, count = 0, h = 0, hs = 0, x = 0, r0 = 0, part = 0, e = 0, scale = 0, w = 0, dw = 0, dh = 0, pieces = 0, db = 0;
@@ -88,7 +88,7 @@ Plan make_plan(const npd_head_desc& d, int op, int32_t cap) {
   // an odd number of 128-byte lines between rows: a tile reads 256 rows at one column, which would else come from few channels
   p.e_stride = up(d.vocab, 64);
   if (p.e_stride / 64 % 2 == 0) p.e_stride += 64;
-  p.small = !p.few && head_small(p.chunk_rows, d.vocab);
+  p.small = p.few ? head_few_small(T, d.vocab) : head_small(p.chunk_rows, d.vocab);
   p.part_columns = p.small ? kHeadSmallPart : kHeadPart;
   p.parts = (d.vocab + p.part_columns - 1) / p.part_columns;
   if (gh) p.splits = head_hidden_splits(p.chunk_rows, d.vocab, d.width);

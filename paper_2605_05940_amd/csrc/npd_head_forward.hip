@@ -146,23 +146,25 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
   }
 }
 
-// The end of a workgroup's 128 columns of up to 64 rows, which lie in LDS as [row][kHeadPart]: a wave per row, two columns per
+// The end of a workgroup's PART columns of up to 64 rows, which lie in LDS as [row][PART]: a wave per row, PART / 64 columns per
 // lane.
-template <HeadForward WHAT, bool CAP>
+template <HeadForward WHAT, bool CAP, int PART>
 __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const float* x, int rows) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const SoftCap soft(CAP ? a.cap : 1.0f);
-  const int n = blockIdx.x * kHeadPart + 2 * lane;
-  float bias[2] = {0.0f, 0.0f};
+  constexpr int N = PART / kWave;
+  const int n = blockIdx.x * PART + N * lane;
+  float bias[N] = {};
   if (a.bias) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) bias[e] = n + e < a.V ? bf16_one(a.bias[n + e]) : 0.0f;
+    for (int e = 0; e < N; ++e) bias[e] = n + e < a.V ? bf16_one(a.bias[n + e]) : 0.0f;
   }
   for (int m = wave; m < rows; m += kHeadThreads / kWave) {
-    float y[2], slope[2] = {1.0f, 1.0f};
+    float y[N], slope[N];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      y[e] = x[m * kHeadPart + 2 * lane + e] + bias[e];
+    for (int e = 0; e < N; ++e) {
+      y[e] = x[m * PART + N * lane + e] + bias[e];
+      slope[e] = 1.0f;
       if constexpr (CAP) {
         const float th = soft.tanh_of(y[e]);
         y[e] = soft.cap * th;
@@ -171,27 +173,38 @@ __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const f
     }
     if constexpr (WHAT == kHeadLogits) {
       uint16_t* out = a.out + m * a.out_stride + n;
-      const uint32_t v = pack_bf16(y[0], y[1]);
-      if (n + 2 <= a.V)
+      if (N == 2 && n + 2 <= a.V) {
+        const uint32_t v = pack_bf16(y[0], y[N - 1]);
         __builtin_memcpy(out, &v, 4);
-      else if (n < a.V)
-        *out = (uint16_t)v;
+      } else if (n < a.V) {
+        *out = one_bf16(y[0]);
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < N; ++e)
         if (n + e >= a.V) y[e] = -__builtin_inff();
-      float top = fmaxf(y[0], y[1]);
+      float top = fmaxf(y[0], y[N - 1]);
 #pragma unroll
       for (int off = kWave / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
       const float r0 = a.r0[m], u = top * a.c;
       const float r = u > r0 + kHeadHeadroom ? __builtin_rintf(u) : r0;
-      float g[2];
+      float g[N], z = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) g[e] = exp2_fast(__builtin_fmaf(y[e], a.c, -r));
-      const float z = wave_sum(g[0] + g[1]);
+      for (int e = 0; e < N; ++e) {
+        g[e] = exp2_fast(__builtin_fmaf(y[e], a.c, -r));
+        z += g[e];
+        g[e] *= slope[e];
+      }
+      z = wave_sum(z);
       if constexpr (WHAT == kHeadSumsKept) {
         // (a part's columns end within the row: its pitch is a multiple of 64 that covers V)
-        if (n < a.e_stride) *reinterpret_cast<uint32_t*>(a.e + m * a.e_stride + n) = pack_bf16(g[0] * slope[0], g[1] * slope[1]);
+        uint16_t* e = a.e + m * a.e_stride + n;
+        if (n < a.e_stride) {
+          if constexpr (N == 2)
+            *reinterpret_cast<uint32_t*>(e) = pack_bf16(g[0], g[1]);
+          else
+            *e = one_bf16(g[0]);
+        }
       }
       if (lane == 0) a.part[(int64_t)m * a.parts + blockIdx.x] = make_float2(r, z);
     }
@@ -278,27 +291,28 @@ __global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_ker
       }
   }
   __syncthreads();
-  finish_columns<WHAT, CAP>(a, &x[0][0], span.rows);
+  finish_columns<WHAT, CAP, kHeadPart>(a, &x[0][0], span.rows);
 }
 
-// The same for up to 16 RT rows: a wave reads the weights of 32 columns straight into the fragments of 16 x 16 x 32 products (64
-// bytes of 16 rows per load, the next 64 with the one after it: 5 TB/s), 8 KB at a time; the hidden states go through LDS, 128
+// The same for up to 16 RT rows: a wave reads the weights of 16 FC columns straight into the fragments of 16 x 16 x 32 products (64
+// bytes of 16 rows per load, the next 64 with the one after it: 5 TB/s), 4 FC KB at a time; the hidden states go through LDS, 128
 // values of k of all rows at a time, so that a compute unit reads them once and not once per wave.
-template <int RT, HeadForward WHAT, bool CAP>
+template <int RT, int FC, HeadForward WHAT, bool CAP>
 __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardArgs a) {
+  constexpr int kPart = 64 * FC;  // columns of the workgroup
   constexpr int kBlock = 128, kSteps = kBlock / kHeadStep;
   constexpr int kPitch = kBlock + 8;  // (rows 17 groups of 16 bytes apart: 16 rows' reads lie in 16 different ones of 256 bytes)
   __shared__ __attribute__((aligned(16))) union {
     uint16_t h[2][16 * RT][kPitch];
-    float x[16 * RT][kHeadPart];
+    float x[16 * RT][kPart];
   } lds;
   const HeadSpan span = head_span(a.chunk);
   if (span.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-  const int v0 = blockIdx.x * kHeadPart + wave * 32;
-  const uint16_t* w[2];
+  const int v0 = blockIdx.x * kPart + wave * 16 * FC;
+  const uint16_t* w[FC];
 #pragma unroll
-  for (int f = 0; f < 2; ++f) {
+  for (int f = 0; f < FC; ++f) {
     const int v = v0 + 16 * f + i;
     w[f] = a.w.p + (int64_t)(v < a.V ? v : a.V - 1) * a.w.stride;
   }
@@ -310,9 +324,9 @@ __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardAr
     const int m = 16 * t + (threadIdx.x >> 4);
     h[t] = a.q.p + (int64_t)(m < span.rows ? m : span.rows - 1) * a.q.stride;
   }
-  f32x4 acc[2][RT];
+  f32x4 acc[FC][RT];
 #pragma unroll
-  for (int f = 0; f < 2; ++f)
+  for (int f = 0; f < FC; ++f)
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int whole = a.D / kBlock, blocks = (a.D + kBlock - 1) / kBlock;
@@ -327,18 +341,18 @@ __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardAr
   for (int n = 0; n < blocks; ++n) {
     const int block = n < whole ? at : whole;
     if (n < whole) at = at + 1 == whole ? 0 : at + 1;
-    bf16x8 wv[kSteps][2];
+    bf16x8 wv[kSteps][FC];
     const int d = block * kBlock + 8 * g;
     if (block < whole) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int f = 0; f < 2; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8(w[f] + d + s * kHeadStep));
+        for (int f = 0; f < FC; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8(w[f] + d + s * kHeadStep));
     } else {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int f = 0; f < 2; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8_of(w[f], d + s * kHeadStep, a.D));
+        for (int f = 0; f < FC; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8_of(w[f], d + s * kHeadStep, a.D));
     }
     // (two buffers: what is written here was last read before the barrier of the block before)
 #pragma unroll
@@ -351,18 +365,18 @@ __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardAr
       for (int t = 0; t < RT; ++t) {
         const bf16x8 y = *reinterpret_cast<const bf16x8*>(&lds.h[n & 1][16 * t + i][8 * g + s * kHeadStep]);
 #pragma unroll
-        for (int f = 0; f < 2; ++f) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s][f], y, acc[f][t], 0, 0, 0);
+        for (int f = 0; f < FC; ++f) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s][f], y, acc[f][t], 0, 0, 0);
       }
     }
   }
   __syncthreads();
   // acc[f][t][e]: row 16 t + i, column v0 + 16 f + 4 g + e
 #pragma unroll
-  for (int f = 0; f < 2; ++f)
+  for (int f = 0; f < FC; ++f)
 #pragma unroll
-    for (int t = 0; t < RT; ++t) *reinterpret_cast<f32x4*>(&lds.x[16 * t + i][wave * 32 + 16 * f + 4 * g]) = acc[f][t];
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<f32x4*>(&lds.x[16 * t + i][wave * 16 * FC + 16 * f + 4 * g]) = acc[f][t];
   __syncthreads();
-  finish_columns<WHAT, CAP>(a, &lds.x[0][0], span.rows);
+  finish_columns<WHAT, CAP, kPart>(a, &lds.x[0][0], span.rows);
 }
 
 template <HeadForward WHAT, bool CAP>
@@ -371,8 +385,11 @@ hipError_t launch_few(const HeadForwardArgs& a, int64_t rows, hipStream_t stream
   if (rows <= 4) return launch_kernel(head_tokens_kernel<1, 8, WHAT, CAP>, grid, block, 0, stream, a);
   if (rows <= 8) return launch_kernel(head_tokens_kernel<2, 8, WHAT, CAP>, grid, block, 0, stream, a);
   if (rows <= 16) return launch_kernel(head_tokens_kernel<4, 4, WHAT, CAP>, grid, block, 0, stream, a);
-  if (rows <= 32) return launch_kernel(head_few_kernel<2, WHAT, CAP>, grid, block, 0, stream, a);
-  return launch_kernel(head_few_kernel<4, WHAT, CAP>, grid, block, 0, stream, a);
+  const dim3 halves((unsigned)((a.V + kHeadSmallPart - 1) / kHeadSmallPart));
+  const dim3 g = a.small ? halves : grid;
+  if (rows <= 32) return launch_kernel(a.small ? head_few_kernel<2, 1, WHAT, CAP> : head_few_kernel<2, 2, WHAT, CAP>, g, block, 0, stream, a);
+  if (rows <= 48) return launch_kernel(a.small ? head_few_kernel<3, 1, WHAT, CAP> : head_few_kernel<3, 2, WHAT, CAP>, g, block, 0, stream, a);
+  return launch_kernel(a.small ? head_few_kernel<4, 1, WHAT, CAP> : head_few_kernel<4, 2, WHAT, CAP>, g, block, 0, stream, a);
 }
 
 template <int MF, int NF, HeadForward WHAT, bool CAP>

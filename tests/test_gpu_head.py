@@ -98,6 +98,20 @@ def test_loss_forward_only(T, V, D, k, gs, ce, tau, bias, cap):
     check_loss(inputs(T, V, D, k, bias, seed=1), cap=cap, tau=tau, grads=())
 
 
+@pytest.mark.parametrize("T", [3, 4, 5, 8, 9, 16, 17, 31, 33, 48, 49, 64])
+@pytest.mark.parametrize("V,D,bias,cap", [(515, 129, True, 0.0), (33000, 40, False, 30.0), (1000, 256, True, 2.0)])
+def test_few_rows(T, V, D, bias, cap):
+    """Every number of rows that has a kernel of its own, both widths of its workgroups: scalars, gradients, logits."""
+    s = inputs(T, V, D, 3, bias, mask=0.9)
+    check_loss(s, cap=cap, grad_scale=0.9, ce=0.1)
+    full, out = padded(T, V, V + 3)
+    npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], softcap=cap, logits_out=out)
+    torch.cuda.synchronize()
+    untouched(full, out)
+    x, _, dx = head64(s, cap)
+    near(out, (x, dx + 2.0 ** -8 * (x.abs() + dx)), "logits")
+
+
 @pytest.mark.parametrize("grads", [("hidden",), ("weight",), ("bias",), ("hidden", "bias")])
 def test_loss_any_gradient_alone(grads):
     s = inputs(150, 777, 96, 12, True)
