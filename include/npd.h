@@ -463,6 +463,9 @@ size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op);
  *   dev_status   int32 [1] or NULL: a label (if used) or id outside [0, V) gives NaN scalars, a NaN row of grad_hidden and
  *                no part in grad_weight and grad_bias
  *   workspace    device, >= npd_head_workspace_bytes(desc, NPD_HEAD_LOSS) bytes, 256-byte aligned; scratch of the call
+ *                (contents meaningless before and after); must not overlap any other argument, and two calls that may
+ *                run at the same time need one each, likewise two captured graphs (NPD_ERR_WORKSPACE: too small or
+ *                unaligned)
  *
  * NPD_ERR_UNSUPPORTED: tau != 1 together with nll_tok, lse_tok or ce_grad_scale != 0 (quantities at tau = 1: ask for them in
  * a call of their own), and gradients with grad_scale and ce_grad_scale of opposite sign.  NPD_ERR_VALUE: ce_grad_scale != 0

@@ -36,113 +36,113 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
   Product x;
   x.start(q, a.w, (int64_t)tile.m * Product::kTileM, (int64_t)tile.n * Product::kTileN, 0, a.K, lds);
   for (unsigned block = blockIdx.x + gridDim.x; tile.there; block += gridDim.x) {
-  const HeadTile next = head_tile(block, mt, nt);
-  const int64_t m0 = (int64_t)tile.m * Product::kTileM;
-  const int n0 = tile.n * Product::kTileN;
-  const int64_t mw = m0 + (wave >> 1) * 16 * MF + (lane & 15);  // + 16 i
-  const int columns = n0 + (x.wave & 1) * 16 * NF;              // of the wave
-  const int nw = columns + 8 * (lane >> 4);                     // + 32 j + 0 .. 7, fragments 2 j and 2 j + 1
+    const HeadTile next = head_tile(block, mt, nt);
+    const int64_t m0 = (int64_t)tile.m * Product::kTileM;
+    const int n0 = tile.n * Product::kTileN;
+    const int64_t mw = m0 + (wave >> 1) * 16 * MF + (lane & 15);  // + 16 i
+    const int columns = n0 + (x.wave & 1) * 16 * NF;              // of the wave
+    const int nw = columns + 8 * (lane >> 4);                     // + 32 j + 0 .. 7, fragments 2 j and 2 j + 1
 #pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.bias) {
-      const int n = nw + 32 * (j >> 1) + 4 * (j & 1);
+    for (int j = 0; j < NF; ++j) {
+      f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (a.bias) {
+        const int n = nw + 32 * (j >> 1) + 4 * (j & 1);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) b[t] = n + t < a.V ? bf16_one(a.bias[n + t]) : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < MF; ++i) x.acc[i][j] = b;
-  }
-  float r0[MF];  // (requested here: there is no time to wait for them once the products are done)
-  if constexpr (WHAT != kHeadLogits) {
-#pragma unroll
-    for (int i = 0; i < MF; ++i) r0[i] = a.r0[mw + 16 * i < span.rows ? mw + 16 * i : 0];
-  }
-  x.run(q, a.w, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, a.K, lds);
-  tile = next;
-
-  const SoftCap soft(CAP ? a.cap : 1.0f);
-  const float c = CAP ? a.cap * a.c : a.c;
-  const bool edge = n0 + Product::kTileN > a.V;  // uniform
-#pragma unroll
-  for (int i = 0; i < MF; ++i) {
-    __builtin_amdgcn_sched_barrier(0);  // (a row's sums at a time: the fragments of the next tile are in registers already)
-    const int64_t m = mw + 16 * i;
-    const bool row = m < span.rows;
-    if constexpr (WHAT == kHeadLogits) {
-      uint16_t* out = a.out + (row ? m : 0) * a.out_stride;
-#pragma unroll
-      for (int j = 0; j < NF; j += 2) {
-        const int n = nw + 16 * j;
-        uint32_t v[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          float lo = x.acc[i][j + (t >> 1)][2 * (t & 1)], hi = x.acc[i][j + (t >> 1)][2 * (t & 1) + 1];
-          if constexpr (CAP) {
-            lo = soft.cap * soft.tanh_of(lo);
-            hi = soft.cap * soft.tanh_of(hi);
-          }
-          v[t] = pack_bf16(lo, hi);
-        }
-        if (!row) continue;
-        if (columns + 16 * j + 32 <= a.V) {
-          stream8(out + n, make_uint4(v[0], v[1], v[2], v[3]));
-        } else {
-#pragma unroll
-          for (int t = 0; t < 8; ++t)
-            if (n + t < a.V) out[n + t] = (uint16_t)(v[t >> 1] >> (16 * (t & 1)));
-        }
+        for (int t = 0; t < 4; ++t) b[t] = n + t < a.V ? bf16_one(a.bias[n + t]) : 0.0f;
       }
-    } else {
-      // logits, or with a soft cap their tanh: that times cap is the logit, and one less its square the slope
-      float v[4 * NF];
-      float top = -__builtin_inff();
 #pragma unroll
-      for (int j = 0; j < NF; ++j)
+      for (int i = 0; i < MF; ++i) x.acc[i][j] = b;
+    }
+    float r0[MF];  // (requested here: there is no time to wait for them once the products are done)
+    if constexpr (WHAT != kHeadLogits) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) v[4 * j + t] = CAP ? soft.tanh_of(x.acc[i][j][t]) : x.acc[i][j][t];
-      if (edge) {  // (columns that are not there: e is 0, and with a finite slope e times it)
+      for (int i = 0; i < MF; ++i) r0[i] = a.r0[mw + 16 * i < span.rows ? mw + 16 * i : 0];
+    }
+    x.run(q, a.w, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, a.K, lds);
+    tile = next;
+
+    const SoftCap soft(CAP ? a.cap : 1.0f);
+    const float c = CAP ? a.cap * a.c : a.c;
+    const bool edge = n0 + Product::kTileN > a.V;  // uniform
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      __builtin_amdgcn_sched_barrier(0);  // (a row's sums at a time: the fragments of the next tile are in registers already)
+      const int64_t m = mw + 16 * i;
+      const bool row = m < span.rows;
+      if constexpr (WHAT == kHeadLogits) {
+        uint16_t* out = a.out + (row ? m : 0) * a.out_stride;
+#pragma unroll
+        for (int j = 0; j < NF; j += 2) {
+          const int n = nw + 16 * j;
+          uint32_t v[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            float lo = x.acc[i][j + (t >> 1)][2 * (t & 1)], hi = x.acc[i][j + (t >> 1)][2 * (t & 1) + 1];
+            if constexpr (CAP) {
+              lo = soft.cap * soft.tanh_of(lo);
+              hi = soft.cap * soft.tanh_of(hi);
+            }
+            v[t] = pack_bf16(lo, hi);
+          }
+          if (!row) continue;
+          if (columns + 16 * j + 32 <= a.V) {
+            stream8(out + n, make_uint4(v[0], v[1], v[2], v[3]));
+          } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+              if (n + t < a.V) out[n + t] = (uint16_t)(v[t >> 1] >> (16 * (t & 1)));
+          }
+        }
+      } else {
+        // logits, or with a soft cap their tanh: that times cap is the logit, and one less its square the slope
+        float v[4 * NF];
+        float top = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
-            if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = CAP ? -1.0e18f : -__builtin_inff();
-      }
+          for (int t = 0; t < 4; ++t) v[4 * j + t] = CAP ? soft.tanh_of(x.acc[i][j][t]) : x.acc[i][j][t];
+        if (edge) {  // (columns that are not there: e is 0, and with a finite slope e times it)
 #pragma unroll
-      for (int p = 0; p < 4 * NF; p += 2) top = max3(top, v[p], v[p + 1]);
-      top = fmaxf(top, __shfl_xor(top, 16, kWave));
-      top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float u = top * c;
-      const float r = u > r0[i] + kHeadHeadroom ? __builtin_rintf(u) : r0[i];
-      float z = 0.0f;
-      uint16_t* e = WHAT == kHeadSumsKept ? a.e + (row ? m : 0) * a.e_stride : nullptr;
+          for (int j = 0; j < NF; ++j)
 #pragma unroll
-      for (int j = 0; j < NF; j += 2) {
-        uint32_t w[4];
+            for (int t = 0; t < 4; ++t)
+              if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = CAP ? -1.0e18f : -__builtin_inff();
+        }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int p = 4 * j + 2 * t;
-          float lo = exp2_fast(__builtin_fmaf(v[p], c, -r)), hi = exp2_fast(__builtin_fmaf(v[p + 1], c, -r));
-          z += lo;
-          z += hi;
-          if constexpr (CAP && WHAT == kHeadSumsKept) {
-            lo *= __builtin_fmaf(-v[p], v[p], 1.0f);
-            hi *= __builtin_fmaf(-v[p + 1], v[p + 1], 1.0f);
+        for (int p = 0; p < 4 * NF; p += 2) top = max3(top, v[p], v[p + 1]);
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float u = top * c;
+        const float r = u > r0[i] + kHeadHeadroom ? __builtin_rintf(u) : r0[i];
+        float z = 0.0f;
+        uint16_t* e = WHAT == kHeadSumsKept ? a.e + (row ? m : 0) * a.e_stride : nullptr;
+#pragma unroll
+        for (int j = 0; j < NF; j += 2) {
+          uint32_t w[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int p = 4 * j + 2 * t;
+            float lo = exp2_fast(__builtin_fmaf(v[p], c, -r)), hi = exp2_fast(__builtin_fmaf(v[p + 1], c, -r));
+            z += lo;
+            z += hi;
+            if constexpr (CAP && WHAT == kHeadSumsKept) {
+              lo *= __builtin_fmaf(-v[p], v[p], 1.0f);
+              hi *= __builtin_fmaf(-v[p + 1], v[p + 1], 1.0f);
+            }
+            if constexpr (WHAT == kHeadSumsKept) w[t] = pack_bf16(lo, hi);
           }
-          if constexpr (WHAT == kHeadSumsKept) w[t] = pack_bf16(lo, hi);
+          if constexpr (WHAT == kHeadSumsKept) {
+            const int n = nw + 16 * j;
+            // (rows of e begin on 16 bytes, n is a multiple of 8)
+            if (row && (columns + 16 * j + 32 <= a.V || n < a.e_stride)) stream8(e + n, make_uint4(w[0], w[1], w[2], w[3]));
+          }
         }
-        if constexpr (WHAT == kHeadSumsKept) {
-          const int n = nw + 16 * j;
-          // (rows of e begin on 16 bytes, n is a multiple of 8)
-          if (row && (columns + 16 * j + 32 <= a.V || n < a.e_stride)) stream8(e + n, make_uint4(w[0], w[1], w[2], w[3]));
-        }
+        z += __shfl_xor(z, 16, kWave);
+        z += __shfl_xor(z, 32, kWave);
+        const int part = columns / kPart;
+        if (lane < 16 && row && part < a.parts) a.part[m * a.parts + part] = make_float2(r, z);
       }
-      z += __shfl_xor(z, 16, kWave);
-      z += __shfl_xor(z, 32, kWave);
-      const int part = columns / kPart;
-      if (lane < 16 && row && part < a.parts) a.part[m * a.parts + part] = make_float2(r, z);
     }
-  }
   }
 }
 

@@ -41,7 +41,7 @@ __device__ __forceinline__ f32x4 load_columns(const uint16_t* in, int n, int N) 
 
 // How many pieces the contraction over K is split into.  A compute unit has one tile at a time, so `tiles` in s pieces take
 // ceil(tiles s / 256) rounds of K / s and what a tile costs besides (about 14 steps of 32, of which a step takes 0.8 us); the pieces are written and
-// read once more, at about 4 bytes per ns.  130 tiles of 1,152 columns over 262,144 (6,554 rows): 5.0 ms in one piece.
+// read once more, at about 3.2 bytes per ns.  Measured (MI355X): 130 tiles of 6,554 x 1,152 over 262,144 5.0 ms in one piece, 3.5 in 16.
 constexpr int kUnits = 256;
 __host__ __device__ inline int hidden_pieces(int tiles, int rows, int K, int N, int most) {
   const int steps = (K + kHeadStep - 1) / kHeadStep;
@@ -154,41 +154,41 @@ __device__ __forceinline__ void weight_tiles_of(const HeadWeightArgs& a, unsigne
   // rows of the chunk: behind the last one nothing is read
   x.start(a.g, a.h, (int64_t)tile.m * Product::kTileM, (int64_t)tile.n * Product::kTileN, 0, span.rows, lds);
   for (unsigned block = block0 + blocks; tile.there; block += blocks) {
-  const HeadTile next = head_tile(block, mt, nt);
-  const int64_t m0 = (int64_t)tile.m * Product::kTileM;
-  const int n0 = tile.n * Product::kTileN;
+    const HeadTile next = head_tile(block, mt, nt);
+    const int64_t m0 = (int64_t)tile.m * Product::kTileM;
+    const int n0 = tile.n * Product::kTileN;
 #pragma unroll
-  for (int i = 0; i < MF; ++i)
+    for (int i = 0; i < MF; ++i)
 #pragma unroll
-    for (int j = 0; j < NF; ++j) x.acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  x.run(a.g, a.h, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, span.rows, lds);
-  tile = next;
-  const int64_t mw = m0 + (wave >> 1) * 16 * MF + (lane & 15);
-  const int columns = n0 + (x.wave & 1) * 16 * NF, nw = columns + 4 * (lane >> 4);
+      for (int j = 0; j < NF; ++j) x.acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    x.run(a.g, a.h, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, span.rows, lds);
+    tile = next;
+    const int64_t mw = m0 + (wave >> 1) * 16 * MF + (lane & 15);
+    const int columns = n0 + (x.wave & 1) * 16 * NF, nw = columns + 4 * (lane >> 4);
 #pragma unroll
-  for (int i = 0; i < MF; ++i) {
-    __builtin_amdgcn_sched_barrier(0);  // (a row's sums at a time)
-    const int64_t m = mw + 16 * i;
-    if (m >= a.M) continue;
-    f32x4* partial = reinterpret_cast<f32x4*>(a.partial + m * pitch4(a.N));
-    uint16_t* out = a.out + m * a.out_stride;
+    for (int i = 0; i < MF; ++i) {
+      __builtin_amdgcn_sched_barrier(0);  // (a row's sums at a time)
+      const int64_t m = mw + 16 * i;
+      if (m >= a.M) continue;
+      f32x4* partial = reinterpret_cast<f32x4*>(a.partial + m * pitch4(a.N));
+      uint16_t* out = a.out + m * a.out_stride;
 #pragma unroll
-    for (int j = 0; j < NF; j += 2) {
-      f32x4 v[2] = {x.acc[i][j], x.acc[i][j + 1]};
+      for (int j = 0; j < NF; j += 2) {
+        f32x4 v[2] = {x.acc[i][j], x.acc[i][j + 1]};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int n = nw + 16 * (j + t);
-        if constexpr (ADD) {
-          if (columns + 16 * (j + t) + 16 <= a.N || n < a.N) v[t] += partial[n / 4];
+        for (int t = 0; t < 2; ++t) {
+          const int n = nw + 16 * (j + t);
+          if constexpr (ADD) {
+            if (columns + 16 * (j + t) + 16 <= a.N || n < a.N) v[t] += partial[n / 4];
+          }
+          if constexpr (ACCUMULATE) v[t] += load_columns(out, n, a.N);
+          if constexpr (!LAST) {
+            if (columns + 16 * (j + t) + 16 <= a.N || n < a.N) partial[n / 4] = v[t];
+          }
         }
-        if constexpr (ACCUMULATE) v[t] += load_columns(out, n, a.N);
-        if constexpr (!LAST) {
-          if (columns + 16 * (j + t) + 16 <= a.N || n < a.N) partial[n / 4] = v[t];
-        }
+        if constexpr (LAST) store_two(out, nw + 16 * j, a.N, columns + 16 * j + 32 <= a.N, v[0], v[1]);
       }
-      if constexpr (LAST) store_two(out, nw + 16 * j, a.N, columns + 16 * j + 32 <= a.N, v[0], v[1]);
     }
-  }
   }
 }
 

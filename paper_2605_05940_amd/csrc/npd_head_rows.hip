@@ -184,8 +184,8 @@ __global__ __launch_bounds__(kRowThreads) void head_gather_kernel(HeadLossArgs a
 }
 
 // The same where one chunk holds every position, with what head_scan_kernel and head_zero_kernel do besides, in one launch: a
-// workgroup per position, which counts the scored positions in front of its own itself.  Measured (MI355X, 512 positions of 256
-// values): 5 us for the 19 of the four launches; 8,192 positions make 8,192 passes over a mask of 8 KB, out of L2.
+// workgroup per position, which counts the scored positions in front of its own itself.  Measured (MI355X, us): 512 positions of width
+// 256 5.8 for the 19.6 of the four launches, 8,192 of 1,152 39 for 46 (8,192 passes over a mask of 8 KB, out of the L2).
 __global__ __launch_bounds__(kRowThreads) void head_prepare_kernel(HeadRowsArgs r, HeadLossArgs a) {
   __shared__ int ired[kRowThreads / kWave];
   const int64_t p = blockIdx.x;
