@@ -9,7 +9,7 @@
 namespace npd {
 
 // Columns of one partial sum of a row: what a wave of the forward product holds of it, 128, or 64 with the small tiles.
-constexpr int kHeadPart = 128, kHeadSmallPart = 64;
+constexpr int kHeadPart = 128, kHeadSmallPart = 64, kHeadTokensPart = 32;
 
 // Tiles of 128 x 128 in place of 256 x 256: where there are so few that each has a compute unit to itself either way, a tile's own
 // time decides.  Measured (MI355X, loss of 512 positions of width 1,024 with the hidden states' / the weights' gradient, us, 256 / 128):
@@ -41,7 +41,8 @@ struct HeadForwardArgs {
   const float* r0;      // [rows] a logit of the row times c, whole, or -1e30: the reference of columns not far above it
   float2* part;
   int32_t parts;
-  int32_t small;        // head_small(), head_few_small(): parts of 64 columns
+  int32_t part_columns; // head_few_part(); 64: head_small(), 128
+  int32_t tokens;       // head_tokens()
   uint16_t* e;
   int64_t e_stride;
   uint16_t* out;
@@ -51,10 +52,20 @@ hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64
 
 // Rows that are so few that reading the weights is all the time: the weights go straight into registers, at any alignment.
 constexpr int64_t kHeadFewRows = 64;
-// 17 and more of them, and a vocabulary of less than a workgroup of 128 columns per compute unit: of 64 columns.  Measured (MI355X, us,
-// 20 / 48 rows, of 128 and of 64): 16,000 x 2,048 27.5, 20.5 / 42.6, 27.8; 50,048 x 1,024 22.7, 26.2 / 32.0, 30.5; 98,000 x 1,024 39.6,
-// 40.6 / 46.7, 57.8.
-inline bool head_few_small(int64_t rows, int64_t columns) { return rows > 16 && columns < 256 * 128; }
+// Up to eight of them are head_tokens_kernel's, unless rows of the weights begin on odd values: the loads that cost least there are
+// head_few_kernel's (49,152 x 4,095, 1 / 8 rows, MI355X: 132 / 178 us here, 109 there).  Nine rows of 151,936 x 2,048 take 177 us here, 113
+// there.
+inline bool head_tokens(int64_t rows, int64_t weight_stride) { return rows <= 8 && weight_stride % 2 == 0; }
+// Columns of a workgroup of either.  Narrower ones where 128 columns leave compute units without a workgroup, and always for rows
+// that begin on odd values.  Measured (MI355X, us, of 128 and narrower, weights out of the caches):
+//   head_tokens_kernel, 1 / 8 rows: 8,000 x 1,024 12.1, 9.5 / 17.1, 10.1; 16,000 x 2,048 20.2, 16.5 / 29.0, 18.8; 32,000 x 4,096 41.9, 52.1 /
+//   54.8, 47.6; 50,048 x 1,024 21.8, 23.6 / 26.7, 30.3; 32,000 x 512 (a wave has one block of k) 10.2, 12.8 / 13.0, 18.0
+//   head_few_kernel, 16 / 48 rows: 16,000 x 2,048 30.3, 22.5 / 37.6, 28.5; 32,000 x 4,096 62.2, 49.4 / 77.4, 65.8; 50,048 x 1,024 21.7, 26.4 /
+//   29.1, 28.0; 98,000 x 1,024 39.2, 43.6 / 42.3, 50.6; odd: 49,152 x 4,095 169, 110 / 177, 136; 100,003 x 1,023 71.1, 66.6 / 90.5, 84.5
+inline int head_few_part(int64_t rows, int64_t columns, int64_t width, int64_t weight_stride) {
+  if (head_tokens(rows, weight_stride)) return width >= 1024 && columns < 256 * (rows <= 4 ? 96 : 128) ? kHeadTokensPart : kHeadPart;
+  return weight_stride % 2 != 0 || columns < 256 * 128 ? kHeadSmallPart : kHeadPart;
+}
 hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream);
 
 // out[position of row m][n] = scale[m] sum_k g[m][k] w[k][n], k < K: the gradient of the hidden states.  k may be split into

@@ -62,8 +62,8 @@ struct Plan {
   int32_t K = 0;          // width, a multiple of eight
   int64_t e_stride = 0;
   int32_t parts = 0, part_columns = 0, splits = 1;
-  bool small = false;     // head_small(), head_few_small()
-  bool few = false;       // rows that head_few_kernel takes
+  bool tokens = false;    // head_tokens()
+  bool few = false;       // up to kHeadFewRows
   bool pack_w = false, pack_h = false, pack_g = false;
   size_t rows = 0, count = 0, h = 0, hs = 0, x = 0, r0 = 0, part = 0, e = 0, scale = 0, w = 0, dw = 0, dh = 0, pieces = 0, db = 0;
   size_t bytes = 0;
@@ -88,9 +88,11 @@ Plan make_plan(const npd_head_desc& d, int op, int32_t cap) {
   // an odd number of 128-byte lines between rows: a tile reads 256 rows at one column, which would else come from few channels
   p.e_stride = up(d.vocab, 64);
   if (p.e_stride / 64 % 2 == 0) p.e_stride += 64;
-  p.small = p.few ? head_few_small(T, d.vocab) : head_small(p.chunk_rows, d.vocab);
-  p.part_columns = p.small ? kHeadSmallPart : kHeadPart;
-  p.parts = (d.vocab + p.part_columns - 1) / p.part_columns;
+  p.tokens = p.few && head_tokens(T, d.weight_stride);
+  p.part_columns = p.few ? head_few_part(T, d.vocab, d.width, d.weight_stride) : head_small(p.chunk_rows, d.vocab) ? kHeadSmallPart : kHeadPart;
+  // (parts of 32: as many as two for each of 64, so that rows of e are written as far)
+  p.parts = p.part_columns == kHeadTokensPart ? (int32_t)(up(d.vocab, kHeadSmallPart) / kHeadTokensPart)
+                                              : (d.vocab + p.part_columns - 1) / p.part_columns;
   if (gh) p.splits = head_hidden_splits(p.chunk_rows, d.vocab, d.width);
   auto take = [&p](size_t bytes) {
     const size_t at = p.bytes;
@@ -335,7 +337,8 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   f.r0 = l.r0;
   f.part = part;
   f.parts = p.parts;
-  f.small = p.small;
+  f.part_columns = p.part_columns;
+  f.tokens = p.tokens;
   f.e = l.e;
   f.e_stride = p.e_stride;
 
@@ -401,7 +404,9 @@ npd_status npd_head_logits(const npd_head_desc* desc, const void* hidden, const 
   f.K = p.K;
   f.V = d.vocab;
   f.cap = d.softcap;
-  f.small = p.small;
+  f.parts = p.parts;
+  f.part_columns = p.part_columns;
+  f.tokens = p.tokens;
   f.out = static_cast<uint16_t*>(logits);
   f.out_stride = d.logits_stride;
   NPD_TRY((p.few ? launch_head_few : launch_head_forward)(f, kHeadLogits, T, on));

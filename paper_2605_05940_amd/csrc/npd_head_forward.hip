@@ -147,13 +147,14 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
 }
 
 // The end of a workgroup's PART columns of up to 64 rows, which lie in LDS as [row][PART]: a wave per row, PART / 64 columns per
-// lane.
+// lane (of 32, half the lanes have one).
 template <HeadForward WHAT, bool CAP, int PART>
 __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const float* x, int rows) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const SoftCap soft(CAP ? a.cap : 1.0f);
-  constexpr int N = PART / kWave;
-  const int n = blockIdx.x * PART + N * lane;
+  constexpr int N = PART < kWave ? 1 : PART / kWave;
+  const bool there = PART >= kWave || lane < PART;
+  const int n = there ? blockIdx.x * PART + N * lane : a.V, at = there ? N * lane : 0;
   float bias[N] = {};
   if (a.bias) {
 #pragma unroll
@@ -163,7 +164,7 @@ __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const f
     float y[N], slope[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      y[e] = x[m * PART + N * lane + e] + bias[e];
+      y[e] = x[m * PART + at + e] + bias[e];
       slope[e] = 1.0f;
       if constexpr (CAP) {
         const float th = soft.tanh_of(y[e]);
@@ -199,7 +200,7 @@ __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const f
       if constexpr (WHAT == kHeadSumsKept) {
         // (a part's columns end within the row: its pitch is a multiple of 64 that covers V)
         uint16_t* e = a.e + m * a.e_stride + n;
-        if (n < a.e_stride) {
+        if (there && n < a.e_stride) {
           if constexpr (N == 2)
             *reinterpret_cast<uint32_t*>(e) = pack_bf16(g[0], g[1]);
           else
@@ -217,87 +218,102 @@ __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const f
 // of 16 rows, 105 in pieces of 256 of four, 91 if the caches are told that nothing is read twice, as here; waves begin at
 // different places of their rows and wrap around, since rows of a power of two of bytes would else be read out of few memory
 // channels (126 us: 145).  A workgroup has 128 columns, a wave 4 G of them at a time.
-template <int NT, int G, HeadForward WHAT, bool CAP>
+//
+// PART 128: a wave has 32 columns of its own.  32: the four waves have the same ones and every fourth block of k, added up at the end.
+template <int NT, int PART, HeadForward WHAT, bool CAP>
 __global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_kernel(HeadForwardArgs a) {
-  __shared__ __attribute__((aligned(16))) float x[4 * NT][kHeadPart];
+  constexpr int kWaves = kHeadThreads / kWave, G = 8, kShare = PART == 4 * G ? kWaves : 1;
+  static_assert(PART == 4 * G * kWaves / kShare, "");
+  __shared__ __attribute__((aligned(16))) float x[kShare][4 * NT][PART];
   const HeadSpan span = head_span(a.chunk);
   if (span.rows == 0) return;
   typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 3, b = lane >> 2;
   constexpr int kBlock = 128;  // values of k per load
   const int blocks = a.D / kBlock, tail = blocks * kBlock + 8 * b;
-  const uint16_t* h[NT];
+  const int first = kShare > 1 ? wave : 0, mine = (blocks - first + kShare - 1) / kShare;  // blocks first, first + kShare ..
+  const int c0 = kShare > 1 ? 0 : wave * 4 * G;  // of the workgroup's columns
+  const uint16_t *h[NT], *w[G];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int m = 4 * t + i;
     h[t] = a.q.p + (int64_t)(m < span.rows ? m : span.rows - 1) * a.q.stride;
   }
-  for (int part = 0; part < 32 / (4 * G); ++part) {
-    const int c0 = wave * 32 + part * 4 * G;  // of the workgroup's columns
-    const uint16_t* w[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const int v = blockIdx.x * kHeadPart + c0 + 4 * g + i;
-      w[g] = a.w.p + (int64_t)(v < a.V ? v : a.V - 1) * a.w.stride;
-    }
-    f32x4 acc[G][NT];
+  for (int g = 0; g < G; ++g) {
+    const int v = blockIdx.x * PART + c0 + 4 * g + i;
+    w[g] = a.w.p + (int64_t)(v < a.V ? v : a.V - 1) * a.w.stride;
+  }
+  f32x4 acc[G][NT];
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+  for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[g][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto multiply = [&](const uint4 (&wv)[G], const uint4 (&hv)[NT]) {
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          acc[g][t] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, make_uint2(wv[g].x, wv[g].y)),
-                                                             __builtin_bit_cast(s16x4, make_uint2(hv[t].x, hv[t].y)), acc[g][t], 0, 0, 0);
-          acc[g][t] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, make_uint2(wv[g].z, wv[g].w)),
-                                                             __builtin_bit_cast(s16x4, make_uint2(hv[t].z, hv[t].w)), acc[g][t], 0, 0, 0);
-        }
-    };
-    int at = blocks ? (int)((blockIdx.x * 4 + wave) % (unsigned)blocks) : 0;
-    for (int n = 0; n < blocks; ++n) {
-      const int d = at * kBlock + 8 * b;
-      at = at + 1 == blocks ? 0 : at + 1;
-      uint4 wv[G], hv[NT];
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const words v = __builtin_nontemporal_load(reinterpret_cast<const words*>(w[g] + d));
-        wv[g] = make_uint4(v[0], v[1], v[2], v[3]);
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) hv[t] = load8(h[t] + d);
-      multiply(wv, hv);
-    }
-    if (tail - 8 * b < a.D) {  // uniform
-      uint4 wv[G], hv[NT];
-#pragma unroll
-      for (int g = 0; g < G; ++g) wv[g] = load8_of(w[g], tail, a.D);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) hv[t] = load8_of(h[t], tail, a.D);
-      multiply(wv, hv);
-    }
-    // acc[g][t][e] of lane (b, i): column 4 g + e, row 4 t + i, piece b of k
+    for (int t = 0; t < NT; ++t) acc[g][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto multiply = [&](const uint4 (&wv)[G], const uint4 (&hv)[NT]) {
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int off = 4; off < kWave; off <<= 1)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[g][t][e] += __shfl_xor(acc[g][t][e], off, kWave);
-        if (b == g) *reinterpret_cast<f32x4*>(&x[4 * t + i][c0 + 4 * g]) = acc[g][t];
+        acc[g][t] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, make_uint2(wv[g].x, wv[g].y)),
+                                                           __builtin_bit_cast(s16x4, make_uint2(hv[t].x, hv[t].y)), acc[g][t], 0, 0, 0);
+        acc[g][t] = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, make_uint2(wv[g].z, wv[g].w)),
+                                                           __builtin_bit_cast(s16x4, make_uint2(hv[t].z, hv[t].w)), acc[g][t], 0, 0, 0);
       }
+  };
+  int at = mine > 0 ? (int)((blockIdx.x * 4 + wave) % (unsigned)mine) : 0;
+  for (int n = 0; n < mine; ++n) {
+    const int d = (first + at * kShare) * kBlock + 8 * b;
+    at = at + 1 == mine ? 0 : at + 1;
+    uint4 wv[G], hv[NT];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const words v = __builtin_nontemporal_load(reinterpret_cast<const words*>(w[g] + d));
+      wv[g] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) hv[t] = load8(h[t] + d);
+    // All requested before the first is waited for: 32,000 x 4,096 for one row 41.9 us, 50.0 in the compiler's order, which is the
+    // better one with two rows of products (8 rows 54.8 us: 71.3).
+    if constexpr (NT == 1) __builtin_amdgcn_sched_barrier(0);
+    multiply(wv, hv);
   }
+  if (tail - 8 * b < a.D && (kShare == 1 || wave == kWaves - 1)) {  // uniform (the last wave has the fewest blocks)
+    uint4 wv[G], hv[NT];
+#pragma unroll
+    for (int g = 0; g < G; ++g) wv[g] = load8_of(w[g], tail, a.D);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) hv[t] = load8_of(h[t], tail, a.D);
+    multiply(wv, hv);
+  }
+  // acc[g][t][e] of lane (b, i): column 4 g + e, row 4 t + i, piece b of k
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int off = 4; off < kWave; off <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[g][t][e] += __shfl_xor(acc[g][t][e], off, kWave);
+      if (b == g) *reinterpret_cast<f32x4*>(&x[kShare > 1 ? wave : 0][4 * t + i][c0 + 4 * g]) = acc[g][t];
+    }
   __syncthreads();
-  finish_columns<WHAT, CAP, kHeadPart>(a, &x[0][0], span.rows);
+  if constexpr (kShare > 1) {
+    static_assert(4 * NT * PART <= kHeadThreads, "a thread per sum");
+    const int t = threadIdx.x;
+    if (t < 4 * NT * PART) {
+      float* sum = &x[0][0][0] + t;
+#pragma unroll
+      for (int u = 1; u < kShare; ++u) *sum += sum[u * 4 * NT * PART];
+    }
+    __syncthreads();
+  }
+  finish_columns<WHAT, CAP, PART>(a, &x[0][0][0], span.rows);
 }
 
 // The same for up to 16 RT rows: a wave reads the weights of 16 FC columns straight into the fragments of 16 x 16 x 32 products (64
 // bytes of 16 rows per load, the next 64 with the one after it: 5 TB/s), 4 FC KB at a time; the hidden states go through LDS, 128
 // values of k of all rows at a time, so that a compute unit reads them once and not once per wave.
-template <int RT, int FC, HeadForward WHAT, bool CAP>
+template <int RT, int FC, bool ODD, HeadForward WHAT, bool CAP>
 __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardArgs a) {
   constexpr int kPart = 64 * FC;  // columns of the workgroup
   constexpr int kBlock = 128, kSteps = kBlock / kHeadStep;
@@ -335,7 +351,9 @@ __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardAr
   auto request = [&](int block) {
 #pragma unroll
     for (int t = 0; t < RT; ++t)
-      hv[t] = block < whole ? load8(h[t] + block * kBlock + 8 * hg) : load8_of(h[t], block * kBlock + 8 * hg, a.D);
+      hv[t] = block >= whole ? load8_of<ODD>(h[t], block * kBlock + 8 * hg, a.D)
+              : ODD          ? load8_odd(h[t] + block * kBlock + 8 * hg)
+                             : load8(h[t] + block * kBlock + 8 * hg);
   };
   request(whole ? at : 0);
   for (int n = 0; n < blocks; ++n) {
@@ -347,12 +365,15 @@ __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardAr
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int f = 0; f < FC; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8(w[f] + d + s * kHeadStep));
+        for (int f = 0; f < FC; ++f) {
+          const uint16_t* p = w[f] + d + s * kHeadStep;
+          wv[s][f] = __builtin_bit_cast(bf16x8, ODD ? load8_odd(p) : load8(p));
+        }
     } else {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int f = 0; f < FC; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8_of(w[f], d + s * kHeadStep, a.D));
+        for (int f = 0; f < FC; ++f) wv[s][f] = __builtin_bit_cast(bf16x8, load8_of<ODD>(w[f], d + s * kHeadStep, a.D));
     }
     // (two buffers: what is written here was last read before the barrier of the block before)
 #pragma unroll
@@ -379,17 +400,30 @@ __global__ __launch_bounds__(kHeadThreads, 3) void head_few_kernel(HeadForwardAr
   finish_columns<WHAT, CAP, kPart>(a, &lds.x[0][0], span.rows);
 }
 
+template <int RT, HeadForward WHAT, bool CAP>
+hipError_t launch_fragments(const HeadForwardArgs& a, unsigned grid, bool odd, hipStream_t stream) {
+  const dim3 g(grid), block(kHeadThreads);
+  if (odd) return launch_kernel(head_few_kernel<RT, 1, true, WHAT, CAP>, g, block, 0, stream, a);
+  return launch_kernel(a.part_columns == kHeadSmallPart ? head_few_kernel<RT, 1, false, WHAT, CAP> : head_few_kernel<RT, 2, false, WHAT, CAP>, g, block,
+                       0, stream, a);
+}
+
 template <HeadForward WHAT, bool CAP>
 hipError_t launch_few(const HeadForwardArgs& a, int64_t rows, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.V + kHeadPart - 1) / kHeadPart)), block(kHeadThreads);
-  if (rows <= 4) return launch_kernel(head_tokens_kernel<1, 8, WHAT, CAP>, grid, block, 0, stream, a);
-  if (rows <= 8) return launch_kernel(head_tokens_kernel<2, 8, WHAT, CAP>, grid, block, 0, stream, a);
-  if (rows <= 16) return launch_kernel(head_tokens_kernel<4, 4, WHAT, CAP>, grid, block, 0, stream, a);
-  const dim3 halves((unsigned)((a.V + kHeadSmallPart - 1) / kHeadSmallPart));
-  const dim3 g = a.small ? halves : grid;
-  if (rows <= 32) return launch_kernel(a.small ? head_few_kernel<2, 1, WHAT, CAP> : head_few_kernel<2, 2, WHAT, CAP>, g, block, 0, stream, a);
-  if (rows <= 48) return launch_kernel(a.small ? head_few_kernel<3, 1, WHAT, CAP> : head_few_kernel<3, 2, WHAT, CAP>, g, block, 0, stream, a);
-  return launch_kernel(a.small ? head_few_kernel<4, 1, WHAT, CAP> : head_few_kernel<4, 2, WHAT, CAP>, g, block, 0, stream, a);
+  const unsigned grid = (unsigned)a.parts;
+  if (a.tokens) {
+    const bool share = a.part_columns == kHeadTokensPart;
+    const dim3 g(grid), block(kHeadThreads);
+    if (rows <= 4)
+      return launch_kernel(share ? head_tokens_kernel<1, kHeadTokensPart, WHAT, CAP> : head_tokens_kernel<1, kHeadPart, WHAT, CAP>, g, block, 0, stream, a);
+    return launch_kernel(share ? head_tokens_kernel<2, kHeadTokensPart, WHAT, CAP> : head_tokens_kernel<2, kHeadPart, WHAT, CAP>, g, block, 0, stream, a);
+  }
+  // load8_odd() where rows of the weights begin on odd values and both matrices on four bytes (parts of 64 columns, see head_few_part())
+  const bool odd = a.w.stride % 2 != 0 && a.part_columns == kHeadSmallPart && ((uintptr_t)a.w.p | (uintptr_t)a.q.p) % 4 == 0;
+  if (rows <= 16) return launch_fragments<1, WHAT, CAP>(a, grid, odd, stream);
+  if (rows <= 32) return launch_fragments<2, WHAT, CAP>(a, grid, odd, stream);
+  if (rows <= 48) return launch_fragments<3, WHAT, CAP>(a, grid, odd, stream);
+  return launch_fragments<4, WHAT, CAP>(a, grid, odd, stream);
 }
 
 template <int MF, int NF, HeadForward WHAT, bool CAP>
@@ -423,7 +457,7 @@ hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t r
 }
 
 hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream) {
-  if (a.small) return launch_tiles<4, 4>(a, what, rows, stream);
+  if (a.part_columns == kHeadSmallPart) return launch_tiles<4, 4>(a, what, rows, stream);
   if (rows <= 128) return launch_tiles<4, 8>(a, what, rows, stream);
   return launch_tiles<8, 8>(a, what, rows, stream);
 }

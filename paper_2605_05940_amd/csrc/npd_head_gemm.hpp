@@ -112,14 +112,40 @@ __device__ __forceinline__ void stream8(uint16_t* p, const uint4& v) {
   __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, reinterpret_cast<words*>(p));
 }
 __device__ __forceinline__ void store4(uint16_t* p, const uint2& v) { __builtin_memcpy(p, &v, 8); }
-// values [d, d + 8) of a row of `cols`, 0 behind its end
+// The same of a row that may begin on an odd value, in a matrix that begins on four bytes: the memory pipeline takes 16 bytes from a
+// multiple of four at twice the rate of those that are not (49,152 rows of 4,094 values 105 us, of 4,095 214; MI355X), so the four words
+// begin a value earlier there, in the row before, and the last value comes by itself.
+__device__ __forceinline__ uint4 load8_odd(const uint16_t* p) {
+  typedef uint32_t words __attribute__((ext_vector_type(4), aligned(4)));
+  const uint32_t odd = (uint32_t)(uintptr_t)p >> 1 & 1;
+  const words v = *reinterpret_cast<const words*>(p - odd);
+  const uint32_t last = p[7], shift = 16 * odd;
+  return make_uint4(__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift),
+                    __builtin_amdgcn_alignbit(v[3], v[2], shift), __builtin_amdgcn_alignbit(last, v[3], shift));
+}
+// Values [d, d + 8) of a row of `cols`, 0 behind its end: where that is among them, the last eight of the row, shifted (one load; one
+// for each value left of a row of 4,095 took as long as the rest of it where there are few rows).
+template <bool ODD = false>
 __device__ __forceinline__ uint4 load8_of(const uint16_t* row, int d, int cols) {
-  if (d + 8 <= cols) return load8(row + d);
-  uint32_t w[4] = {};
+  const int over = d + 8 - cols;
+  if (cols < 8) {  // uniform
+    uint32_t w[4] = {};
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
-    if (d + t < cols) w[t >> 1] |= (uint32_t)row[d + t] << (16 * (t & 1));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int t = 0; t < 8; ++t)
+      if (d + t < cols) w[t >> 1] |= (uint32_t)row[d + t] << (16 * (t & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  const uint16_t* p = row + (over > 0 ? cols - 8 : d);
+  uint4 v = ODD ? load8_odd(p) : load8(p);
+  if (over > 0) {
+    if (over & 4) v = make_uint4(v.z, v.w, 0, 0);
+    if (over & 2) v = make_uint4(v.y, v.z, v.w, 0);
+    if (over & 1)
+      v = make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16), __builtin_amdgcn_alignbit(v.w, v.z, 16),
+                     v.w >> 16);
+    if (over >= 8) v = make_uint4(0, 0, 0, 0);
+  }
+  return v;
 }
 
 // 16-byte groups of a KC tile's rows (64 bytes: four groups) are stored at group ^ kc_swizzle(row): the lanes of a fragment

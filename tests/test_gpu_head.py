@@ -441,3 +441,44 @@ def test_the_operators_together():
     full = loss64(dict(student, idx=idx, val=val), grad_scale=0.9, ce=0.1)
     for n, v in (("kd", b[0]), ("nll", b[1]), ("grad_hidden", direct[0]), ("grad_weight", direct[1])):
         near(v, full[n], n)
+
+
+def placed(t, stride, offset):
+    """`t` in rows `stride` apart, `offset` values behind an address of 16 bytes, with NaN around every row."""
+    full = torch.full((offset + t.shape[0] * stride + 16,), NAN, dtype=t.dtype, device=t.device)
+    at = full[offset:offset + t.shape[0] * stride].view(t.shape[0], stride)[:, :t.shape[1]]
+    at.copy_(t)
+    return at
+
+
+@pytest.mark.parametrize("T", [1, 5, 8, 16, 40, 64])
+@pytest.mark.parametrize("D", [3, 8, 9, 127, 129, 261])
+@pytest.mark.parametrize("extra,offset", [(0, 0), (1, 0), (2, 1), (1, 1), (4, 2)])
+def test_few_rows_wherever_they_begin(T, D, extra, offset):
+    """Rows of the weights and of the hidden states on any multiple of two bytes; what is around a row is not seen."""
+    s = inputs(T, 300, D, 3, True, mask=0.9)
+    s["weight"] = placed(s["weight"], D + extra, offset)
+    s["hidden"] = placed(s["hidden"], D + (extra + 1) % 3, offset // 2 * 2)
+    full, out = padded(T, 300, 301)
+    npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], softcap=4.0, logits_out=out)
+    torch.cuda.synchronize()
+    untouched(full, out)
+    x, _, dx = head64(s, 4.0)
+    near(out, (x, dx + 2.0 ** -8 * (x.abs() + dx)), "logits")
+    check_loss(s, cap=4.0, grads=())
+
+
+@pytest.mark.parametrize("T", [1, 4, 5, 8])
+@pytest.mark.parametrize("V", [1, 31, 33, 64, 97, 1000])
+@pytest.mark.parametrize("D", [1024, 1160, 1400])
+def test_few_rows_of_a_small_vocabulary(T, V, D):
+    """Workgroups whose waves share their columns: scalars, gradients, logits; parts that lie behind the vocabulary."""
+    s = inputs(T, V, D, 1, True, mask=0.9)
+    check_loss(s, grad_scale=0.9, ce=0.1)
+    check_loss(s, tau=2.0, grads=())
+    full, out = padded(T, V, V + 1)
+    npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], logits_out=out)
+    torch.cuda.synchronize()
+    untouched(full, out)
+    x, _, dx = head64(s, 0.0)
+    near(out, (x, dx + 2.0 ** -8 * (x.abs() + dx)), "logits")
