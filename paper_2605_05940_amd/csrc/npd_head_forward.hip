@@ -272,9 +272,9 @@ __global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_ker
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) hv[t] = load8(h[t] + d);
-    // All requested before the first is waited for: 32,000 x 4,096 for one row 41.9 us, 50.0 in the compiler's order, which is the
-    // better one with two rows of products (8 rows 54.8 us: 71.3).
-    if constexpr (NT == 1) __builtin_amdgcn_sched_barrier(0);
+    // All requested before the first is waited for, where that is faster than the compiler's order (MI355X, us, one row: logits of
+    // 32,000 x 4,096 41.9 for 50.0; sums of 16,000 x 2,048 27.4 for 34.5, but of 151,936 x 2,048 112 for 106; 8 rows of 32,000 x 4,096 71 for 55).
+    if constexpr (NT == 1 && (WHAT == kHeadLogits || kShare > 1)) __builtin_amdgcn_sched_barrier(0);
     multiply(wv, hv);
   }
   if (tail - 8 * b < a.D && (kShare == 1 || wave == kWaves - 1)) {  // uniform (the last wave has the fewest blocks)
