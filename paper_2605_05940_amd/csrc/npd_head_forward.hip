@@ -217,7 +217,7 @@ __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const f
 // bytes of each of four rows of the weights.  That is what decides: reading 151,936 x 2,048 alone (MI355X) takes 126 us in pieces of 64 bytes
 // of 16 rows, 105 in pieces of 256 of four, 91 if the caches are told that nothing is read twice, as here; waves begin at
 // different places of their rows and wrap around, since rows of a power of two of bytes would else be read out of few memory
-// channels (126 us: 145).  A workgroup has 128 columns, a wave 4 G of them at a time.
+// channels (126 us: 145).
 //
 // PART 128: a wave has 32 columns of its own.  32: the four waves have the same ones and every fourth block of k, added up at the end.
 template <int NT, int PART, HeadForward WHAT, bool CAP>
