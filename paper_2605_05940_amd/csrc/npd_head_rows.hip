@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kRowThreads) void head_prepare_kernel(HeadRowsArgs 
   if (r.grad_hidden) zero_row(r.grad_hidden + p * r.grad_stride, r.D);
 }
 
-// Joins the sums of a row over the vocabulary (part, one pair per 128 or 64 columns), writes its scalars, and turns what is kept of it,
+// Joins the sums of a row over the vocabulary (part, one pair per 128, 64 or 32 columns), writes its scalars, and turns what is kept of it,
 // e = 2^(x c - R), into the gradient up to the row's factor: with w = grad_scale / tau + ce_grad_scale and Z the row's sum
 //   G(v) = w / Z (e(v) - Z / w (grad_scale / tau p_T(v) + ce_grad_scale [v = label])),
 // so that only the entries at the label and the teacher's ids change (they are rounded to bf16 once, from fp32 values).  Those are
