@@ -1,0 +1,39 @@
+"""The head operators at the ends of what a call may ask for: soft caps of any size, far temperatures, labels that are not used."""
+import pytest
+import torch
+
+import head_util
+import paper_2605_05940_amd as npd
+from head_util import dev, head64, inputs, near
+from test_gpu_head import check_loss
+
+pytestmark = pytest.mark.gpu
+
+
+def head64_relative(s, cap=0.0):
+    """`head64` with a soft cap that is off by 2^-20 of itself: below |tanh| = 1/3 a product of five roundings and a polynomial fitted
+    to 3.3e-8 (less than 2^-21 together), above it 1 - 2 / (1 + e) with errors of 2^-22 in all (e's and the reciprocal's 2^-23
+    relative, at derivatives of at most 4/9 and 4/3, and two roundings); times cap 2^-24 more."""
+    z, _, dx = head64(s)
+    if not cap:
+        return z, torch.ones_like(z), dx
+    y = cap * torch.tanh(z / cap)
+    return y, 1 - (y / cap) ** 2, dx + 2.0 ** -20 * y.abs()
+
+
+@pytest.mark.parametrize("T", [1, 7, 40, 70, 150])
+@pytest.mark.parametrize("cap", [5.0, 30.0, 1e3, 1e4, 1e6, 1e12])
+def test_soft_caps_of_any_size(T, cap, monkeypatch):
+    """A logit is as accurate below a high cap as below a low one: logits, scalars and gradients."""
+    s = inputs(T, 1003, 64, 3, True, mask=0.9)
+    s["hidden"][0] *= 2.0 ** -8          # logits far below the cap
+    s["bias"][::2] *= 2.0 ** -8
+    s["mask"][T // 2] = 1
+    out = torch.empty((T, 1003), dtype=torch.bfloat16, device=dev())
+    npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], softcap=cap, logits_out=out)
+    torch.cuda.synchronize()
+    x, _, dx = head64_relative(s, cap)
+    near(out, (x, dx + 2.0 ** -8 * (x.abs() + dx)), "logits")
+    monkeypatch.setattr(head_util, "head64", head64_relative)
+    check_loss(s, cap=cap, grads=())
+    check_loss(s, cap=cap, grad_scale=0.9, ce=0.1)
