@@ -108,12 +108,12 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
         for (int j = 0; j < NF; ++j)
 #pragma unroll
           for (int t = 0; t < 4; ++t) v[4 * j + t] = CAP ? soft.tanh_of(x.acc[i][j][t]) : x.acc[i][j][t];
-        if (edge) {  // (columns that are not there: e is 0, and with a finite slope e times it)
+        if (edge) {  // columns that are not there: e is 0 however small c is, and so is the slope
 #pragma unroll
           for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-              if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = CAP ? -1.0e18f : -__builtin_inff();
+              if (nw + 32 * (j >> 1) + 4 * (j & 1) + t >= a.V) v[4 * j + t] = -__builtin_inff();
         }
 #pragma unroll
         for (int p = 0; p < 4 * NF; p += 2) top = max3(top, v[p], v[p + 1]);
@@ -133,8 +133,8 @@ __global__ __launch_bounds__(kHeadThreads, 1) void head_forward_kernel(HeadForwa
             z += lo;
             z += hi;
             if constexpr (CAP && WHAT == kHeadSumsKept) {
-              lo *= __builtin_fmaf(-v[p], v[p], 1.0f);
-              hi *= __builtin_fmaf(-v[p + 1], v[p + 1], 1.0f);
+              lo *= __builtin_amdgcn_fmed3f(__builtin_fmaf(-v[p], v[p], 1.0f), 0.0f, 1.0f);
+              hi *= __builtin_amdgcn_fmed3f(__builtin_fmaf(-v[p + 1], v[p + 1], 1.0f), 0.0f, 1.0f);
             }
             if constexpr (WHAT == kHeadSumsKept) w[t] = pack_bf16(lo, hi);
           }

@@ -37,3 +37,14 @@ def test_soft_caps_of_any_size(T, cap, monkeypatch):
     monkeypatch.setattr(head_util, "head64", head64_relative)
     check_loss(s, cap=cap, grads=())
     check_loss(s, cap=cap, grad_scale=0.9, ce=0.1)
+
+
+@pytest.mark.parametrize("tau", [1e10, 1e20, 1e30])
+@pytest.mark.parametrize("cap", [0.0, 30.0, 1e-3])
+@pytest.mark.parametrize("T,V", [(6, 300), (40, 1003), (100, 1003), (100, 1000), (300, 20001)])
+def test_temperatures_that_leave_nothing_of_the_logits(T, V, cap, tau):
+    """Every entry counts alike then, and entries behind the vocabulary do not count."""
+    s = inputs(T, V, 40, 7, True, mask=0.9)
+    s["mask"][T // 2] = 1
+    check_loss(s, cap=cap, tau=tau, grads=())
+    check_loss(s, cap=cap, tau=tau, grad_scale=tau)
