@@ -426,7 +426,7 @@ typedef struct {
   float tau;                  /* loss: KD temperature, finite, > 0                                   */
   float grad_scale;           /* loss: finite; multiplies the KD gradient (ignored without a teacher) */
   float ce_grad_scale;        /* loss: finite; weight of the hard-label CE gradient                  */
-  float softcap;              /* finite, >= 0; 0: none                                               */
+  float softcap;              /* 0: none; finite, >= 2^-126                                          */
 } npd_head_desc;
 
 /*
@@ -469,7 +469,7 @@ size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op);
  *
  * NPD_ERR_UNSUPPORTED: tau != 1 together with nll_tok, lse_tok or ce_grad_scale != 0 (quantities at tau = 1: ask for them in
  * a call of their own), and gradients with grad_scale and ce_grad_scale of opposite sign.  NPD_ERR_VALUE: ce_grad_scale != 0
- * without a gradient, gradients with neither a teacher nor ce_grad_scale.
+ * without a gradient, gradients with neither a teacher nor ce_grad_scale, 1 / tau, softcap / tau or grad_scale / tau beyond fp32.
  *
  * Products are of bf16 operands with fp32 sums (for the gradients each row of G is rounded to bf16 once, up to a factor of the
  * row, and hidden times that factor once); softmax statistics are fp32.  Results are reproducible bit by bit for the same sizes

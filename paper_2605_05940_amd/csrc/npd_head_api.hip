@@ -1,5 +1,6 @@
 // C ABI of the head operators (include/npd.h): argument checks, the workspace's layout, and the launches of a call.
 // Every check runs before the first HIP call.
+#include <float.h>
 #include <math.h>
 
 #include "../../include/npd.h"
@@ -14,6 +15,9 @@ constexpr uint32_t kGradFlags = NPD_HEAD_GRAD_HIDDEN | NPD_HEAD_GRAD_WEIGHT | NP
 constexpr int32_t kWhole = 0x7fffff00;  // a chunk that takes every row
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+float exponent_scale(const npd_head_desc& d) { return (float)(1.4426950408889634 / (double)d.tau); }
+float kd_weight(const npd_head_desc& d) { return (float)((double)d.grad_scale / (double)d.tau); }
 
 npd_status check_head(const npd_head_desc* d, int op) {
   if (!d) return NPD_ERR_NULL;
@@ -39,12 +43,16 @@ npd_status check_head(const npd_head_desc* d, int op) {
     if (s[0] && s[1] < s[2]) return NPD_ERR_SHAPE;
   for (const auto& s : strides)
     if (s[0] && s[1] > NPD_HEAD_MAX_VOCAB) return NPD_ERR_UNSUPPORTED;  // offsets within a tile are 32-bit
-  if (!(d->softcap >= 0.0f) || !isfinite(d->softcap)) return NPD_ERR_VALUE;
+  if (!(d->softcap >= 0.0f) || !isfinite(d->softcap) || (d->softcap > 0.0f && d->softcap < FLT_MIN)) return NPD_ERR_VALUE;
   if (op != NPD_HEAD_LOSS) return NPD_OK;
   if (d->topk < 0 || d->topk > d->vocab) return NPD_ERR_SHAPE;
   if (d->topk > kTopkMax) return NPD_ERR_UNSUPPORTED;
   if (!(d->tau > 0.0f) || !isfinite(d->tau)) return NPD_ERR_VALUE;
   if (!isfinite(d->grad_scale) || !isfinite(d->ce_grad_scale)) return NPD_ERR_VALUE;
+  // what the kernels multiply by has to be a number: the base-2 scale of the logits, with the soft cap in it, and a row's weight
+  const float c = exponent_scale(*d);
+  if (!isfinite(c) || (d->softcap != 0.0f && (!isfinite(c * d->softcap) || c * d->softcap == 0.0f))) return NPD_ERR_VALUE;
+  if (grads && d->topk > 0 && !isfinite(kd_weight(*d) + d->ce_grad_scale)) return NPD_ERR_VALUE;
   if (!grads && d->ce_grad_scale != 0.0f) return NPD_ERR_VALUE;
   if (grads && d->topk == 0 && d->ce_grad_scale == 0.0f) return NPD_ERR_VALUE;  // nothing to differentiate
   if (d->tau != 1.0f && d->ce_grad_scale != 0.0f) return NPD_ERR_UNSUPPORTED;
@@ -304,7 +312,7 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   l.V = V;
   l.k = d.topk;
   l.cap = d.softcap;
-  l.c = (float)(1.4426950408889634 / (double)d.tau);
+  l.c = exponent_scale(d);
   l.labels = labels;
   l.tidx = teacher_idx;
   l.tval = teacher_val;
@@ -318,7 +326,7 @@ npd_status npd_head_loss_fwd_bwd(const npd_head_desc* desc, const void* hidden, 
   l.nll = nll_tok;
   l.lse = lse_tok;
   l.status = dev_status;
-  l.kd_weight = (float)((double)d.grad_scale / (double)d.tau);
+  l.kd_weight = kd_weight(d);
   l.ce_weight = d.ce_grad_scale;
   l.e = grads ? reinterpret_cast<uint16_t*>(ws + p.e) : nullptr;
   l.e_stride = p.e_stride;
