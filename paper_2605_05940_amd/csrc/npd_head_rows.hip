@@ -272,6 +272,7 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
   const float* x = a.x + i * (1 + a.k);
   const int label = a.labels ? entry_id(a, p, 0) : -1;
   const bool no_label = a.labels && label < 0;
+  const bool bad_label = no_label && (a.nll || a.ce_weight != 0.0f);  // (labels that nothing uses are not checked)
   // the teacher's distribution over its ids at this temperature
   float tmax = -__builtin_inff();
   for (int j = threadIdx.x; j < a.k; j += kRowThreads) tmax = fmaxf(tmax, a.tval[p * a.k + j]);
@@ -322,14 +323,14 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
   }
   const bool label_done = __syncthreads_or(at_label);
   kd = block_sum<kRowThreads>(kd, fred);
-  const bool bad = (no_label && (a.nll || a.ce_weight != 0.0f)) || no_id;
+  const bool bad = bad_label || no_id;
   if (threadIdx.x == 0) {
     const float nan = __builtin_nanf("");
     if (a.e && label >= 0 && !label_done && a.ce_weight != 0.0f) put(label, x[0], take * a.ce_weight);
     if (a.lse) a.lse[p] = (R + lz) * kLn2;
     if (a.nll) a.nll[p] = no_label ? nan : (__builtin_fmaf(-x[0], a.c, R) + lz) * kLn2;
     if (a.kd) a.kd[p] = no_id ? nan : kd * kLn2;
-    if (a.status && bad) atomicOr(a.status, (no_label ? NPD_DEV_BAD_LABEL : 0) | (no_id ? NPD_DEV_BAD_TOPK_INDEX : 0));
+    if (a.status && bad) atomicOr(a.status, (bad_label ? NPD_DEV_BAD_LABEL : 0) | (no_id ? NPD_DEV_BAD_TOPK_INDEX : 0));
   }
   if (!a.e) return;
   off = block_sum<kRowThreads>(off, fred);

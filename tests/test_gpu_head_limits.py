@@ -5,6 +5,7 @@ import torch
 import head_util
 import paper_2605_05940_amd as npd
 from head_util import dev, head64, inputs, near
+from paper_2605_05940_amd import binding
 from test_gpu_head import check_loss
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +49,22 @@ def test_temperatures_that_leave_nothing_of_the_logits(T, V, cap, tau):
     s["mask"][T // 2] = 1
     check_loss(s, cap=cap, tau=tau, grads=())
     check_loss(s, cap=cap, tau=tau, grad_scale=tau)
+
+
+@pytest.mark.parametrize("T", [20, 90])
+@pytest.mark.parametrize("grads", [False, True])
+def test_labels_that_nothing_uses_are_not_reported(T, grads):
+    """Padding labels in a call for the KL alone: the status tells of the ids."""
+    s = inputs(T, 400, 64, 4)
+    s["mask"].fill_(1)
+    s["idx"][11, 2] = 400
+    kd, lse = (torch.empty(T, device=dev()) for _ in range(2))
+    for labels in (-100, 400):
+        s["labels"].fill_(labels)
+        status = torch.zeros(1, dtype=torch.int32, device=dev())
+        npd.npd_head_loss_fwd_bwd(s["hidden"], s["weight"], s["mask"], labels=s["labels"], teacher_idx=s["idx"],
+                                  teacher_val=s["val"], kd_tok=kd, lse_tok=lse, dev_status=status,
+                                  grad_hidden=torch.empty_like(s["hidden"]) if grads else None)
+        torch.cuda.synchronize()
+        assert status.item() == binding.NPD_DEV_BAD_TOPK_INDEX
+        assert kd.isnan().nonzero().tolist() == [[11]] and bool(lse.isfinite().all())
