@@ -215,11 +215,17 @@ struct HeadSource {
       if (left <= kpos[j & 1]) o = kHeadRecords;
     }
     // Written out: a wait that the compiler puts in front of every read of LDS behind such a load (it does in front of the
-    // transposing ones) would undo what the stages are for.  The instruction writes no register; m0 is set for every use of it.
+    // transposing ones) would undo what the stages are for.  The instruction writes no register.  Nor does the compiler keep distances to
+    // what is written out: a scalar register that a vector instruction wrote (a spilled one comes back through v_readlane) may be read
+    // by the load five wait states later, of which s_mov and s_nop are two.  s_nop 3 in here would do, for 3 % of the large calls (loss of
+    // 32,768 x 151,936 x 2,048 36.7 ms for 35.5), so the built code is checked instead, with the products' distances (tests/test_head_code.py).
     const uint64_t at = reinterpret_cast<uint64_t>(base + (left > 0 ? s * step : 0));
     const i32x4 r = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)records, 0x00020000};
     const uint32_t lds = (uint32_t)(uintptr_t)(NPD_LDS char*)(to + (wave * kLoads + j) * 1024);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(o), "s"(r) : "memory");
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is never allocated; named so that no value of it is kept across this)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(o), "s"(r) : "memory", "m0");
+#pragma clang diagnostic pop
   }
 };
 
@@ -289,7 +295,8 @@ struct HeadProduct {
   static __device__ __forceinline__ char* p_stage(char* lds, int s) { return lds + kHeadStages * Q::kBytes + s * P::kBytes; }
 
   // acc += p q, written out so that the sums stay where they are (256 registers of sums leave the compiler none to move them
-  // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one)
+  // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one).  An operand that a vector instruction
+  // wrote may be read two wait states later, the sums by anything else eleven (see HeadSource::load; s_nop 1 in here: 7 %).
   static __device__ __forceinline__ void multiply(f32x4& c, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   }
