@@ -254,16 +254,16 @@ __global__ __launch_bounds__(kRowThreads) void head_finish_kernel(HeadLossArgs a
   block_merge<kRowThreads, 1>(sum, fred);
   const float R = sum[0].r, Z = sum[0].z, lz = __log2f(Z);
   const bool rescale = a.e && __syncthreads_or(apart || first != R);
-  if (rescale) {  // exact unless it underflows: references are whole numbers
+  if (rescale) {  // exact: references are whole numbers (a factor 2^(r - R) by itself would underflow where its products, of up to 2^40, do not)
     for (int t = wave; t < a.parts; t += kRowThreads / kWave) {
       const float r = part[t].x;
       if (r == R) continue;
-      const float f = exp2_fast(r - R);
+      const int by = (int)fmaxf(r - R, -400.0f);  // (-400: nothing is left)
       uint16_t* e = a.e + i * a.e_stride + t * a.part_columns;
       const int n = 2 * lane;
       if (n < a.part_columns && t * a.part_columns + n < a.V) {
         uint32_t* w = reinterpret_cast<uint32_t*>(e + n);
-        *w = f == 0.0f ? 0u : pack_bf16(bf16_lo(*w) * f, bf16_hi(*w) * f);
+        *w = pack_bf16(__builtin_ldexpf(bf16_lo(*w), by), __builtin_ldexpf(bf16_hi(*w), by));
       }
     }
     __syncthreads();

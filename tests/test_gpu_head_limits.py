@@ -68,3 +68,22 @@ def test_labels_that_nothing_uses_are_not_reported(T, grads):
         torch.cuda.synchronize()
         assert status.item() == binding.NPD_DEV_BAD_TOPK_INDEX
         assert kd.isnan().nonzero().tolist() == [[11]] and bool(lse.isfinite().all())
+
+
+@pytest.mark.parametrize("T", [1, 6, 40, 70, 200])
+@pytest.mark.parametrize("cap", [0.0, 500.0])
+def test_columns_between_a_far_label_and_the_top(T, cap):
+    """A row's label lies 2^137 below its most likely entry, other entries 2^39 above the label: their share of 2^-98 is kept."""
+    V = 520
+    logits = torch.full((V,), -20.0, device=dev())
+    logits[3:40] = 27.0
+    logits[300] = 95.0
+    weight = torch.zeros((V, 8), dtype=torch.bfloat16, device=dev())
+    weight[:, 0] = logits.to(torch.bfloat16)
+    weight[1] = 0.0   # the label's
+    hidden = torch.zeros((T, 8), dtype=torch.bfloat16, device=dev())
+    hidden[:, 0] = 1.0
+    s = dict(hidden=hidden, weight=weight, labels=torch.ones(T, dtype=torch.int32, device=dev()),
+             mask=torch.ones(T, dtype=torch.uint8, device=dev()), bias=None, idx=None, val=None)
+    got = check_loss(s, cap=cap, ce=1.0)
+    assert bool((got["grad_weight"][3:40, 0] > 0).all())
