@@ -477,8 +477,14 @@ def _head_workspace(L, desc, op: int, workspace: Optional[torch.Tensor]):
 
 
 def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor of a call: the kernels run on the current device, which need not reach another one's memory."""
+    current = None
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+        if t is None or not t.is_cuda:
+            continue
+        if current is None:
+            current = torch.cuda.current_device()
+        if t.device.index != current:
             raise ValueError(f"a tensor is on {t.device}, kernels run on the current device: make it current first")
 
 
@@ -506,7 +512,8 @@ def npd_head_loss_fwd_bwd(hidden: torch.Tensor, weight: torch.Tensor, loss_mask:
                 teacher_idx.is_contiguous() and teacher_val.is_contiguous() and teacher_val.shape == teacher_idx.shape
                 and teacher_idx.shape[0] == T):
             raise ValueError("teacher_idx / teacher_val must be contiguous [T, k]")
-    _on_current_device(hidden, weight, grad_hidden, grad_weight)
+    _on_current_device(hidden, weight, loss_mask, bias, labels, teacher_idx, teacher_val, grad_hidden, grad_weight, grad_bias, kd_tok,
+                       nll_tok, lse_tok, dev_status, workspace)
     desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight), 0, k,
                                  _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, hidden, weight), tau, grad_scale,
                                  ce_grad_scale, softcap))
@@ -528,7 +535,7 @@ def npd_head_logits(hidden: torch.Tensor, weight: torch.Tensor, *, logits_out: t
     """Enqueue ``logits_out = hidden @ weight.T + bias``, soft-capped, rounded to bf16 once (see ``npd_head_logits`` in npd.h)."""
     T, D = hidden.shape
     V = weight.shape[0]
-    _on_current_device(hidden, weight, logits_out)
+    _on_current_device(hidden, weight, logits_out, bias, workspace)
     desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), 0, 0, _pitch(logits_out), 0,
                                  _head_flags(None, None, None, False, hidden, weight), 1.0, 0.0, 0.0, softcap))
     args = (desc, _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
@@ -547,11 +554,11 @@ def npd_head_logits_bwd(grad_logits: torch.Tensor, hidden: torch.Tensor, weight:
     npd.h); ``logits`` are its outputs, needed with a soft cap (and ignored without)."""
     T, D = hidden.shape
     V = weight.shape[0]
-    _on_current_device(grad_logits, hidden, weight, grad_hidden, grad_weight)
     if softcap == 0.0:
         logits = None
     elif logits is not None and logits.shape == grad_logits.shape and _pitch(logits) != _pitch(grad_logits):
         raise ValueError("logits must have the row stride of grad_logits")
+    _on_current_device(grad_logits, hidden, weight, logits, grad_hidden, grad_weight, grad_bias, workspace)
     desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight),
                                  _pitch(grad_logits), 0,
                                  _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, grad_logits, hidden, weight), 1.0,

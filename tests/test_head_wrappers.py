@@ -1,0 +1,77 @@
+"""The Python wrappers of the head operators without a GPU: what they refuse before the library is called."""
+import pytest
+import torch
+
+import paper_2605_05940_amd as npd
+from paper_2605_05940_amd import binding
+
+T, V, D, K = 4, 50, 16, 3
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it is on a device."""
+    index = 0
+    is_cuda = property(lambda self: True)
+    device = property(lambda self: torch.device("cuda", self.index))
+
+
+def tensor(*shape, dtype=torch.bfloat16, index=0):
+    t = torch.zeros(shape, dtype=dtype).as_subclass(OnDevice)
+    t.index = index
+    return t
+
+
+@pytest.fixture(autouse=True)
+def no_device(monkeypatch):
+    """The library's calls are counted, not made."""
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or 0
+
+    monkeypatch.setattr(binding, "load", Library)
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    return calls
+
+
+def arguments():
+    f, i = torch.float32, torch.int32
+    scalars = {n: tensor(T, dtype=f) for n in ("kd_tok", "nll_tok", "lse_tok")}
+    bias, ws = dict(bias=tensor(V)), dict(workspace=tensor(1 << 20, dtype=torch.uint8))
+    grads = dict(grad_hidden=tensor(T, D), grad_weight=tensor(V, D), grad_bias=tensor(V))
+    both = dict(hidden=tensor(T, D), weight=tensor(V, D))
+    return {
+        npd.npd_head_loss_fwd_bwd: dict(**both, loss_mask=tensor(T, dtype=torch.uint8), labels=tensor(T, dtype=i),
+                                        teacher_idx=tensor(T, K, dtype=i), teacher_val=tensor(T, K, dtype=f),
+                                        dev_status=tensor(1, dtype=i), **bias, **grads, **scalars, **ws),
+        npd.npd_head_logits: dict(**both, logits_out=tensor(T, V), **bias, **ws),
+        npd.npd_head_logits_bwd: dict(grad_logits=tensor(T, V), **both, logits=tensor(T, V), softcap=30.0, **grads, **ws),
+    }
+
+
+CALLS = [(f, n) for f, a in arguments().items() for n, t in a.items() if isinstance(t, torch.Tensor)]
+
+
+@pytest.mark.parametrize("call", arguments(), ids=lambda f: f.__name__)
+def test_the_calls_that_these_are_made_from(call, no_device):
+    call(**arguments()[call])
+    assert no_device == [call.__name__]
+
+
+@pytest.mark.parametrize("call,name", CALLS, ids=lambda x: x if isinstance(x, str) else x.__name__)
+def test_a_tensor_on_another_device(call, name, no_device):
+    a = arguments()[call]
+    a[name].index = 1
+    with pytest.raises(ValueError, match="cuda:1"):
+        call(**a)
+    assert not no_device
+
+
+def test_logits_that_a_call_has_no_use_for(no_device):
+    a = arguments()[npd.npd_head_logits_bwd]
+    a.update(softcap=0.0)
+    a["logits"].index = 1
+    npd.npd_head_logits_bwd(**a)
+    assert no_device == ["npd_head_logits_bwd"]
