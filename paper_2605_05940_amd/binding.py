@@ -465,6 +465,8 @@ def _head_workspace(L, desc, op: int, workspace: Optional[torch.Tensor]):
     """(pointer, bytes) of a call's workspace: the caller's, or a block from torch's stream-ordered allocator, which it goes
     back to when the call has been enqueued (smaller where there is no memory for what the call prefers)."""
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         return workspace, _ptr(workspace), workspace.numel() * workspace.element_size()
     want = L.npd_head_workspace_bytes_preferred(desc, op)
     if not want:

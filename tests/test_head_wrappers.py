@@ -75,3 +75,12 @@ def test_logits_that_a_call_has_no_use_for(no_device):
     a["logits"].index = 1
     npd.npd_head_logits_bwd(**a)
     assert no_device == ["npd_head_logits_bwd"]
+
+
+@pytest.mark.parametrize("call", arguments(), ids=lambda f: f.__name__)
+def test_a_workspace_in_pieces(call, no_device):
+    """What counts is the memory behind a workspace's address, not its number of elements."""
+    for ws in (tensor(256, dtype=torch.uint8).expand(1 << 12, 256), tensor(1 << 13, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            call(**dict(arguments()[call], workspace=ws))
+    assert not no_device
