@@ -455,6 +455,11 @@ def _pitch(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _head_desc(T: int, V: int, D: int, *rest):
+    """A descriptor by reference.  Its vocabulary and width are 32 bits wide: what does not fit stays too large to be taken."""
+    return ctypes.byref(HeadDesc(T, min(V, 0x7fffffff), min(D, 0x7fffffff), *rest))
+
+
 def _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, *inputs) -> int:
     return ((NPD_HEAD_GRAD_HIDDEN if grad_hidden is not None else 0) | (NPD_HEAD_GRAD_WEIGHT if grad_weight is not None else 0) |
             (NPD_HEAD_GRAD_BIAS if grad_bias is not None else 0) | (NPD_HEAD_ACCUMULATE if accumulate else 0) |
@@ -509,16 +514,15 @@ def npd_head_loss_fwd_bwd(hidden: torch.Tensor, weight: torch.Tensor, loss_mask:
     V = weight.shape[0]
     k = 0
     if teacher_idx is not None:
-        k = teacher_idx.shape[1] if teacher_idx.dim() == 2 else 0
+        k = min(teacher_idx.shape[1], 0x7fffffff) if teacher_idx.dim() == 2 else 0
         if teacher_val is None or k == 0 or not (
                 teacher_idx.is_contiguous() and teacher_val.is_contiguous() and teacher_val.shape == teacher_idx.shape
                 and teacher_idx.shape[0] == T):
             raise ValueError("teacher_idx / teacher_val must be contiguous [T, k]")
     _on_current_device(hidden, weight, loss_mask, bias, labels, teacher_idx, teacher_val, grad_hidden, grad_weight, grad_bias, kd_tok,
                        nll_tok, lse_tok, dev_status, workspace)
-    desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight), 0, k,
-                                 _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, hidden, weight), tau, grad_scale,
-                                 ce_grad_scale, softcap))
+    desc = _head_desc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight), 0, k,
+                      _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, hidden, weight), tau, grad_scale, ce_grad_scale, softcap)
     args = (desc, _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
             _array("bias", bias, V, torch.bfloat16), _array("labels", labels, T, torch.int32),
             _ptr(teacher_idx, torch.int32), _ptr(teacher_val, torch.float32),
@@ -538,8 +542,8 @@ def npd_head_logits(hidden: torch.Tensor, weight: torch.Tensor, *, logits_out: t
     T, D = hidden.shape
     V = weight.shape[0]
     _on_current_device(hidden, weight, logits_out, bias, workspace)
-    desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), 0, 0, _pitch(logits_out), 0,
-                                 _head_flags(None, None, None, False, hidden, weight), 1.0, 0.0, 0.0, softcap))
+    desc = _head_desc(T, V, D, _pitch(hidden), _pitch(weight), 0, 0, _pitch(logits_out), 0,
+                      _head_flags(None, None, None, False, hidden, weight), 1.0, 0.0, 0.0, softcap)
     args = (desc, _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
             _array("bias", bias, V, torch.bfloat16), _matrix("logits_out", logits_out, (T, V)))
     L = load()
@@ -561,10 +565,8 @@ def npd_head_logits_bwd(grad_logits: torch.Tensor, hidden: torch.Tensor, weight:
     elif logits is not None and logits.shape == grad_logits.shape and _pitch(logits) != _pitch(grad_logits):
         raise ValueError("logits must have the row stride of grad_logits")
     _on_current_device(grad_logits, hidden, weight, logits, grad_hidden, grad_weight, grad_bias, workspace)
-    desc = ctypes.byref(HeadDesc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight),
-                                 _pitch(grad_logits), 0,
-                                 _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, grad_logits, hidden, weight), 1.0,
-                                 0.0, 0.0, softcap))
+    desc = _head_desc(T, V, D, _pitch(hidden), _pitch(weight), _pitch(grad_hidden), _pitch(grad_weight), _pitch(grad_logits), 0,
+                      _head_flags(grad_hidden, grad_weight, grad_bias, accumulate, grad_logits, hidden, weight), 1.0, 0.0, 0.0, softcap)
     args = (desc, _matrix("grad_logits", grad_logits, (T, V)), _matrix("logits", logits, (T, V)),
             _matrix("hidden", hidden, (T, D)), _matrix("weight", weight, (V, D)),
             _matrix("grad_hidden", grad_hidden, (T, D)), _matrix("grad_weight", grad_weight, (V, D)),

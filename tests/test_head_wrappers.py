@@ -6,6 +6,7 @@ import paper_2605_05940_amd as npd
 from paper_2605_05940_amd import binding
 
 T, V, D, K = 4, 50, 16, 3
+LOAD = binding.load
 
 
 class OnDevice(torch.Tensor):
@@ -84,3 +85,39 @@ def test_a_workspace_in_pieces(call, no_device):
         with pytest.raises(ValueError, match="workspace"):
             call(**dict(arguments()[call], workspace=ws))
     assert not no_device
+
+
+@pytest.mark.parametrize("call", arguments(), ids=lambda f: f.__name__)
+@pytest.mark.parametrize("V,D", [((1 << 32) + 5, 1), (5, (1 << 32) + 3)])
+def test_sizes_beyond_the_descriptors_fields(call, V, D, monkeypatch):
+    """2^32 + 5 rows are not five."""
+    monkeypatch.setattr(binding, "load", LOAD)
+
+    def matrix(rows, cols):
+        return tensor(1, 1).expand(rows, cols) if max(rows, cols) > 1 << 31 else tensor(rows, cols)
+
+    monkeypatch.setattr(binding, "_matrix", lambda name, t, shape: None if t is None else 4096)
+    weight, hidden = matrix(V, D), matrix(T, D)
+    monkeypatch.setattr(binding, "_array", lambda name, t, n, dtype: None if t is None else 4096)
+    a = dict(hidden=hidden, weight=weight)
+    if call is npd.npd_head_loss_fwd_bwd:
+        a.update(loss_mask=tensor(T, dtype=torch.uint8), lse_tok=tensor(T, dtype=torch.float32))
+    elif call is npd.npd_head_logits:
+        a.update(logits_out=matrix(T, V))
+    else:
+        a.update(grad_logits=matrix(T, V), grad_bias=tensor(5))
+    with pytest.raises(binding.NpdError) as e:
+        call(**a)
+    assert e.value.status == 5   # not supported
+
+
+def test_a_record_beyond_the_descriptors_field(monkeypatch):
+    monkeypatch.setattr(binding, "load", LOAD)
+    a = arguments()[npd.npd_head_loss_fwd_bwd]
+    k = (1 << 32) + 2
+    for name, dtype in (("teacher_idx", torch.int32), ("teacher_val", torch.float32)):
+        a[name] = tensor(1, 1, dtype=dtype).expand(T, k)
+        monkeypatch.setattr(OnDevice, "is_contiguous", lambda self: True, raising=False)
+    with pytest.raises(binding.NpdError) as e:
+        npd.npd_head_loss_fwd_bwd(**a)
+    assert e.value.status == 2   # more ids than the vocabulary has
