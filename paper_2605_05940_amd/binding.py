@@ -483,6 +483,20 @@ def _head_workspace(L, desc, op: int, workspace: Optional[torch.Tensor]):
     return block, block.data_ptr(), want
 
 
+def npd_head_workspace_bytes(op: int, n_tokens: int, vocab: int, width: int, *, topk: int = 0, flags: int = 0, softcap: float = 0.0,
+                             hidden_stride: Optional[int] = None, weight_stride: Optional[int] = None,
+                             logits_stride: Optional[int] = None, preferred: bool = False) -> int:
+    """Bytes of workspace that a call of a head operator (``op``: ``NPD_HEAD_LOSS``, ``NPD_HEAD_LOGITS`` or
+    ``NPD_HEAD_LOGITS_BWD``) takes: the least, or as many as it can make use of.  ``flags``: ``NPD_HEAD_GRAD_*`` of the gradients
+    that it is given, ``NPD_HEAD_UNALIGNED`` where hidden, weight or grad_logits do not begin on 16 bytes (a view; torch's
+    allocations do).  Strides are in elements between rows and default to rows without gaps."""
+    grads = flags & (NPD_HEAD_GRAD_HIDDEN | NPD_HEAD_GRAD_WEIGHT | NPD_HEAD_GRAD_BIAS)
+    desc = _head_desc(n_tokens, vocab, width, hidden_stride or width, weight_stride or width, width, width, logits_stride or vocab, topk,
+                      flags, 1.0, 1.0, 1.0 if grads and not topk else 0.0, softcap)
+    L = load()
+    return int((L.npd_head_workspace_bytes_preferred if preferred else L.npd_head_workspace_bytes)(desc, op))
+
+
 def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
     """Every tensor of a call: the kernels run on the current device, which need not reach another one's memory."""
     current = None
@@ -507,8 +521,8 @@ def npd_head_loss_fwd_bwd(hidden: torch.Tensor, weight: torch.Tensor, loss_mask:
     """Enqueue the loss of ``npd_kd_loss_fwd_bwd`` on logits ``hidden @ weight.T + bias`` that are not stored, with the
     gradients that are given a tensor (see ``npd_head_loss_fwd_bwd`` in npd.h); with none of them the call is forward only.
     ``accumulate``: the gradients of weight and bias are added to what their tensors hold.  ``workspace``: a uint8 tensor of
-    at least ``npd_head_workspace_bytes`` bytes; without it the call takes a block from torch's allocator for as long as it
-    is being enqueued.
+    at least ``npd_head_workspace_bytes(NPD_HEAD_LOSS, ...)`` bytes; without it the call takes a block from torch's allocator
+    for as long as it is being enqueued.
     """
     T, D = hidden.shape
     V = weight.shape[0]

@@ -121,3 +121,38 @@ def test_a_record_beyond_the_descriptors_field(monkeypatch):
     with pytest.raises(binding.NpdError) as e:
         npd.npd_head_loss_fwd_bwd(**a)
     assert e.value.status == 2   # more ids than the vocabulary has
+
+
+def test_the_workspace_that_a_call_takes(monkeypatch):
+    """The function's answers are those for the descriptors that the calls make: one byte less is refused as too small."""
+    L = LOAD()
+
+    class Library:
+        """Host checks alone: a call that would be made on the device ends here."""
+        def __getattr__(self, name):
+            f = getattr(L, name)
+            return (lambda *a: f(*a[:-1], None) if a[-2] < need else 0) if name == call.__name__ else f
+
+    monkeypatch.setattr(binding, "load", Library)
+    ops = {npd.npd_head_loss_fwd_bwd: binding.NPD_HEAD_LOSS, npd.npd_head_logits: binding.NPD_HEAD_LOGITS,
+           npd.npd_head_logits_bwd: binding.NPD_HEAD_LOGITS_BWD}
+    n, w = 100, 13   # (rows that are copied)
+    for call, op in ops.items():
+        a = arguments()[call]
+        for name, t in a.items():
+            if isinstance(t, torch.Tensor) and name != "workspace":
+                shape = [n if s == T else w if s == D else s for s in t.shape]
+                a[name] = tensor(*shape, dtype=t.dtype)
+        flags = 0 if op == binding.NPD_HEAD_LOGITS else 7
+        if any(isinstance(t, torch.Tensor) and t.data_ptr() & 15 for t in a.values()):
+            flags |= binding.NPD_HEAD_UNALIGNED
+        how = dict(topk=K if op == binding.NPD_HEAD_LOSS else 0, flags=flags, softcap=a.get("softcap", 0.0))
+        need = npd.npd_head_workspace_bytes(op, n, V, w, **how)
+        assert 0 < need <= npd.npd_head_workspace_bytes(op, n, V, w, preferred=True, **how)
+        room = torch.zeros(need + 256, dtype=torch.uint8)
+        room = room[-room.data_ptr() % 256:][:need].as_subclass(OnDevice)
+        call(**dict(a, workspace=room))
+        with pytest.raises(binding.NpdError) as e:
+            call(**dict(a, workspace=room[:-1]))
+        assert e.value.status == 6
+    assert npd.npd_head_workspace_bytes(binding.NPD_HEAD_LOSS, 0, V, D) == 0
