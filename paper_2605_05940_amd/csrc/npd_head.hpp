@@ -66,6 +66,14 @@ inline int head_few_part(int64_t rows, int64_t columns, int64_t width, int64_t w
   if (head_tokens(rows, weight_stride)) return width >= 1024 && columns < 256 * (rows <= 4 ? 96 : 128) ? kHeadTokensPart : kHeadPart;
   return weight_stride % 2 != 0 || columns < 256 * 128 ? kHeadSmallPart : kHeadPart;
 }
+// Whether workgroups of up to four rows and 128 columns request a block's loads together, by their number: with few of them to a
+// compute unit there is little in flight else; with four and more the compiler's order, which multiplies in between, is as fast or
+// faster.  Measured (MI355X, us, together / compiler's order, weights out of the caches), one row, logits and scores: 16,000 x 2,048 (parts of
+// 32, always together) 16.5 / 23.6, 27.8 / 34.9; 32,000 x 4,096 42.6 / 50.3, 56.3 / 62.8; 98,000 x 1,024 32.7 / 35.2, 44.0 / 46.2; 106,000 x 2,048
+// 73.5 / 76.8, 89.6 / 88.8; 120,000 x 2,048 74.7 / 78.0, 91.6 / 90.1; 128,256 x 4,096 153.7 / 157.8, 174.3 / 171.8 and on another card 164.5 /
+// 158.0, 189 / 172; 151,936 x 2,048 93.7 / 94.5, 112.5 / 107.1; 262,144 x 1,152 91.0 / 91.2, 108.2 / 104.5.  Four rows alike; of eight the
+// compiler's order is faster throughout (32,000 x 4,096 71 / 55).
+inline bool head_together(int parts) { return parts <= 256 * 15 / 4; }
 hipError_t launch_head_few(const HeadForwardArgs& a, HeadForward what, int64_t rows, hipStream_t stream);
 
 // out[position of row m][n] = scale[m] sum_k g[m][k] w[k][n], k < K: the gradient of the hidden states.  k may be split into

@@ -227,7 +227,8 @@ __device__ __forceinline__ void finish_columns(const HeadForwardArgs& a, const f
 // channels (126 us: 145).
 //
 // PART 128: a wave has 32 columns of its own.  32: the four waves have the same ones and every fourth block of k, added up at the end.
-template <int NT, int PART, HeadForward WHAT, bool CAP>
+// TOGETHER: a block's loads are all requested before the first is waited for, and not in the compiler's order; see head_together().
+template <int NT, int PART, bool TOGETHER, HeadForward WHAT, bool CAP>
 __global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_kernel(HeadForwardArgs a) {
   constexpr int kWaves = kHeadThreads / kWave, G = 8, kShare = PART == 4 * G ? kWaves : 1;
   static_assert(PART == 4 * G * kWaves / kShare, "");
@@ -279,9 +280,7 @@ __global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void head_tokens_ker
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) hv[t] = load8(h[t] + d);
-    // All requested before the first is waited for, where that is faster than the compiler's order (MI355X, us, one row: logits of
-    // 32,000 x 4,096 41.9 for 50.0; sums of 16,000 x 2,048 27.4 for 34.5, but of 151,936 x 2,048 112 for 106; 8 rows of 32,000 x 4,096 71 for 55).
-    if constexpr (NT == 1 && (WHAT == kHeadLogits || kShare > 1)) __builtin_amdgcn_sched_barrier(0);
+    if constexpr (TOGETHER) __builtin_amdgcn_sched_barrier(0);
     multiply(wv, hv);
   }
   if (tail - 8 * b < a.D && (kShare == 1 || wave == kWaves - 1)) {  // uniform (the last wave has the fewest blocks)
@@ -421,9 +420,12 @@ hipError_t launch_few(const HeadForwardArgs& a, int64_t rows, hipStream_t stream
   if (a.tokens) {
     const bool share = a.part_columns == kHeadTokensPart;
     const dim3 g(grid), block(kHeadThreads);
-    if (rows <= 4)
-      return launch_kernel(share ? head_tokens_kernel<1, kHeadTokensPart, WHAT, CAP> : head_tokens_kernel<1, kHeadPart, WHAT, CAP>, g, block, 0, stream, a);
-    return launch_kernel(share ? head_tokens_kernel<2, kHeadTokensPart, WHAT, CAP> : head_tokens_kernel<2, kHeadPart, WHAT, CAP>, g, block, 0, stream, a);
+    if (rows > 4)
+      return launch_kernel(share ? head_tokens_kernel<2, kHeadTokensPart, false, WHAT, CAP> : head_tokens_kernel<2, kHeadPart, false, WHAT, CAP>, g,
+                           block, 0, stream, a);
+    if (share) return launch_kernel(head_tokens_kernel<1, kHeadTokensPart, true, WHAT, CAP>, g, block, 0, stream, a);
+    return launch_kernel(head_together(a.parts) ? head_tokens_kernel<1, kHeadPart, true, WHAT, CAP> : head_tokens_kernel<1, kHeadPart, false, WHAT, CAP>,
+                         g, block, 0, stream, a);
   }
   // load8_odd() where rows of the weights begin on odd values and both matrices on four bytes (parts of 64 columns, see head_few_part())
   const bool odd = a.w.stride % 2 != 0 && a.part_columns == kHeadSmallPart && ((uintptr_t)a.w.p | (uintptr_t)a.q.p) % 4 == 0;

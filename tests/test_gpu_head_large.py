@@ -94,3 +94,20 @@ def test_a_large_call_repeats_itself():
     a, b = (run_loss(s, grad_scale=0.9, ce=0.1) for _ in range(2))
     for name in a:
         assert torch.equal(a[name], b[name]), name
+
+
+@pytest.mark.parametrize("T", [1, 3, 4, 6, 30])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_few_rows_of_a_large_vocabulary(T, cap):
+    """More workgroups than a compute unit has room for three of: the other order of their loads."""
+    V, D = 130001, 264
+    s = inputs(T, V, D, 5, True)
+    s["mask"][T // 2] = 1
+    check_loss(s, cap=cap, grads=())
+    check_loss(s, cap=cap, grad_scale=0.9, ce=0.1)
+    full, out = padded(T, V, V + 2)
+    npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], softcap=cap, logits_out=out)
+    torch.cuda.synchronize()
+    untouched(full, out)
+    x, _, dx = head64(s, cap)
+    near(out, (x, dx + 2.0 ** -8 * (x.abs() + dx)), "logits")
