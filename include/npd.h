@@ -493,7 +493,7 @@ npd_status npd_head_logits(const npd_head_desc* desc, const void* hidden, const 
 /*
  * The backward pass of npd_head_logits from the gradient of its logits (npd_kd_loss_fwd_bwd's grad_out):
  *
- *   z[p, v] = grad_logits[p, v] * (softcap > 0 ? 1 - (logits[p, v] / softcap)^2 : 1)
+ *   z[p, v] = grad_logits[p, v] * (softcap > 0 ? 1 - (logits[p, v] / softcap)^2 : 1), with a soft cap rounded to bf16
  *   grad_hidden[p] = sum_v z[p, v] weight[v];  grad_weight[v] = sum_p z[p, v] hidden[p];  grad_bias[v] = sum_p z[p, v]
  *
  *   grad_logits bf16 [T, logits_stride], required; logits bf16 [T, logits_stride], required iff softcap > 0, else NULL;

@@ -8,7 +8,8 @@
 
 namespace npd {
 
-// Columns of one partial sum of a row: what a wave of the forward product holds of it, 128, or 64 with the small tiles.
+// Columns of one partial sum of a row: what a wave of the forward product holds of it, 128, or 64 with the small tiles; with few rows
+// what a workgroup holds of it, 128, 64 or 32.
 constexpr int kHeadPart = 128, kHeadSmallPart = 64, kHeadTokensPart = 32;
 
 // Tiles of 128 x 128 in place of 256 x 256: where there are so few that each has a compute unit to itself either way, a tile's own
@@ -29,7 +30,7 @@ enum HeadForward { kHeadLogits = 0, kHeadSums = 1, kHeadSumsKept = 2 };
 
 // x = (q w^T + bias), soft-capped, of a chunk of rows; then by HeadForward
 //   kHeadLogits     out = x, rounded to bf16
-//   kHeadSums       part[row][v / 128 or 64] = (r, z): sum over those columns of 2^(x c - r) is z
+//   kHeadSums       part[row][v / part_columns] = (r, z): sum over those columns of 2^(x c - r) is z
 //   kHeadSumsKept   and e[row][v] = 2^(x c - r) (with a soft cap times dx / d(q w^T)), rounded to bf16; 0 for v >= V
 struct HeadForwardArgs {
   HeadChunk chunk;
@@ -41,7 +42,7 @@ struct HeadForwardArgs {
   const float* r0;      // [rows] a logit of the row times c, whole, or -1e30: the reference of columns not far above it
   float2* part;
   int32_t parts;
-  int32_t part_columns; // head_few_part(); 64: head_small(), 128
+  int32_t part_columns; // up to kHeadFewRows rows head_few_part(): 128, 64 or 32; else 64 with head_small() and 128
   int32_t tokens;       // head_tokens()
   uint16_t* e;
   int64_t e_stride;
@@ -53,7 +54,7 @@ hipError_t launch_head_forward(const HeadForwardArgs& a, HeadForward what, int64
 // Rows that are so few that reading the weights is all the time: the weights go straight into registers, at any alignment.
 constexpr int64_t kHeadFewRows = 64;
 // Up to eight of them are head_tokens_kernel's, unless rows of the weights begin on odd values: the loads that cost least there are
-// head_few_kernel's (49,152 x 4,095, 1 / 8 rows, MI355X: 132 / 178 us here, 109 there).  Nine rows of 151,936 x 2,048 take 177 us here, 113
+// head_few_kernel's (49,152 x 4,095, 1 / 8 rows, MI355X: 132 / 178 us here, 109 there).  Nine rows of 151,936 x 2,048 take 177 us here, 117
 // there.
 inline bool head_tokens(int64_t rows, int64_t weight_stride) { return rows <= 8 && weight_stride % 2 == 0; }
 // Columns of a workgroup of either.  Narrower ones where 128 columns leave compute units without a workgroup, and always for rows
@@ -137,7 +138,8 @@ struct HeadRowsArgs {
 };
 hipError_t launch_head_rows(const HeadRowsArgs& a, hipStream_t stream);
 
-// dst[i][0 .. width) = src[first + i][0 .. cols), 0 behind; with y times 1 - (y / cap)^2
+// dst[i][0 .. width) = src[first + i][0 .. cols), 0 behind; with y times 1 - (y / cap)^2, rounded to bf16 once more: an operand of the
+// matrix products (error of both gradients against 64 bits, as a share of their norm: .00225, without a soft cap .00166)
 struct HeadPackArgs {
   HeadChunk chunk;
   const uint16_t* src;

@@ -1,9 +1,12 @@
-// Logits of a head and the sums of their softmax: x = h W^T (+ bias, soft cap) in the matrix cores, one 256 x 256 tile per workgroup
-// (64 or 128 rows where there are no more), and what becomes of a tile before it leaves the registers.
+// Logits of a head and the sums of their softmax: x = h W^T (+ bias, soft cap) in the matrix cores, and what becomes of a tile before it
+// leaves the registers.  Workgroups take one tile of 256 x 256 after the other (128 x 256 for up to 128 rows, 128 x 128 in small calls);
+// up to 64 rows have kernels of their own, which read the weights straight into registers.
 //
 // The sums of a row are taken against a reference r: sum 2^(x c - r).  r is the row's own r0 (a true logit of the row, its label's as a rule,
 // rounded to a whole number), so that one pass suffices and what is kept of different tiles fits together; only 128 columns whose largest
 // logit lies 2^40 and more above it take that one, rounded, instead.  References are whole numbers: bringing two together is exact.
+// What is kept is rounded to bf16, as an operand of the gradients' matrix products: half a step of the probability whatever the logit's
+// size, in half the bytes of fp32 (2.5 GB for 8,192 rows of 151,936).
 #include "npd_head.hpp"
 
 namespace npd {

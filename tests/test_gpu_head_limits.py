@@ -87,3 +87,50 @@ def test_columns_between_a_far_label_and_the_top(T, cap):
              mask=torch.ones(T, dtype=torch.uint8, device=dev()), bias=None, idx=None, val=None)
     got = check_loss(s, cap=cap, ce=1.0)
     assert bool((got["grad_weight"][3:40, 0] > 0).all())
+
+
+@pytest.mark.parametrize("T,V,D", [(3, 700, 40), (40, 333, 61), (200, 1003, 72)])
+def test_logits_and_their_backward_pass_replay_from_a_graph(T, V, D):
+    """One graph of both, replayed with other inputs and eager calls in between; workspaces of the graph's own."""
+    s = inputs(T, V, D, bias=True)
+    g = torch.zeros((T, V), dtype=torch.bfloat16, device=dev())
+    out = [torch.empty((T, V), dtype=torch.bfloat16, device=dev()), torch.empty_like(s["hidden"]), torch.empty_like(s["weight"]),
+           torch.empty(V, dtype=torch.bfloat16, device=dev())]
+
+    def call():
+        npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], softcap=20.0, logits_out=out[0])
+        npd.npd_head_logits_bwd(g, s["hidden"], s["weight"], logits=out[0], softcap=20.0, grad_hidden=out[1], grad_weight=out[2],
+                                grad_bias=out[3])
+
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        other = inputs(T, V, D, bias=True, seed=i + 1)
+        for n in ("hidden", "weight", "bias"):
+            s[n].copy_(other[n])
+        g.copy_(0.1 * torch.randn((T, V), device=dev(), generator=torch.Generator(device=dev()).manual_seed(i)))
+        got = []
+        for run in (graph.replay, call):
+            for t in out:
+                t.fill_(float("nan"))
+            run()
+            torch.cuda.synchronize()
+            got.append([t.clone() for t in out])
+        for a, b in zip(*got):
+            assert torch.equal(a, b) and bool(a.isfinite().all())
+
+
+def test_logits_on_another_stream():
+    s = inputs(150, 900, 61, bias=True)   # (rows that are copied into the call's own workspace)
+    want = torch.empty((150, 900), dtype=torch.bfloat16, device=dev())
+    npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], logits_out=want)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(want) for _ in range(6)]
+    for i, out in enumerate(outs):
+        with torch.cuda.stream(streams[i % 2]):
+            npd.npd_head_logits(s["hidden"], s["weight"], bias=s["bias"], logits_out=out)
+    torch.cuda.synchronize()
+    for out in outs:
+        assert torch.equal(out, want)
