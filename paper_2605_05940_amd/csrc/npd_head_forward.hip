@@ -16,7 +16,9 @@ constexpr float kHeadHeadroom = 40.0f;  // log2
 
 // cap tanh(x / cap).  With w = 2 log2(e) x / cap: tanh = 1 - 2 / (1 + 2^w), whose rounding errors are absolute (2^-22), from |w| = 1 (tanh
 // .33) on; below w P(w^2), P fitted there to 3.3e-8 relative.  Either is within 2^-20 of itself, so that a logit's accuracy does not
-// depend on the cap: the first form alone is off by cap 2^-22, 0.09 at a cap of 1e6.
+// depend on the cap: the first form alone is off by cap 2^-22, 0.09 at a cap of 1e6.  Measured (MI355X): the forward kernel of 6,554 x
+// 262,144 x 1,152 4.72 ms with the first form alone, 5.04 with both; one of the two by a branch where all values of a wave allow it is 0.1 ms
+// faster there and 5 % slower in small calls (333 x 50,003 x 1,000 logits 88.3 and 92.2 us).
 struct SoftCap {
   float cap, k2;
   __device__ __forceinline__ explicit SoftCap(float c) : cap(c), k2(2.0f * kLog2e / c) {}

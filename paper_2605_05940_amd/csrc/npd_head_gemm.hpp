@@ -296,7 +296,7 @@ struct HeadProduct {
 
   // acc += p q, written out so that the sums stay where they are (256 registers of sums leave the compiler none to move them
   // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one).  An operand that a vector instruction
-  // wrote may be read two wait states later, the sums by anything else eleven (see HeadSource::load; s_nop 1 in here: 7 %).
+  // wrote may be read two wait states later, the sums by anything else eleven (see HeadSource::load; with s_nop 1 in here as well: 7 %).
   static __device__ __forceinline__ void multiply(f32x4& c, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   }
