@@ -489,7 +489,9 @@ def npd_head_workspace_bytes(op: int, n_tokens: int, vocab: int, width: int, *, 
     """Bytes of workspace that a call of a head operator (``op``: ``NPD_HEAD_LOSS``, ``NPD_HEAD_LOGITS`` or
     ``NPD_HEAD_LOGITS_BWD``) takes: the least, or as many as it can make use of.  ``flags``: ``NPD_HEAD_GRAD_*`` of the gradients
     that it is given, ``NPD_HEAD_UNALIGNED`` where hidden, weight or grad_logits do not begin on 16 bytes (a view; torch's
-    allocations do).  Strides are in elements between rows and default to rows without gaps."""
+    allocations do).  Strides are in elements between rows and default to rows without gaps (a matrix of one row has none)."""
+    hidden_stride, logits_stride = (hidden_stride, logits_stride) if n_tokens > 1 else (None, None)
+    weight_stride = weight_stride if vocab > 1 else None
     grads = flags & (NPD_HEAD_GRAD_HIDDEN | NPD_HEAD_GRAD_WEIGHT | NPD_HEAD_GRAD_BIAS)
     desc = _head_desc(n_tokens, vocab, width, hidden_stride or width, weight_stride or width, width, width, logits_stride or vocab, topk,
                       flags, 1.0, 1.0, 1.0 if grads and not topk else 0.0, softcap)

@@ -156,3 +156,14 @@ def test_the_workspace_that_a_call_takes(monkeypatch):
             call(**dict(a, workspace=room[:-1]))
         assert e.value.status == 6
     assert npd.npd_head_workspace_bytes(binding.NPD_HEAD_LOSS, 0, V, D) == 0
+
+
+def test_one_row_has_no_stride(monkeypatch):
+    """As in the calls: the rows of a padded buffer, one of which is taken."""
+    monkeypatch.setattr(binding, "load", LOAD)
+    size = npd.npd_head_workspace_bytes
+    for op in (binding.NPD_HEAD_LOSS, binding.NPD_HEAD_LOGITS, binding.NPD_HEAD_LOGITS_BWD):
+        flags = 0 if op == binding.NPD_HEAD_LOGITS else 7
+        one = size(op, 1, 1000, 64, flags=flags)
+        assert size(op, 1, 1000, 64, flags=flags, hidden_stride=67, logits_stride=1003) == one
+        assert size(op, 100, 1, 64, flags=flags, weight_stride=67) == size(op, 100, 1, 64, flags=flags)
