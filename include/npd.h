@@ -78,6 +78,8 @@ enum {
   NPD_DEV_BAD_LABEL = 1,      /* labels[p] outside [0, V) at a scored position        */
   NPD_DEV_BAD_TOPK_INDEX = 2, /* teacher_idx outside [0, V) at a scored position      */
   NPD_DEV_BAD_CU_SEQLENS = 4, /* cu_seqlens decreasing or outside [0, T]              */
+  NPD_DEV_BAD_SAMPLING = 16,  /* a row's temperature, top-k, top-p, min-p or random number is out of range */
+  NPD_DEV_BAD_LOGITS = 32,    /* a row to draw from holds NaN or +inf, or nothing but -inf                 */
   NPD_DEV_GANG_TIMEOUT = 8    /* workgroups that share a row gave up waiting for one another (never in a healthy
                                  run: every such wait is bounded so that a kernel cannot hang); the outputs of the
                                  rows concerned are NaN                                                        */
@@ -410,7 +412,7 @@ enum {
 };
 
 /* which entry point npd_head_workspace_bytes() is asked about */
-enum { NPD_HEAD_LOSS = 0, NPD_HEAD_LOGITS = 1, NPD_HEAD_LOGITS_BWD = 2 };
+enum { NPD_HEAD_LOSS = 0, NPD_HEAD_LOGITS = 1, NPD_HEAD_LOGITS_BWD = 2, NPD_HEAD_LOGITS_INT8 = 3 };
 
 typedef struct {
   int64_t n_tokens;           /* T in [1, NPD_HEAD_MAX_TOKENS]                                       */
@@ -502,6 +504,134 @@ npd_status npd_head_logits(const npd_head_desc* desc, const void* hidden, const 
 npd_status npd_head_logits_bwd(const npd_head_desc* desc, const void* grad_logits, const void* logits,
                                const void* hidden, const void* weight, void* grad_hidden, void* grad_weight,
                                void* grad_bias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The norm in front of the head: layer norm, or with NPD_NORM_RMS its form without a mean (mean = 0 below).
+ */
+/* npd_norm_desc.flags; all but NPD_NORM_RMS belong to the backward pass */
+enum {
+  NPD_NORM_RMS = 1u,         /* no mean is taken away                                                              */
+  NPD_NORM_GRAD_X = 2u,      /* grad_x is given                                                                    */
+  NPD_NORM_GRAD_WEIGHT = 4u, /* grad_weight is given                                                               */
+  NPD_NORM_GRAD_BIAS = 8u,   /* grad_bias is given                                                                 */
+  NPD_NORM_ACCUMULATE = 16u  /* grad_weight and grad_bias are added to (in fp32, rounded once) instead of written  */
+};
+
+typedef struct {
+  int64_t n_tokens;      /* T in [1, NPD_HEAD_MAX_TOKENS]                                             */
+  int64_t x_stride;      /* elements between rows of x (>= D)                                         */
+  int64_t y_stride;      /* of y, in the backward pass of grad_y (>= D)                               */
+  int64_t grad_x_stride; /* of grad_x, with NPD_NORM_GRAD_X (>= D)                                    */
+  int32_t width;         /* D in [1, NPD_HEAD_MAX_WIDTH]                                              */
+  uint32_t flags;        /* NPD_NORM_*                                                                */
+  float eps;             /* forward: finite, >= 0                                                     */
+} npd_norm_desc;
+
+/*
+ *   mean[p] = sum_d x[p, d] / D,   rstd[p] = 1 / sqrt(sum_d (x[p, d] - mean[p])^2 / D + eps)
+ *   y[p, d] = (x[p, d] - mean[p]) rstd[p] weight[d] + bias[d], rounded to bf16 once
+ *
+ *   x     bf16 [T, x_stride], required          weight, bias  bf16 [D] or NULL (1 and 0)
+ *   y     bf16 [T, y_stride], required; what lies between D and the stride is left as it was
+ *   mean  fp32 [T] or NULL (with NPD_NORM_RMS: NULL)      rstd  fp32 [T] or NULL
+ *
+ * Statistics are fp32 (sums of squares beyond that range, of values of 1e17 and more, give rstd 0).  A row of equal values
+ * with eps = 0 has no rstd (inf) and gives NaN; NaN or infinities stay in their row.
+ */
+npd_status npd_layer_norm(const npd_norm_desc* desc, const void* x, const void* weight, const void* bias, void* y,
+                          float* mean, float* rstd, void* stream);
+
+/*
+ * Its backward pass.  With n[p, d] = (x[p, d] - mean[p]) rstd[p] and a[p, d] = grad_y[p, d] weight[d],
+ *
+ *   grad_x[p, d]   = rstd[p] (a[p, d] - mean_d(a[p]) - n[p, d] mean_d(a[p] n[p]))    (NPD_NORM_RMS: without mean_d(a[p]))
+ *   grad_weight[d] = sum_p grad_y[p, d] n[p, d];   grad_bias[d] = sum_p grad_y[p, d]
+ *
+ * each rounded to bf16 once, sums in fp32.  Any of them may be asked for by its flag, one at least.
+ *
+ *   grad_y  bf16 [T, y_stride], x  bf16 [T, x_stride], rstd  fp32 [T], required; mean  fp32 [T], required without
+ *   NPD_NORM_RMS, else NULL; weight  bf16 [D] or NULL;  grad_x  bf16 [T, grad_x_stride]  grad_weight, grad_bias  bf16 [D]
+ *   workspace  device, >= npd_layer_norm_workspace_bytes(desc) bytes (0 for grad_x alone), 256-byte aligned; as for the head's calls
+ *
+ * Reproducible bit by bit for the same sizes.  The gradients that rows share are non-finite where a row's is.
+ */
+npd_status npd_layer_norm_bwd(const npd_norm_desc* desc, const void* grad_y, const void* x, const void* weight,
+                              const float* mean, const float* rstd, void* grad_x, void* grad_weight, void* grad_bias,
+                              void* workspace, size_t workspace_bytes, void* stream);
+/* Host call; 0 is a legal answer and what an invalid desc gets. */
+size_t npd_layer_norm_workspace_bytes(const npd_norm_desc* desc);
+
+/*
+ * Rows of bf16 values as 8-bit integers, for npd_head_logits_int8: hidden states of a call, or the head's weights once.
+ *
+ *   scale[r] = max_d |x[r, d]| / 127;   q[r, d] = x[r, d] / scale[r] to the nearest whole number (of two the even one), in -127 .. 127
+ *
+ * q is exact (of 127 x / max, before scale is rounded).  A row of zeros has scale 0 and zeros; a row with NaN or an infinity
+ * scale NaN and zeros.
+ *
+ *   x  bf16 [R, x_stride];  q  int8 [R, q_stride], what lies between the width and the stride is left as it was;  scale  fp32 [R]
+ *   n_rows in [1, NPD_HEAD_MAX_TOKENS], width in [1, NPD_HEAD_MAX_WIDTH], strides in elements, >= width
+ */
+npd_status npd_quantize_rows(int64_t n_rows, int32_t width, int64_t x_stride, int64_t q_stride, const void* x, int8_t* q,
+                             float* scale, void* stream);
+
+/*
+ * npd_head_logits of 8-bit hidden states and weights:
+ *
+ *   logits[p, v] = hidden_scale[p] weight_scale[v] sum_d hidden[p, d] weight[v, d] + bias[v],   soft-capped as there,
+ *
+ * the sum exact, the rest in fp32, rounded to bf16 once.
+ *
+ *   desc          n_tokens, vocab, width, hidden_stride, weight_stride, logits_stride, softcap and NPD_HEAD_UNALIGNED (hidden or
+ *                 weight begins anywhere, not on 16 bytes) as for npd_head_logits; strides of hidden and weight are bytes
+ *   hidden        int8 [T, hidden_stride], hidden_scale  fp32 [T], weight  int8 [V, weight_stride], weight_scale  fp32 [V], required
+ *   bias          bf16 [V] or NULL         logits  bf16 [T, logits_stride], required
+ *   workspace     >= npd_head_workspace_bytes(desc, NPD_HEAD_LOGITS_INT8) bytes.  Widths and strides that are multiples of 16 need
+ *                 none; others are copied in calls of more than 64 positions, so weights are best laid out with such rows
+ */
+npd_status npd_head_logits_int8(const npd_head_desc* desc, const int8_t* hidden, const float* hidden_scale,
+                                const int8_t* weight, const float* weight_scale, const void* bias, void* logits,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int64_t n_tokens;      /* T in [1, NPD_MAX_TOKENS]: rows                                            */
+  int64_t logits_stride; /* elements between rows (>= V)                                              */
+  int32_t vocab;         /* V in [1, NPD_MAX_VOCAB]                                                   */
+  uint32_t flags;        /* 0                                                                         */
+  float temperature;     /* finite, >= 0; 0: the largest logit                                        */
+  int32_t top_k;         /* >= 0; 0: no limit                                                         */
+  float top_p;           /* in [0, 1]; 1: no limit                                                    */
+  float min_p;           /* in [0, 1]; 0: no limit                                                    */
+} npd_sample_desc;
+
+/*
+ * A token for each row of logits, from a given random number: one step of a rollout (and what Delta-IFD and the policy monitor
+ * want of it besides).  A row's entries are ordered by logit, equal ones by increasing id; entries of -inf are not among them.
+ * With weights w = exp((x - x_max) / temperature), what is kept of that order are the first n, n >= 1, by
+ *
+ *   top_k > 0   at most top_k;
+ *   top_p < 1   the fewest whose weights add up to top_p times the sum of what top_k left;
+ *   min_p > 0   those of weight min_p and more (of min_p times the largest's probability);
+ *   temperature 0   the first alone;
+ *
+ *   token[p]    the first of them whose cumulative weight exceeds uniform[p] times the sum of the n
+ *   logprob[p]  log of its weight over that sum: of the probability with which it was drawn (0 at temperature 0)
+ *   nll[p]      log(sum_v exp(x[p, v])) - x[p, token]: its NLL under the untruncated distribution at temperature 1
+ *   kept[p]     n
+ *
+ *   logits  bf16 [T, logits_stride], required     uniform  fp32 [T] in [0, 1), required
+ *   loss_mask  uint8 [T] or NULL: rows of 0 (sequences that have ended) get token -1, zeros, and are not read
+ *   temperature, top_k, top_p, min_p   fp32 / int32 / fp32 / fp32 [T], each NULL: the desc's for all rows
+ *   token  int32 [T], required;  logprob, nll  fp32 [T], kept  int32 [T], each may be NULL
+ *   dev_status  int32 [1] or NULL: a setting or random number out of range (NPD_DEV_BAD_SAMPLING), NaN, +inf or nothing but
+ *               -inf among a row's logits (NPD_DEV_BAD_LOGITS) give token -1, NaN and kept 0
+ *
+ * Weights and their sums are 64-bit; nothing depends on the order in which a row is read: reproducible.  No workspace.
+ */
+npd_status npd_sample_tokens(const npd_sample_desc* desc, const void* logits, const float* uniform,
+                             const uint8_t* loss_mask, const float* temperature, const int32_t* top_k, const float* top_p,
+                             const float* min_p, int32_t* token, float* logprob, float* nll, int32_t* kept,
+                             int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -21,11 +21,13 @@ NPD_TEACHER_DENSE_BF16, NPD_TEACHER_TOPK, NPD_TEACHER_NONE = 0, 1, 2
 NPD_FLAG_FWD_ONLY, NPD_FLAG_INPLACE_GRAD, NPD_FLAG_NO_WORKSPACE = 1, 2, 4
 NPD_DIV_FORWARD_KL, NPD_DIV_REVERSE_KL, NPD_DIV_SKEW_KL, NPD_DIV_SKEW_REVERSE_KL = 0, 1, 2, 3
 NPD_DEV_BAD_LABEL, NPD_DEV_BAD_TOPK_INDEX, NPD_DEV_BAD_CU_SEQLENS, NPD_DEV_GANG_TIMEOUT = 1, 2, 4, 8
+NPD_DEV_BAD_SAMPLING, NPD_DEV_BAD_LOGITS = 16, 32
 NPD_ZONE_DEGENERATE, NPD_ZONE_PROXIMAL, NPD_ZONE_DISCONNECT, NPD_ZONE_INVALID = 0, 1, 2, 3
 NPD_IFD_REQUIRE_TEACHER_LE_1 = 1
 NPD_TOPK_LOG_PROBS = 1
 NPD_HEAD_GRAD_HIDDEN, NPD_HEAD_GRAD_WEIGHT, NPD_HEAD_GRAD_BIAS, NPD_HEAD_ACCUMULATE, NPD_HEAD_UNALIGNED = 1, 2, 4, 8, 16
-NPD_HEAD_LOSS, NPD_HEAD_LOGITS, NPD_HEAD_LOGITS_BWD = 0, 1, 2
+NPD_HEAD_LOSS, NPD_HEAD_LOGITS, NPD_HEAD_LOGITS_BWD, NPD_HEAD_LOGITS_INT8 = 0, 1, 2, 3
+NPD_NORM_RMS, NPD_NORM_GRAD_X, NPD_NORM_GRAD_WEIGHT, NPD_NORM_GRAD_BIAS, NPD_NORM_ACCUMULATE = 1, 2, 4, 8, 16
 NOALLOC_WORKSPACE_BYTES = 16 << 20   # NPD_NOALLOC_WORKSPACE_BYTES
 
 EXPORTS = ("npd_version", "npd_status_string", "npd_workspace_bytes", "npd_kd_loss_fwd_bwd",
@@ -33,7 +35,9 @@ EXPORTS = ("npd_version", "npd_status_string", "npd_workspace_bytes", "npd_kd_lo
            "npd_kd_loss_fwd_bwd_noalloc", "npd_policy_lag", "npd_segment_ppl", "npd_kd_kernel_name",
            "npd_forward_scratch_bytes", "npd_kd_loss_forward", "npd_workspace_bytes_preferred",
            "npd_kept_workspace_bytes", "npd_kd_loss_fwd_bwd_kept", "npd_head_workspace_bytes",
-           "npd_head_workspace_bytes_preferred", "npd_head_loss_fwd_bwd", "npd_head_logits", "npd_head_logits_bwd")
+           "npd_head_workspace_bytes_preferred", "npd_head_loss_fwd_bwd", "npd_head_logits", "npd_head_logits_bwd",
+           "npd_layer_norm", "npd_layer_norm_bwd", "npd_layer_norm_workspace_bytes", "npd_quantize_rows", "npd_head_logits_int8",
+           "npd_sample_tokens")
 
 
 class NpdError(RuntimeError):
@@ -59,6 +63,19 @@ class HeadDesc(ctypes.Structure):
                 ("logits_stride", ctypes.c_int64), ("topk", ctypes.c_int32), ("flags", ctypes.c_uint32),
                 ("tau", ctypes.c_float), ("grad_scale", ctypes.c_float), ("ce_grad_scale", ctypes.c_float),
                 ("softcap", ctypes.c_float)]
+
+
+class NormDesc(ctypes.Structure):
+    """Mirror of ``npd_norm_desc``."""
+    _fields_ = [("n_tokens", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("grad_x_stride", ctypes.c_int64), ("width", ctypes.c_int32), ("flags", ctypes.c_uint32), ("eps", ctypes.c_float)]
+
+
+class SampleDesc(ctypes.Structure):
+    """Mirror of ``npd_sample_desc``."""
+    _fields_ = [("n_tokens", ctypes.c_int64), ("logits_stride", ctypes.c_int64), ("vocab", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float)]
 
 
 _lib = None
@@ -123,6 +140,17 @@ def load() -> ctypes.CDLL:
             if here or hasattr(L, name):
                 getattr(L, name).restype = result
                 getattr(L, name).argtypes = [ctypes.POINTER(HeadDesc)] + more
+        i64, i32, size = ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+        around = {"npd_layer_norm": (ctypes.c_int, [ctypes.POINTER(NormDesc)] + [_vp] * 7),
+                  "npd_layer_norm_bwd": (ctypes.c_int, [ctypes.POINTER(NormDesc)] + [_vp] * 9 + [size, _vp]),
+                  "npd_layer_norm_workspace_bytes": (size, [ctypes.POINTER(NormDesc)]),
+                  "npd_quantize_rows": (ctypes.c_int, [i64, i32, i64, i64] + [_vp] * 4),
+                  "npd_head_logits_int8": (ctypes.c_int, [ctypes.POINTER(HeadDesc)] + [_vp] * 7 + [size, _vp]),
+                  "npd_sample_tokens": (ctypes.c_int, [ctypes.POINTER(SampleDesc)] + [_vp] * 13)}
+        for name, (result, arguments) in around.items():
+            if here or hasattr(L, name):
+                getattr(L, name).restype = result
+                getattr(L, name).argtypes = arguments
         _host = _load_host(L) if native else None
         _lib = L
     return _lib
@@ -441,13 +469,13 @@ def npd_segment_ppl(seg_mean_nll: torch.Tensor, seg_count: torch.Tensor, seg_ppl
 
 # ------------------------------------------------------------------------------------------------------------- the head
 
-def _matrix(name: str, t: Optional[torch.Tensor], shape):
-    """Device pointer of a bf16 matrix of ``shape`` with unit stride along its rows (None if it is absent)."""
+def _matrix(name: str, t: Optional[torch.Tensor], shape, dtype=torch.bfloat16):
+    """Device pointer of a matrix of ``shape`` with unit stride along its rows (None if it is absent)."""
     if t is None:
         return None
     if t.shape != shape or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be {list(shape)} with unit stride along its rows")
-    return _ptr(t, torch.bfloat16)
+    return _ptr(t, dtype)
 
 
 def _pitch(t: Optional[torch.Tensor]) -> int:
@@ -486,8 +514,8 @@ def _head_workspace(L, desc, op: int, workspace: Optional[torch.Tensor]):
 def npd_head_workspace_bytes(op: int, n_tokens: int, vocab: int, width: int, *, topk: int = 0, flags: int = 0, softcap: float = 0.0,
                              hidden_stride: Optional[int] = None, weight_stride: Optional[int] = None,
                              logits_stride: Optional[int] = None, preferred: bool = False) -> int:
-    """Bytes of workspace that a call of a head operator (``op``: ``NPD_HEAD_LOSS``, ``NPD_HEAD_LOGITS`` or
-    ``NPD_HEAD_LOGITS_BWD``) takes: the least, or as many as it can make use of.  ``flags``: ``NPD_HEAD_GRAD_*`` of the gradients
+    """Bytes of workspace that a call of a head operator (``op``: ``NPD_HEAD_LOSS``, ``NPD_HEAD_LOGITS``,
+    ``NPD_HEAD_LOGITS_BWD`` or ``NPD_HEAD_LOGITS_INT8``) takes: the least, or as many as it can make use of.  ``flags``: ``NPD_HEAD_GRAD_*`` of the gradients
     that it is given, ``NPD_HEAD_UNALIGNED`` where hidden, weight or grad_logits do not begin on 16 bytes (a view; torch's
     allocations do).  Strides are in elements between rows and default to rows without gaps (a matrix of one row has none)."""
     hidden_stride, logits_stride = (hidden_stride, logits_stride) if n_tokens > 1 else (None, None)
@@ -590,3 +618,125 @@ def npd_head_logits_bwd(grad_logits: torch.Tensor, hidden: torch.Tensor, weight:
     L = load()
     _block, ws, n = _head_workspace(L, desc, NPD_HEAD_LOGITS_BWD, workspace)
     _check(L.npd_head_logits_bwd(*args, ws, n, _stream()))
+
+
+# ------------------------------------------------------------------------------------------------- on either side of the head
+
+def _width32(n: int) -> int:
+    """A size for a field of 32 bits: what does not fit stays too large to be taken."""
+    return min(n, 0x7fffffff)
+
+
+def npd_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, y_out: torch.Tensor,
+                   bias: Optional[torch.Tensor] = None, eps: float = 1e-5, rms: bool = False,
+                   mean_out: Optional[torch.Tensor] = None, rstd_out: Optional[torch.Tensor] = None) -> None:
+    """Enqueue ``y_out = (x - mean) * rstd * weight + bias`` of every row of a bf16 matrix (``rms``: without the mean), and the
+    row statistics that the backward pass takes (see ``npd_layer_norm`` in npd.h)."""
+    T, D = x.shape
+    _on_current_device(x, weight, bias, y_out, mean_out, rstd_out)
+    desc = NormDesc(T, _pitch(x), _pitch(y_out), 0, _width32(D), NPD_NORM_RMS if rms else 0, eps)
+    _check(load().npd_layer_norm(
+        ctypes.byref(desc), _matrix("x", x, (T, D)), _array("weight", weight, D, torch.bfloat16), _array("bias", bias, D, torch.bfloat16),
+        _matrix("y_out", y_out, (T, D)), _array("mean_out", mean_out, T, torch.float32), _array("rstd_out", rstd_out, T, torch.float32),
+        _stream()))
+
+
+def _norm_grad_desc(T, D, strides, rms, grad_x, grad_weight, grad_bias, accumulate):
+    flags = ((NPD_NORM_RMS if rms else 0) | (NPD_NORM_GRAD_X if grad_x else 0) | (NPD_NORM_GRAD_WEIGHT if grad_weight else 0) |
+             (NPD_NORM_GRAD_BIAS if grad_bias else 0) | (NPD_NORM_ACCUMULATE if accumulate else 0))
+    return NormDesc(T, *strides, _width32(D), flags, 0.0)
+
+
+def npd_layer_norm_workspace_bytes(n_tokens: int, width: int, *, grad_weight: bool = True, grad_bias: bool = False) -> int:
+    """Bytes of workspace that ``npd_layer_norm_bwd`` takes for the gradients of the norm's parameters that it is asked for."""
+    if not (grad_weight or grad_bias):
+        return 0
+    desc = _norm_grad_desc(n_tokens, width, (width, width, width), False, False, grad_weight, grad_bias, False)
+    return int(load().npd_layer_norm_workspace_bytes(ctypes.byref(desc)))
+
+
+def npd_layer_norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, rstd: torch.Tensor,
+                       mean: Optional[torch.Tensor] = None, rms: bool = False, grad_x: Optional[torch.Tensor] = None,
+                       grad_weight: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                       accumulate: bool = False, workspace: Optional[torch.Tensor] = None) -> None:
+    """Enqueue the backward pass of ``npd_layer_norm`` from the statistics that it left, for the gradients that are given a tensor
+    (see ``npd_layer_norm_bwd`` in npd.h).  ``accumulate``: the gradients of weight and bias are added to what their tensors
+    hold.  ``workspace``: a uint8 tensor of at least ``npd_layer_norm_workspace_bytes`` bytes; without it the call takes a block
+    from torch's allocator for as long as it is being enqueued."""
+    T, D = x.shape
+    _on_current_device(grad_y, x, weight, rstd, mean, grad_x, grad_weight, grad_bias, workspace)
+    desc = _norm_grad_desc(T, D, (_pitch(x), _pitch(grad_y), _pitch(grad_x)), rms, grad_x is not None, grad_weight is not None,
+                           grad_bias is not None, accumulate)
+    args = (_matrix("grad_y", grad_y, (T, D)), _matrix("x", x, (T, D)), _array("weight", weight, D, torch.bfloat16),
+            _array("mean", mean, T, torch.float32), _array("rstd", rstd, T, torch.float32), _matrix("grad_x", grad_x, (T, D)),
+            _array("grad_weight", grad_weight, D, torch.bfloat16), _array("grad_bias", grad_bias, D, torch.bfloat16))
+    L = load()
+    ref = ctypes.byref(desc)
+    _block, ws, n = _given_or_own(workspace, lambda: L.npd_layer_norm_workspace_bytes(ref))
+    _check(L.npd_layer_norm_bwd(ref, *args, ws, n, _stream()))
+
+
+def _given_or_own(workspace: Optional[torch.Tensor], bytes_of):
+    """(tensor, pointer, bytes) of a call's workspace: the caller's, or a block from torch's stream-ordered allocator."""
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        return workspace, _ptr(workspace), workspace.numel() * workspace.element_size()
+    want = bytes_of()
+    if not want:
+        return None, None, 0
+    block = torch.empty(want, dtype=torch.uint8, device="cuda")
+    return block, block.data_ptr(), want
+
+
+def npd_quantize_rows(x: torch.Tensor, *, q_out: torch.Tensor, scale_out: torch.Tensor) -> None:
+    """Enqueue ``scale_out = max|x| / 127`` and ``q_out = round(x / scale_out)`` of every row of a bf16 matrix, as 8-bit integers
+    (see ``npd_quantize_rows`` in npd.h).  A ``q_out`` whose rows begin on multiples of 16 (a view of a wider tensor where the
+    width is none) is read as it is by ``npd_head_logits_int8``."""
+    R, D = x.shape
+    _on_current_device(x, q_out, scale_out)
+    _check(load().npd_quantize_rows(R, _width32(D), _pitch(x), _pitch(q_out), _matrix("x", x, (R, D)),
+                                    _matrix("q_out", q_out, (R, D), torch.int8), _array("scale_out", scale_out, R, torch.float32),
+                                    _stream()))
+
+
+def npd_head_logits_int8(hidden: torch.Tensor, hidden_scale: torch.Tensor, weight: torch.Tensor, weight_scale: torch.Tensor, *,
+                         logits_out: torch.Tensor, bias: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                         workspace: Optional[torch.Tensor] = None) -> None:
+    """Enqueue ``npd_head_logits`` of 8-bit hidden states and weights with a scale for each of their rows (see
+    ``npd_head_logits_int8`` in npd.h)."""
+    T, D = hidden.shape
+    V = weight.shape[0]
+    _on_current_device(hidden, hidden_scale, weight, weight_scale, logits_out, bias, workspace)
+    desc = _head_desc(T, V, D, _pitch(hidden), _pitch(weight), 0, 0, _pitch(logits_out), 0,
+                      _head_flags(None, None, None, False, hidden, weight), 1.0, 0.0, 0.0, softcap)
+    args = (desc, _matrix("hidden", hidden, (T, D), torch.int8), _array("hidden_scale", hidden_scale, T, torch.float32),
+            _matrix("weight", weight, (V, D), torch.int8), _array("weight_scale", weight_scale, V, torch.float32),
+            _array("bias", bias, V, torch.bfloat16), _matrix("logits_out", logits_out, (T, V)))
+    L = load()
+    _block, ws, n = _given_or_own(workspace, lambda: L.npd_head_workspace_bytes(desc, NPD_HEAD_LOGITS_INT8))
+    _check(L.npd_head_logits_int8(*args, ws, n, _stream()))
+
+
+def npd_sample_tokens(logits: torch.Tensor, uniform: torch.Tensor, *, tokens_out: torch.Tensor, temperature=1.0, top_k=0,
+                      top_p=1.0, min_p=0.0, loss_mask: Optional[torch.Tensor] = None, logprob_out: Optional[torch.Tensor] = None,
+                      nll_out: Optional[torch.Tensor] = None, kept_out: Optional[torch.Tensor] = None,
+                      dev_status: Optional[torch.Tensor] = None) -> None:
+    """Enqueue the drawing of a token from every row of bf16 logits by the random numbers ``uniform`` in [0, 1) (see
+    ``npd_sample_tokens`` in npd.h).  ``temperature``, ``top_p``, ``min_p`` (numbers, or fp32 tensors of one per row) and ``top_k``
+    (int32) truncate the distribution; 0 or None for no ``top_k``, 1 for no ``top_p``, 0 for no ``min_p``, temperature 0 for the largest
+    logit."""
+    T, V = logits.shape
+    top_k = 0 if top_k is None else top_k
+    settings = (temperature, top_k, top_p, min_p)
+    rows = [s if isinstance(s, torch.Tensor) else None for s in settings]
+    numbers = [n if r is None else 0 for n, r in zip(settings, rows)]
+    _on_current_device(logits, uniform, tokens_out, *rows, loss_mask, logprob_out, nll_out, kept_out, dev_status)
+    desc = SampleDesc(T, _pitch(logits), _width32(V), 0, numbers[0], max(-1, _width32(numbers[1])), numbers[2], numbers[3])
+    f32, i32 = torch.float32, torch.int32
+    _check(load().npd_sample_tokens(
+        ctypes.byref(desc), _matrix("logits", logits, (T, V)), _array("uniform", uniform, T, f32),
+        _array("loss_mask", loss_mask, T, torch.uint8), _array("temperature", rows[0], T, f32), _array("top_k", rows[1], T, i32),
+        _array("top_p", rows[2], T, f32), _array("min_p", rows[3], T, f32), _array("tokens_out", tokens_out, T, i32),
+        _array("logprob_out", logprob_out, T, f32), _array("nll_out", nll_out, T, f32), _array("kept_out", kept_out, T, i32),
+        _array("dev_status", dev_status, 1, i32), _stream()))

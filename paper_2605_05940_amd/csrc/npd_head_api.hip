@@ -6,6 +6,7 @@
 #include "../../include/npd.h"
 #include "npd_check.hpp"
 #include "npd_head.hpp"
+#include "npd_int8.hpp"
 
 namespace {
 
@@ -233,6 +234,7 @@ npd_status check_grads(const npd_head_desc& d, const void* gh, const void* gw, c
 extern "C" {
 
 size_t npd_head_workspace_bytes(const npd_head_desc* desc, int op) {
+  if (op == NPD_HEAD_LOGITS_INT8) return int8_workspace_bytes(desc);
   if (check_head(desc, op) != NPD_OK) return 0;
   // (one chunk more needs sums of the weights' gradient between them: the shortest chunks are not always the least)
   size_t least = SIZE_MAX;
@@ -244,6 +246,7 @@ size_t npd_head_workspace_bytes(const npd_head_desc* desc, int op) {
 }
 
 size_t npd_head_workspace_bytes_preferred(const npd_head_desc* desc, int op) {
+  if (op == NPD_HEAD_LOGITS_INT8) return int8_workspace_bytes(desc);
   return check_head(desc, op) == NPD_OK ? make_plan(*desc, op, kCaps[0]).bytes : 0;
 }
 

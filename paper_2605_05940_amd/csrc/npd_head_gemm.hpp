@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "npd_device.hpp"
 
 namespace npd {
@@ -267,14 +269,19 @@ struct HeadReader {
 // requests the next one's first steps while it works on its own last ones, so that they are there when the tile's sums
 // have been dealt with.  acc[i][j][e]: row m = 16 i + (lane & 15) of the wave's 16 MF, column 16 j + 4 (lane >> 4) + e of its
 // 16 NF (PAIRED: 32 (j / 2) + 8 (lane >> 4) + 4 (j & 1) + e).
-template <int MF, int NF, bool QKS, bool PKS, bool PAIRED>
+//
+// BYTES: the operands are 8-bit integers, two to each "value" above (rows of an even number of bytes, k counted in pairs), and the
+// sums 32-bit ones.  v_mfma_i32_16x16x64_i8 takes its operands from the same 16 bytes of a lane in the same time.
+template <int MF, int NF, bool QKS, bool PKS, bool PAIRED, bool BYTES = false>
 struct HeadProduct {
+  static_assert(!BYTES || !(QKS || PKS), "bytes are read along k");
+  using Sum = std::conditional_t<BYTES, i32x4, f32x4>;
   using Q = HeadSource<MF, QKS>;
   using P = HeadSource<NF, PKS>;
   static constexpr int kLds = kHeadStages * (Q::kBytes + P::kBytes);
   static constexpr int kTileM = 32 * MF, kTileN = 32 * NF;
   static constexpr int kLoads = Q::kLoads + P::kLoads;
-  f32x4 acc[MF][NF];
+  Sum acc[MF][NF];
   Q q;
   P p;
   HeadReader<MF, QKS, false> qr;
@@ -297,8 +304,11 @@ struct HeadProduct {
   // acc += p q, written out so that the sums stay where they are (256 registers of sums leave the compiler none to move them
   // through: from the builtin it makes copies in every step, 24 of 64 products then wait for one).  An operand that a vector instruction
   // wrote may be read two wait states later, the sums by anything else eleven (see HeadSource::load; with s_nop 1 in here as well: 7 %).
-  static __device__ __forceinline__ void multiply(f32x4& c, const bf16x8& a, const bf16x8& b) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  static __device__ __forceinline__ void multiply(Sum& c, const bf16x8& a, const bf16x8& b) {
+    if constexpr (BYTES)
+      asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else
+      asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
   }
 
   // One step, in stage S; requests step `ahead` of (nq, np) into the same stage.

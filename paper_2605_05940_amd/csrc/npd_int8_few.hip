@@ -1,0 +1,374 @@
+// Rows to 8-bit integers, and logits of a head in them for up to 64 rows, where reading the weights is all the time: they go straight
+// into registers, at any alignment.
+#include "npd_int8.hpp"
+#include "npd_softcap.hpp"
+
+namespace npd {
+namespace {
+
+// ------------------------------------------------------------------------------------------------------- whole numbers
+
+constexpr int kQuantizeThreads = 256;
+template <int TH>
+constexpr int quantize_block() { return TH < kQuantizeThreads ? kQuantizeThreads : TH; }
+
+// Eight values over the row's largest, times 127, to the nearest whole number.  With the row's exponent taken out (`down`) everything
+// below is exact but the quotient; a quotient of 15 and 8 bits that is not half way between two whole numbers is 2^-17 of itself and
+// more away from there, so a product with the reciprocal decides wherever it is further from half way than its own error (two
+// roundings of up to 127: 2^-16), and the division, rounded correctly, does where it is not: it is exact half way.
+__device__ __forceinline__ uint2 quantize8(const uint4& x, int down, float top, float inv) {
+  float v[8], n[8];
+  unpack8(x, v);
+  bool close = false;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    v[t] = __builtin_ldexpf(v[t], down) * 127.0f;
+    const float y = v[t] * inv;
+    n[t] = __builtin_rintf(y);
+    close |= __builtin_fabsf(y - n[t]) > 0.4999f;
+  }
+  if (close) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) n[t] = __builtin_rintf(v[t] / top);
+  }
+  uint32_t w[2] = {};
+#pragma unroll
+  for (int t = 0; t < 8; ++t) w[t >> 2] |= (uint32_t)((int)n[t] & 255) << (8 * (t & 3));
+  return make_uint2(w[0], w[1]);
+}
+
+template <int TH, int G>
+__global__ __launch_bounds__(quantize_block<TH>()) void quantize_kernel(QuantizeArgs a) {
+  __shared__ uint32_t tops[quantize_block<TH>() / kWave];
+  constexpr int kRows = quantize_block<TH>() / TH;
+  const int at = (threadIdx.x % TH) * 8;
+  for (int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / TH; p < a.R; p += (int64_t)gridDim.x * kRows) {
+    const uint16_t* row = a.x + p * a.x_stride;
+    uint4 x[G];
+#pragma unroll
+    for (int u = 0; u < G; ++u) x[u] = load8_of(row, at + 8 * TH * u, a.D);
+    // largest magnitude, as bits: a NaN is above infinity
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t lo = w[t] & 0x7fff, hi = w[t] >> 16 & 0x7fff;
+        top = top > lo ? top : lo;
+        top = top > hi ? top : hi;
+      }
+    }
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) {
+      const uint32_t o = __shfl_xor(top, off, kWave);
+      top = top > o ? top : o;
+    }
+    if constexpr (TH > kWave) {
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < TH / kWave; ++w) top = top > tops[w] ? top : tops[w];
+    }
+    const bool finite = top < 0x7f80;
+    const float most = bf16_one((uint16_t)top);
+    if (threadIdx.x % TH == 0) a.scale[p] = finite ? most / 127.0f : __builtin_nanf("");
+    const int down = top ? -__builtin_amdgcn_frexp_expf(most) : 0;
+    const float m = top ? __builtin_ldexpf(most, down) : 1.0f, inv = 1.0f / m;  // (m in [1/2, 1])
+    int8_t* q = a.q + p * a.q_stride;
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      const int d = at + 8 * TH * u;
+      if (d >= a.D) break;
+      const uint2 w = finite ? quantize8(x[u], down, m, inv) : make_uint2(0, 0);
+      if (d + 8 <= a.D) {
+        __builtin_memcpy(q + d, &w, 8);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (d + t < a.D) q[d + t] = (int8_t)((t < 4 ? w.x : w.y) >> (8 * (t & 3)));
+      }
+    }
+  }
+}
+
+template <int TH, int G>
+hipError_t launch_rows(const QuantizeArgs& a, hipStream_t stream) {
+  constexpr int kRows = quantize_block<TH>() / TH;
+  const int64_t blocks = (a.R + kRows - 1) / kRows;
+  return launch_kernel(quantize_kernel<TH, G>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(quantize_block<TH>()), 0, stream, a);
+}
+
+// ------------------------------------------------------------------------------------------------------------- products
+
+// sixteen bytes at any address
+__device__ __forceinline__ i32x4 load16(const int8_t* p) {
+  i32x4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+// bytes [d, d + 16) of a row of `cols`, 0 behind its end
+__device__ __forceinline__ i32x4 load16_of(const int8_t* row, int d, int cols) {
+  if (d + 16 <= cols) return load16(row + d);
+  uint32_t w[4] = {};
+#pragma unroll
+  for (int t = 0; t < 16; ++t)
+    if (d + t < cols) w[t >> 2] |= (uint32_t)(uint8_t)row[d + t] << (8 * (t & 3));
+  return i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+}
+
+// The end of a workgroup's PART columns, whose sums lie in LDS as [row][PART]: a wave per row, PART / 64 columns per lane.
+template <bool CAP, int PART>
+__device__ __forceinline__ void finish_columns(const Int8Args& a, const int* x) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const SoftCap soft(CAP ? a.cap : 1.0f);
+  constexpr int N = PART < kWave ? 1 : PART / kWave;
+  if (PART < kWave && lane >= PART) return;
+  const int n = blockIdx.x * PART + N * lane;
+  if (n >= a.V) return;
+  float scale[N], bias[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const int v = n + e < a.V ? n + e : n;
+    scale[e] = a.w_scale[v];
+    bias[e] = a.bias ? bf16_one(a.bias[v]) : 0.0f;
+  }
+  for (int m = wave; m < (int)a.T; m += kHeadThreads / kWave) {
+    const float hs = a.h_scale[m];
+    float y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      y[e] = __builtin_fmaf((float)x[m * PART + N * lane + e] * hs, scale[e], bias[e]);
+      if constexpr (CAP) y[e] = soft.cap * soft.tanh_of(y[e]);
+    }
+    uint16_t* out = a.out + m * a.out_stride + n;
+    if (N == 2 && n + 2 <= a.V) {
+      const uint32_t v = pack_bf16(y[0], y[N - 1]);
+      __builtin_memcpy(out, &v, 4);
+    } else {
+      *out = one_bf16(y[0]);
+    }
+  }
+}
+
+// Up to 4 NT rows: v_mfma_i32_4x4x4_16b_i8 as 16 pieces of k of the same four columns and four rows, added up at the end, so that one
+// load of a wave is 256 consecutive bytes of each of four rows of the weights, read past the caches.  Waves begin at different places
+// of their rows and wrap around (rows of a power of two of bytes would else be read out of few memory channels).
+//
+// PART 128: a wave has 32 columns of its own.  32: the four waves have the same ones and every fourth block of k, added up at the end.
+template <int NT, int PART, bool CAP>
+__global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void int8_tokens_kernel(Int8Args a) {
+  constexpr int kWaves = kHeadThreads / kWave, G = 8, kShare = PART == 4 * G ? kWaves : 1;
+  static_assert(PART == 4 * G * kWaves / kShare, "");
+  __shared__ __attribute__((aligned(16))) int x[kShare][4 * NT][PART];
+  typedef int words __attribute__((ext_vector_type(4), aligned(1)));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 3, b = lane >> 2;
+  constexpr int kBlock = 256;  // bytes of k per load
+  const int blocks = a.D / kBlock, tail = blocks * kBlock + 16 * b;
+  const int first = kShare > 1 ? wave : 0, mine = (blocks - first + kShare - 1) / kShare;  // blocks first, first + kShare ..
+  const int c0 = kShare > 1 ? 0 : wave * 4 * G;  // of the workgroup's columns
+  const int8_t *h[NT], *w[G];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int m = 4 * t + i;
+    h[t] = a.h + (m < a.T ? m : a.T - 1) * a.h_stride;
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int v = blockIdx.x * PART + c0 + 4 * g + i;
+    w[g] = a.w + (int64_t)(v < a.V ? v : a.V - 1) * a.w_stride;
+  }
+  i32x4 acc[G][NT];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[g][t] = i32x4{0, 0, 0, 0};
+  auto multiply = [&](const i32x4 (&wv)[G], const i32x4 (&hv)[NT]) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[g][t] = __builtin_amdgcn_mfma_i32_4x4x4i8(wv[g][e], hv[t][e], acc[g][t], 0, 0, 0);
+  };
+  int at = mine > 0 ? (int)((blockIdx.x * 4 + wave) % (unsigned)mine) : 0;
+  for (int n = 0; n < mine; ++n) {
+    const int d = (first + at * kShare) * kBlock + 16 * b;
+    at = at + 1 == mine ? 0 : at + 1;
+    i32x4 wv[G], hv[NT];
+#pragma unroll
+    for (int g = 0; g < G; ++g) wv[g] = __builtin_nontemporal_load(reinterpret_cast<const words*>(w[g] + d));
+#pragma unroll
+    for (int t = 0; t < NT; ++t) hv[t] = load16(h[t] + d);
+    multiply(wv, hv);
+  }
+  if (tail - 16 * b < a.D && (kShare == 1 || wave == kWaves - 1)) {  // uniform (the last wave has the fewest blocks)
+    i32x4 wv[G], hv[NT];
+#pragma unroll
+    for (int g = 0; g < G; ++g) wv[g] = load16_of(w[g], tail, a.D);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) hv[t] = load16_of(h[t], tail, a.D);
+    multiply(wv, hv);
+  }
+  // acc[g][t][e] of lane (b, i): column 4 g + e, row 4 t + i, piece b of k
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int off = 4; off < kWave; off <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[g][t][e] += __shfl_xor(acc[g][t][e], off, kWave);
+      if (b == g) *reinterpret_cast<i32x4*>(&x[kShare > 1 ? wave : 0][4 * t + i][c0 + 4 * g]) = acc[g][t];
+    }
+  __syncthreads();
+  if constexpr (kShare > 1) {
+    static_assert(4 * NT * PART <= kHeadThreads, "a thread per sum");
+    const int t = threadIdx.x;
+    if (t < 4 * NT * PART) {
+      int* sum = &x[0][0][0] + t;
+#pragma unroll
+      for (int u = 1; u < kShare; ++u) *sum += sum[u * 4 * NT * PART];
+    }
+    __syncthreads();
+  }
+  finish_columns<CAP, PART>(a, &x[0][0][0]);
+}
+
+// Up to 16 RT rows: a wave reads the weights of 16 FC columns straight into the fragments of 16 x 16 x 64 products, 64 bytes of 16
+// rows per load, 256 of each at a time; the hidden states go through LDS, 256 bytes of all rows at a time.
+template <int RT, int FC, bool CAP>
+__global__ __launch_bounds__(kHeadThreads, 3) void int8_few_kernel(Int8Args a) {
+  constexpr int kPart = 64 * FC;  // columns of the workgroup
+  constexpr int kBlock = 256, kStep = 64, kSteps = kBlock / kStep;
+  constexpr int kPitch = kBlock + 16;  // (rows 17 groups of 16 bytes apart: 16 rows' reads lie in 16 different ones of 256 bytes)
+  __shared__ __attribute__((aligned(16))) union {
+    int8_t h[2][16 * RT][kPitch];
+    int x[16 * RT][kPart];
+  } lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const int v0 = blockIdx.x * kPart + wave * 16 * FC;
+  const int8_t* w[FC];
+#pragma unroll
+  for (int f = 0; f < FC; ++f) {
+    const int v = v0 + 16 * f + i;
+    w[f] = a.w + (int64_t)(v < a.V ? v : a.V - 1) * a.w_stride;
+  }
+  // this thread's share of a block of the hidden states: group threadIdx.x % 16 of rows threadIdx.x / 16 + 16 t
+  const int hg = threadIdx.x & 15;
+  const int8_t* h[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int m = 16 * t + (threadIdx.x >> 4);
+    h[t] = a.h + (m < a.T ? m : a.T - 1) * a.h_stride;
+  }
+  i32x4 acc[FC][RT];
+#pragma unroll
+  for (int f = 0; f < FC; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[f][t] = i32x4{0, 0, 0, 0};
+  const int whole = a.D / kBlock, blocks = (a.D + kBlock - 1) / kBlock;
+  int at = whole ? (int)((blockIdx.x * 5) % (unsigned)whole) : 0;  // (where the workgroup begins, see above)
+  i32x4 hv[RT];
+  auto request = [&](int block) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+      hv[t] = block >= whole ? load16_of(h[t], block * kBlock + 16 * hg, a.D) : load16(h[t] + block * kBlock + 16 * hg);
+  };
+  request(whole ? at : 0);
+  for (int n = 0; n < blocks; ++n) {
+    const int block = n < whole ? at : whole;
+    if (n < whole) at = at + 1 == whole ? 0 : at + 1;
+    i32x4 wv[kSteps][FC];
+    const int d = block * kBlock + 16 * g;
+    if (block < whole) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int f = 0; f < FC; ++f) wv[s][f] = load16(w[f] + d + s * kStep);
+    } else {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int f = 0; f < FC; ++f) wv[s][f] = load16_of(w[f], d + s * kStep, a.D);
+    }
+    // (two buffers: what is written here was last read before the barrier of the block before)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<i32x4*>(&lds.h[n & 1][16 * t + (threadIdx.x >> 4)][16 * hg]) = hv[t];
+    __syncthreads();
+    if (n + 1 < blocks) request(n + 1 < whole ? at : whole);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const i32x4 y = *reinterpret_cast<const i32x4*>(&lds.h[n & 1][16 * t + i][16 * g + s * kStep]);
+#pragma unroll
+        for (int f = 0; f < FC; ++f) acc[f][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[s][f], y, acc[f][t], 0, 0, 0);
+      }
+    }
+  }
+  __syncthreads();
+  // acc[f][t][e]: row 16 t + i, column v0 + 16 f + 4 g + e
+#pragma unroll
+  for (int f = 0; f < FC; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<i32x4*>(&lds.x[16 * t + i][wave * 16 * FC + 16 * f + 4 * g]) = acc[f][t];
+  __syncthreads();
+  finish_columns<CAP, kPart>(a, &lds.x[0][0]);
+}
+
+constexpr int kPackThreads = 256;
+__global__ __launch_bounds__(kPackThreads) void int8_pack_kernel(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width,
+                                                                 int64_t rows, int32_t cols) {
+  const int64_t groups = to_width / 16, all = rows * groups;
+  for (int64_t n = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; n < all; n += (int64_t)gridDim.x * kPackThreads) {
+    const int64_t p = n / groups, d = (n - p * groups) * 16;
+    *reinterpret_cast<i32x4*>(to + p * to_width + d) = load16_of(from + p * from_stride, (int)d, cols);
+  }
+}
+
+template <bool CAP>
+hipError_t launch_few(const Int8Args& a, hipStream_t stream) {
+  const dim3 block(kHeadThreads);
+  const auto parts = [&](int columns) { return dim3((unsigned)((a.V + (int64_t)columns - 1) / columns)); };
+  if (a.T <= 8) {
+    const bool share = a.D >= 2048 && a.V < 256 * 96;
+    if (a.T > 4)
+      return share ? launch_kernel(int8_tokens_kernel<2, 32, CAP>, parts(32), block, 0, stream, a)
+                   : launch_kernel(int8_tokens_kernel<2, 128, CAP>, parts(128), block, 0, stream, a);
+    return share ? launch_kernel(int8_tokens_kernel<1, 32, CAP>, parts(32), block, 0, stream, a)
+                 : launch_kernel(int8_tokens_kernel<1, 128, CAP>, parts(128), block, 0, stream, a);
+  }
+  const bool narrow = a.V < 256 * 128;
+  if (a.T <= 16) return narrow ? launch_kernel(int8_few_kernel<1, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<1, 2, CAP>, parts(128), block, 0, stream, a);
+  if (a.T <= 32) return narrow ? launch_kernel(int8_few_kernel<2, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<2, 2, CAP>, parts(128), block, 0, stream, a);
+  if (a.T <= 48) return narrow ? launch_kernel(int8_few_kernel<3, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<3, 2, CAP>, parts(128), block, 0, stream, a);
+  return narrow ? launch_kernel(int8_few_kernel<4, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<4, 2, CAP>, parts(128), block, 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t stream) {
+  if (a.D <= 512) return launch_rows<64, 1>(a, stream);
+  if (a.D <= 1024) return launch_rows<64, 2>(a, stream);
+  if (a.D <= 2048) return launch_rows<64, 4>(a, stream);
+  if (a.D <= 4096) return launch_rows<256, 2>(a, stream);
+  if (a.D <= 8192) return launch_rows<256, 4>(a, stream);
+  if (a.D <= 16384) return launch_rows<1024, 2>(a, stream);
+  if (a.D <= 32768) return launch_rows<1024, 4>(a, stream);
+  return launch_rows<1024, 8>(a, stream);
+}
+
+hipError_t launch_int8_few(const Int8Args& a, hipStream_t stream) {
+  return a.cap != 0.0f ? launch_few<true>(a, stream) : launch_few<false>(a, stream);
+}
+
+hipError_t launch_int8_pack(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width, int64_t rows, int32_t cols,
+                            hipStream_t stream) {
+  const int64_t blocks = (rows * (to_width / 16) + kPackThreads - 1) / kPackThreads;
+  return launch_kernel(int8_pack_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kPackThreads), 0, stream, from, from_stride, to,
+                       to_width, rows, cols);
+}
+
+}  // namespace npd

@@ -1,0 +1,317 @@
+// Layer norm, forward and backward, and its form without a mean (npd_norm.hpp).  A row lies in the registers of TH threads, G groups
+// of eight values each, from its one read to its one write; its sums are taken over what is there (the mean first, then the squares of
+// what is left: the difference of two large sums is never formed).  Bytes bound it.
+#include "../../include/npd.h"
+#include "npd_head_gemm.hpp"
+#include "npd_norm.hpp"
+
+namespace npd {
+namespace {
+
+constexpr int kNormThreads = 256;  // of a workgroup with rows of a wave each
+
+template <int TH>
+constexpr int norm_block() { return TH < kNormThreads ? kNormThreads : TH; }
+
+// sums of N values over the TH threads of a row, in the same order in every thread
+template <int TH, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* smem) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+  if constexpr (TH > kWave) {
+    constexpr int kWaves = TH / kWave;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();  // (the sums before these have been read)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (lane == 0) smem[n * kWaves + wave] = v[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float t = smem[n * kWaves];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) t += smem[n * kWaves + w];
+      v[n] = t;
+    }
+  }
+}
+
+// values [d, d + 8) of a row, those behind its end are left as they are
+__device__ __forceinline__ void store8_of(uint16_t* row, int d, int cols, const float (&v)[8]) {
+  const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  if (d + 8 <= cols) {
+    store8(row + d, w);
+  } else {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (d + t < cols) row[d + t] = (uint16_t)(u[t >> 1] >> (16 * (t & 1)));
+  }
+}
+
+constexpr uint32_t kOnes = 0x3f803f80u;  // two bf16 ones
+
+template <int TH, int G>
+__global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
+  __shared__ float smem[norm_block<TH>() / kWave];
+  constexpr int kRows = norm_block<TH>() / TH;  // a workgroup's at a time
+  const int at = (threadIdx.x % TH) * 8;        // + 8 TH u
+  uint4 w[G], b[G];
+#pragma unroll
+  for (int u = 0; u < G; ++u) {
+    w[u] = a.w ? load8_of(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
+    b[u] = a.b ? load8_of(a.b, at + 8 * TH * u, a.D) : make_uint4(0, 0, 0, 0);
+  }
+  const float per = 1.0f / (float)a.D;
+  for (int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / TH; p < a.T; p += (int64_t)gridDim.x * kRows) {
+    const uint16_t* row = a.x + p * a.x_stride;
+    uint4 x[G];
+#pragma unroll
+    for (int u = 0; u < G; ++u) x[u] = load8_of(row, at + 8 * TH * u, a.D);
+    float mean = 0.0f;
+    if (!a.rms) {
+      float s[1] = {0.0f};
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        float v[8];
+        unpack8(x[u], v);
+        s[0] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+      }
+      row_sums<TH, 1>(s, smem);
+      mean = s[0] * per;
+    }
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      float v[8];
+      unpack8(x[u], v);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const float d = at + 8 * TH * u + t < a.D ? v[t] - mean : 0.0f;
+        s[0] = __builtin_fmaf(d, d, s[0]);
+      }
+    }
+    row_sums<TH, 1>(s, smem);
+    const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
+    if (threadIdx.x % TH == 0) {
+      if (a.mean) a.mean[p] = mean;
+      if (a.rstd) a.rstd[p] = rstd;
+    }
+    uint16_t* out = a.y + p * a.y_stride;
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      float v[8], wv[8], bv[8];
+      unpack8(x[u], v);
+      unpack8(w[u], wv);
+      unpack8(b[u], bv);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v[t] = __builtin_fmaf((v[t] - mean) * rstd, wv[t], bv[t]);
+      store8_of(out, at + 8 * TH * u, a.D, v);
+    }
+  }
+}
+
+// HELD: the workgroup's sums over its rows for the parameters' gradients stay in registers, and go to its piece at the end.
+template <int TH, int G, bool HELD>
+__global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArgs a) {
+  __shared__ float smem[2 * norm_block<TH>() / kWave];
+  __shared__ float joined[HELD && TH == kWave ? 2 * TH * 8 * G : 1];
+  constexpr int kRows = norm_block<TH>() / TH;
+  const int at = (threadIdx.x % TH) * 8;
+  uint4 w[G];
+#pragma unroll
+  for (int u = 0; u < G; ++u) w[u] = a.w ? load8_of(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
+  float dw[HELD ? G : 1][8] = {}, db[HELD ? G : 1][8] = {};
+  const float per = 1.0f / (float)a.D;
+  for (int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / TH; p < a.T; p += (int64_t)gridDim.x * kRows) {
+    const uint16_t *grow = a.g + p * a.g_stride, *xrow = a.x + p * a.x_stride;
+    uint4 g[G], x[G];
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      g[u] = load8_of(grow, at + 8 * TH * u, a.D);  // (0 behind the end: no part in any sum)
+      x[u] = load8_of(xrow, at + 8 * TH * u, a.D);
+    }
+    const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      float gv[8], xv[8], wv[8];
+      unpack8(g[u], gv);
+      unpack8(x[u], xv);
+      unpack8(w[u], wv);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const float n = (xv[t] - mean) * rstd, q = gv[t] * wv[t];
+        s[0] = __builtin_fmaf(q, n, s[0]);
+        s[1] += q;
+        if constexpr (HELD) {
+          dw[u][t] = __builtin_fmaf(gv[t], n, dw[u][t]);
+          db[u][t] += gv[t];
+        }
+      }
+    }
+    if (!a.dx) continue;
+    row_sums<TH, 2>(s, smem);
+    const float along = s[0] * per, flat = a.rms ? 0.0f : s[1] * per;
+    uint16_t* out = a.dx + p * a.dx_stride;
+#pragma unroll
+    for (int u = 0; u < G; ++u) {
+      float gv[8], xv[8], wv[8];
+      unpack8(g[u], gv);
+      unpack8(x[u], xv);
+      unpack8(w[u], wv);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const float n = (xv[t] - mean) * rstd;
+        gv[t] = __builtin_fmaf(-n, along, gv[t] * wv[t] - flat) * rstd;
+      }
+      store8_of(out, at + 8 * TH * u, a.D, gv);
+    }
+  }
+  if constexpr (HELD) {
+    if constexpr (kRows > 1) {
+      // the workgroup's rows one after the other
+      static_assert(TH == kWave, "rows that share a workgroup are a wave each");
+      for (int r = 0; r < kRows; ++r) {
+        if (threadIdx.x / TH == r) {
+#pragma unroll
+          for (int u = 0; u < G; ++u)
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+              const int i = (u * 8 + t) * TH + (threadIdx.x & 63);
+              const float w0 = r ? joined[i] : 0.0f, b0 = r ? joined[G * 8 * TH + i] : 0.0f;
+              dw[u][t] += w0;
+              db[u][t] += b0;
+              joined[i] = dw[u][t];
+              joined[G * 8 * TH + i] = db[u][t];
+            }
+        }
+        __syncthreads();
+      }
+      if (threadIdx.x / TH != kRows - 1) return;
+    }
+    float* pw = a.dw_pieces + (int64_t)blockIdx.x * a.D;
+    float* pb = a.db_pieces + (int64_t)blockIdx.x * a.D;
+#pragma unroll
+    for (int u = 0; u < G; ++u)
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int d = at + 8 * TH * u + t;
+        if (d >= a.D) break;
+        if (a.dw) pw[d] = dw[u][t];
+        if (a.db) pb[d] = db[u][t];
+      }
+  }
+}
+
+// The sums alone, of wide rows: a wave has 512 columns of every fourth row of the workgroup's.
+__global__ __launch_bounds__(kNormThreads) void norm_columns_kernel(NormGradArgs a) {
+  constexpr int kWaves = kNormThreads / kWave;
+  __shared__ float joined[kWaves][2][8][kWave];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * (kWave * 8) + lane * 8;
+  float dw[8] = {}, db[8] = {};
+  for (int64_t p = (int64_t)blockIdx.y * kWaves + wave; p < a.T; p += (int64_t)gridDim.y * kWaves) {
+    float g[8], x[8];
+    unpack8(load8_of(a.g + p * a.g_stride, d, a.D), g);
+    unpack8(load8_of(a.x + p * a.x_stride, d, a.D), x);
+    const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      dw[t] = __builtin_fmaf(g[t], (x[t] - mean) * rstd, dw[t]);
+      db[t] += g[t];
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    joined[wave][0][t][lane] = dw[t];
+    joined[wave][1][t][lane] = db[t];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * kWave * 8; i += kNormThreads) {
+    const int what = i / (kWave * 8), t = i % (kWave * 8) / kWave, l = i % kWave;
+    float s = joined[0][what][t][l];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) s += joined[w][what][t][l];
+    const int e = blockIdx.x * (kWave * 8) + l * 8 + t;
+    float* pieces = what ? a.db_pieces : a.dw_pieces;
+    if (e < a.D && (what ? a.db : a.dw)) pieces[(int64_t)blockIdx.y * a.D + e] = s;
+  }
+}
+
+// Joins the pieces: 64 columns to a workgroup, a wave has every sixteenth piece of them.
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormGradArgs a) {
+  constexpr int kWaves = kJoinThreads / kWave;
+  __shared__ float joined[kWaves][kWave];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * kWave + lane;
+  const bool bias = blockIdx.y == 1 || !a.dw;
+  const float* pieces = bias ? a.db_pieces : a.dw_pieces;
+  float s = 0.0f;
+  if (d < a.D)
+    for (int i = wave; i < a.pieces; i += kWaves) s += pieces[(int64_t)i * a.D + d];
+  joined[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && d < a.D) {
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) s += joined[w][lane];
+    uint16_t* out = bias ? a.db : a.dw;
+    out[d] = one_bf16(a.accumulate ? s + bf16_one(out[d]) : s);
+  }
+}
+
+template <int TH, int G>
+hipError_t launch_rows(const NormArgs& a, hipStream_t stream) {
+  constexpr int kRows = norm_block<TH>() / TH;
+  const int64_t blocks = (a.T + kRows - 1) / kRows;
+  return launch_kernel(norm_kernel<TH, G>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(norm_block<TH>()), 0, stream, a);
+}
+
+template <int TH, int G>
+hipError_t launch_grad(const NormGradArgs& a, hipStream_t stream) {
+  constexpr int kRows = norm_block<TH>() / TH;
+  const int64_t blocks = (a.T + kRows - 1) / kRows;
+  const dim3 block(norm_block<TH>());
+  if constexpr (TH * 8 * G <= kNormHeldWidth) {
+    if (a.dw || a.db) return launch_kernel(norm_grad_kernel<TH, G, true>, dim3((unsigned)a.pieces), block, 0, stream, a);
+  }
+  if (!a.dx) return hipSuccess;
+  return launch_kernel(norm_grad_kernel<TH, G, false>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), block, 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
+  if (a.D <= 512) return launch_rows<64, 1>(a, stream);
+  if (a.D <= 1024) return launch_rows<64, 2>(a, stream);
+  if (a.D <= 2048) return launch_rows<64, 4>(a, stream);
+  if (a.D <= 4096) return launch_rows<256, 2>(a, stream);
+  if (a.D <= 8192) return launch_rows<256, 4>(a, stream);
+  if (a.D <= 16384) return launch_rows<1024, 2>(a, stream);
+  if (a.D <= 32768) return launch_rows<1024, 4>(a, stream);
+  return launch_rows<1024, 8>(a, stream);
+}
+
+int norm_pieces(int64_t T, int32_t D) {
+  const int rows = D <= 2048 ? 4 : D <= kNormHeldWidth ? 1 : 4;  // of a workgroup at a time
+  const int64_t blocks = (T + rows - 1) / rows;
+  return (int)(blocks < kNormPieces ? blocks : kNormPieces);
+}
+
+hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t stream) {
+  const hipError_t e = a.D <= 512     ? launch_grad<64, 1>(a, stream)
+                       : a.D <= 1024  ? launch_grad<64, 2>(a, stream)
+                       : a.D <= 2048  ? launch_grad<64, 4>(a, stream)
+                       : a.D <= 4096  ? launch_grad<256, 2>(a, stream)
+                       : a.D <= 8192  ? launch_grad<256, 4>(a, stream)
+                       : a.D <= 16384 ? launch_grad<1024, 2>(a, stream)
+                       : a.D <= 32768 ? launch_grad<1024, 4>(a, stream)
+                                      : launch_grad<1024, 8>(a, stream);
+  if (e != hipSuccess || !(a.dw || a.db)) return e;
+  if (a.D > kNormHeldWidth) {
+    const hipError_t c = launch_kernel(norm_columns_kernel, dim3((unsigned)(a.D + 511) / 512, (unsigned)a.pieces), dim3(kNormThreads), 0, stream, a);
+    if (c != hipSuccess) return c;
+  }
+  return launch_kernel(norm_join_kernel, dim3((unsigned)(a.D + 63) / 64, a.dw && a.db ? 2 : 1), dim3(kJoinThreads), 0, stream, a);
+}
+
+}  // namespace npd
