@@ -14,6 +14,8 @@
 namespace npd {
 namespace {
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 
 // bf16 bits in the order of their values: 0 and -0 alike, -inf below every number, NaN at either end
@@ -25,8 +27,8 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return bf16_one((uint16_t)(key & 0x8000 ? key & 0x7fff : ~key & 0xffffu));
 }
 
-// counters: 3,968 positive values by magnitude, as many negative ones, zero
-constexpr uint32_t kFirst = (127 - 23) << 7, kValues = 31 << 7;
+// counters: 2 i + sign of the 3,968 magnitudes i, 64 that take what has none, zero
+constexpr uint32_t kFirst = (127 - 23) << 7, kValues = 31 << 7, kOthers = 2 * kValues, kZero = kOthers + kWave;
 constexpr int kEach = 8, kOwners = kValues / kEach;  // a thread has eight values; thread kOwners zero
 static_assert(2 * kOwners + 1 <= kThreads, "");
 
@@ -35,13 +37,20 @@ struct Place {       // where a search over the order ended
   double mass;       // of those above it
 };
 
+struct Choice {
+  uint32_t key, kept, which;  // the token's value, and its place among the entries of that value
+  double logprob;
+};
+
 struct Shared {
-  uint32_t counts[2 * kValues + 1];
+  __attribute__((aligned(16))) uint32_t counts[kZero + 4];
+  double mass_ends[kThreads];
+  uint32_t count_ends[kThreads];
   double masses[2][kWaves];
   uint32_t sums[kWaves];
-  uint32_t big, odd, first;
+  uint32_t big, odd, first, listed;
   int32_t found;
-  Place place;
+  Choice choice;
 };
 
 struct Row {
@@ -50,33 +59,60 @@ struct Row {
   RowSplit split;
 };
 
-// f(id, bits) of the row's entries: groups of eight, kAhead of them requested together, then what is left
-template <class F>
-__device__ __forceinline__ void each_entry(const Row& r, F&& f) {
+// eight(id, bits of eight entries) of the row's aligned groups, kAhead of them requested while as many are looked at, and
+// one(id, bits) of the entries around them
+template <class E, class F>
+__device__ __forceinline__ void each_group(const Row& r, E&& eight, F&& one) {
   constexpr int kAhead = 4;
   const uint4* groups = reinterpret_cast<const uint4*>(r.p + r.split.head);
-  auto eight = [&](int g, const uint4& v) {
-    const int id = r.split.head + 8 * g;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      f(id + 2 * t, w[t] & 0xffff);
-      f(id + 2 * t + 1, w[t] >> 16);
-    }
-  };
+  const int n = r.split.nvec;
   int g = threadIdx.x;
-  for (; g + (kAhead - 1) * kThreads < r.split.nvec; g += kAhead * kThreads) {
-    uint4 v[kAhead];
+  if (g + (kAhead - 1) * kThreads < n) {
+    uint4 next[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = groups[g + u * kThreads];
+    for (int u = 0; u < kAhead; ++u) next[u] = groups[g + u * kThreads];
+#pragma unroll 1
+    for (; g + (kAhead - 1) * kThreads < n; g += kAhead * kThreads) {
+      uint4 v[kAhead];
+      const int after = g + kAhead * kThreads;
+      const bool more = after + (kAhead - 1) * kThreads < n;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) eight(g + u * kThreads, v[u]);
+      for (int u = 0; u < kAhead; ++u) {
+        v[u] = next[u];
+        if (more) next[u] = groups[after + u * kThreads];
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) eight(r.split.head + 8 * (g + u * kThreads), v[u]);
+    }
   }
-  for (; g < r.split.nvec; g += kThreads) eight(g, groups[g]);
-  for (int j = threadIdx.x; j < r.V - 8 * r.split.nvec; j += kThreads) {
+  uint4 v[kAhead - 1];
+#pragma unroll
+  for (int u = 0; u < kAhead - 1; ++u)
+    if (g + u * kThreads < n) v[u] = groups[g + u * kThreads];
+#pragma unroll
+  for (int u = 0; u < kAhead - 1; ++u)
+    if (g + u * kThreads < n) eight(r.split.head + 8 * (g + u * kThreads), v[u]);
+#pragma unroll 1
+  for (int j = threadIdx.x; j < r.V - 8 * n; j += kThreads) {
     const int id = r.split.edge_elem(j);
-    f(id, (uint32_t)r.p[id]);
+    one(id, (uint32_t)r.p[id]);
   }
+}
+
+// f(id, bits) of the row's entries
+template <class F>
+__device__ __forceinline__ void each_entry(const Row& r, F&& f) {
+  each_group(
+      r,
+      [&](int id, const uint4& v) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          f(id + 2 * t, w[t] & 0xffff);
+          f(id + 2 * t + 1, w[t] >> 16);
+        }
+      },
+      f);
 }
 
 // in wave order, so that every thread has the same sum
@@ -100,8 +136,9 @@ __device__ __forceinline__ uint32_t block_count(uint32_t v, uint32_t* smem) {
   return s;
 }
 
-__device__ __forceinline__ double weight_of(uint32_t key, double top, double tau) {
-  return exp(((double)value_of(key) - top) / tau);
+// `per`: 1 / tau.  (Not inlined: the coefficients of the exponential, two registers each, would be kept from one row to the next.)
+__device__ __attribute__((noinline)) double weight_of(uint32_t key, double top, double per) {
+  return exp(((double)value_of(key) - top) * per);
 }
 
 enum Find { kCount, kMassReaches, kMassExceeds };
@@ -111,27 +148,27 @@ struct Passes {
   const Row& row;
   Shared& s;
   uint32_t top_key, all;
-  double top, tau, sum;
-  __device__ __forceinline__ void from(uint32_t key, double at_tau, uint32_t* count, double* mass) const {
+  double top, per, sum;
+  __device__ __forceinline__ void from(uint32_t key, double at, uint32_t* count, double* mass) const {
     uint32_t n = 0;
     double m = 0.0;
     each_entry(row, [&](int, uint32_t b) {
       const uint32_t k = key_of(b);
       if (k < key || k < kLowest) return;
       ++n;
-      m += weight_of(k, top, at_tau);
+      m += weight_of(k, top, at);
     });
     *count = block_count(n, s.sums);
     *mass = block_sum64(m, s.masses[0]);
   }
-  __device__ __forceinline__ void begin(double at_tau) {
-    tau = at_tau;
-    from(kLowest, tau, &all, &sum);
+  __device__ __forceinline__ void begin(double at) {
+    per = at;
+    from(kLowest, per, &all, &sum);
   }
-  __device__ __forceinline__ double sum_at(double at_tau) const {
+  __device__ __forceinline__ double sum_at(double at) const {
     uint32_t n;
     double m;
-    from(kLowest, at_tau, &n, &m);
+    from(kLowest, at, &n, &m);
     return m;
   }
   // how many weigh `least` and more
@@ -139,7 +176,7 @@ struct Passes {
     uint32_t n = 0;
     each_entry(row, [&](int, uint32_t b) {
       const uint32_t k = key_of(b);
-      n += k >= kLowest && weight_of(k, top, tau) >= least;
+      n += k >= kLowest && weight_of(k, top, per) >= least;
     });
     return block_count(n, s.sums);
   }
@@ -151,7 +188,7 @@ struct Passes {
       const uint32_t mid = (lo + hi) / 2;
       uint32_t n;
       double m;
-      from(mid, tau, &n, &m);
+      from(mid, per, &n, &m);
       const bool enough = what == kCount ? n >= count : what == kMassReaches ? m >= mass : m > mass;
       if (enough) {
         lo = mid;
@@ -166,146 +203,145 @@ struct Passes {
   }
 };
 
-// A row whose entries are counted: the values' counts and masses are in registers, eight values to a thread, in their order.
+// A row whose entries are counted.  Stretches of eight values, in their order, were weighed by a thread each (weigh()), and what there
+// is up to the end of each stretch is in LDS; one wave searches there.
 struct Counted {
   Shared& s;
   uint32_t top_key, all;
-  double top, tau, sum;
-  uint32_t n[kEach], before, after;  // of the thread's first and behind its last value
-  double m[kEach], mass_before, mass_after;
+  double top, per, sum;
 
-  static __device__ __forceinline__ uint32_t key(int e) {
-    const int t = threadIdx.x;
+  static __device__ __forceinline__ uint32_t key(int t, int e) {
     if (t < kOwners) return 0x8000u + kFirst + kValues - 1 - (uint32_t)(t * kEach + e);
     if (t == kOwners) return 0x8000u;
     return ~(0x8000u + kFirst + (uint32_t)((t - kOwners - 1) * kEach + e)) & 0xffffu;
   }
-  __device__ __forceinline__ void read() {
-    const int t = threadIdx.x;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      n[e] = 0;
-      if (t < kOwners) n[e] = s.counts[kValues - 1 - (t * kEach + e)];
-      if (t == kOwners && e == 0) n[e] = s.counts[2 * kValues];
-      if (t > kOwners && t <= 2 * kOwners) n[e] = s.counts[kValues + (t - kOwners - 1) * kEach + e];
-    }
-    // the first thread that has any has the largest
-    uint32_t mine = 0;
-#pragma unroll
-    for (int e = kEach - 1; e >= 0; --e)
-      if (n[e]) mine = key(e);
-    const uint64_t any = __ballot(mine != 0);
-    __syncthreads();
-    if ((t & 63) == 0) s.sums[t >> 6] = 0;
-    if (any && (t & 63) == __builtin_ctzll(any)) s.sums[t >> 6] = mine;
-    __syncthreads();
-    top_key = 0;
-    for (int w = kWaves - 1; w >= 0; --w)
-      if (s.sums[w]) top_key = s.sums[w];
-    top = top_key ? value_of(top_key) : 0.0;
-    __syncthreads();
+  static __device__ __forceinline__ uint32_t count_of(const Shared& s, int t, int e) {
+    if (t < kOwners) return s.counts[2 * (kValues - 1 - (t * kEach + e))];
+    if (t == kOwners) return e == 0 ? s.counts[kZero] : 0;
+    return t <= 2 * kOwners ? s.counts[2 * ((t - kOwners - 1) * kEach + e) + 1] : 0;
   }
-  __device__ __forceinline__ double sum_at(double at_tau) const {
-    double mine = 0.0;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (n[e]) mine += n[e] * weight_of(key(e), top, at_tau);
-    return block_sum64(mine, s.masses[0]);
+  // the first stretch for which `is` holds (it holds for those behind it too), all threads of the wave
+  template <class F>
+  static __device__ __forceinline__ int first_stretch(F&& is) {
+    const int lane = threadIdx.x & 63;
+    constexpr int kPer = kThreads / kWave;
+    const uint64_t ends = __ballot(is(lane * kPer + kPer - 1));
+    const int group = ends ? __builtin_ctzll(ends) : kWave - 1;
+    const uint64_t in = __ballot(is(group * kPer + (lane < kPer ? lane : kPer - 1)));
+    return group * kPer + (in ? __builtin_ctzll(in) : kPer - 1);
   }
-  // cumulative counts and masses; a thread's end is the next one's beginning, bit by bit
-  __device__ __forceinline__ void begin(double at_tau) {
-    tau = at_tau;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t c = 0;
-    double w = 0.0;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      m[e] = n[e] ? n[e] * weight_of(key(e), top, tau) : 0.0;
-      c += n[e];
-      w += m[e];
-    }
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      const uint32_t c2 = __shfl_up(c, off, kWave);
-      const double w2 = __shfl_up(w, off, kWave);
-      if (lane >= off) {
-        c += c2;
-        w = w2 + w;
-      }
-    }
-    __syncthreads();
-    if (lane == 63) {
-      s.sums[wave] = c;
-      s.masses[0][wave] = w;
-    }
-    __syncthreads();
-    uint32_t c0 = 0;
-    double w0 = 0.0;
-    before = 0;
-    mass_before = 0.0;
-    for (int i = 0; i < kWaves; ++i) {
-      if (i == wave) {
-        before = c0;
-        mass_before = w0;
-      }
-      c0 += s.sums[i];
-      w0 += s.masses[0][i];
-    }
-    all = c0;
-    sum = w0;
-    const uint32_t c1 = __shfl_up(c, 1, kWave);
-    const double w1 = __shfl_up(w, 1, kWave);
-    after = before + c;
-    mass_after = mass_before + w;
-    if (lane > 0) {
-      before += c1;
-      mass_before += w1;
-    }
-    __syncthreads();
-  }
+  // how many weigh `least` and more (weights fall along the order whether a value occurs or not)
   __device__ __forceinline__ uint32_t at_least(double least) const {
-    uint32_t mine = 0;
+    const int t = first_stretch([&](int t) { return t > 2 * kOwners || weight_of(key(t, t == kOwners ? 0 : kEach - 1), top, per) < least; });
+    uint32_t n = t ? s.count_ends[t - 1] : 0;
+    if (t > 2 * kOwners) return n;
+    const int e = threadIdx.x & (kEach - 1);
+    const uint32_t here = count_of(s, t, e);
+    const uint32_t mine = here && weight_of(key(t, e), top, per) >= least ? here : 0;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (n[e] && weight_of(key(e), top, tau) >= least) mine += n[e];
-    return block_count(mine, s.sums);
+    for (int i = 0; i < kEach; ++i) n += __shfl(mine, i, kWave);
+    return n;
   }
   // (there is enough: what is asked for is at most what there is; the last value there is takes what rounding leaves over)
-  __device__ __forceinline__ Place find(Find what, uint32_t count, double mass) const {
-    if (threadIdx.x == 0) s.first = kThreads;
-    __syncthreads();
-    const bool enough = what == kCount ? after >= count : what == kMassReaches ? mass_after >= mass : mass_after > mass;
-    const bool last = after == all;  // the thread of the lowest value, and those behind it
-    if (after != before && (enough || last)) atomicMin(&s.first, threadIdx.x);
-    __syncthreads();
-    if (threadIdx.x == s.first) {
-      uint32_t c = before;
-      double w = mass_before;
-      Place p{};
+  __device__ __forceinline__ Place find(Find what, uint32_t target, double mass) const {
+    const int t = first_stretch([&](int t) {
+      const uint32_t c = s.count_ends[t];
+      if (what == kCount) return c >= target;
+      const double w = s.mass_ends[t];
+      return c == all || (c > 0 && (what == kMassReaches ? w >= mass : w > mass));
+    });
+    const int e = threadIdx.x & (kEach - 1);
+    const uint32_t n = count_of(s, t, e);
+    const double m = n ? n * weight_of(key(t, e), top, per) : 0.0;
+    uint32_t c = t ? s.count_ends[t - 1] : 0;
+    double w = t ? s.mass_ends[t - 1] : 0.0;
+    Place p{};
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const bool done = p.here && (what == kCount ? c >= count : what == kMassReaches ? w >= mass : w > mass);
-        // (what rounding leaves over is not an entry's of weight 0)
-        if (!done && n[e] && (what == kCount || !p.here || m[e] > 0.0)) p = Place{key(e), c, n[e], w};
-        c += n[e];
-        w += m[e];
-      }
-      s.place = p;
+    for (int i = 0; i < kEach; ++i) {
+      const uint32_t ni = __shfl(n, i, kWave);
+      const double mi = __shfl(m, i, kWave);
+      const bool done = p.here && (what == kCount ? c >= target : what == kMassReaches ? w >= mass : w > mass);
+      // (what rounding leaves over is not an entry's of weight 0)
+      if (!done && ni && (what == kCount || !p.here || mi > 0.0)) p = Place{key(t, i), c, ni, w};
+      c += ni;
+      w += mi;
     }
-    __syncthreads();
-    return s.place;
+    return p;
   }
 };
+
+// the largest value that is counted (0: none), all threads
+__device__ __forceinline__ uint32_t largest_counted(Shared& s) {
+  const int t = threadIdx.x;
+  uint32_t mine = 0;
+#pragma unroll
+  for (int e = kEach - 1; e >= 0; --e)
+    if (Counted::count_of(s, t, e)) mine = Counted::key(t, e);
+  const uint64_t any = __ballot(mine != 0);
+  if (any ? (t & 63) == __builtin_ctzll(any) : (t & 63) == 0) s.sums[t >> 6] = mine;
+  __syncthreads();
+  uint32_t top = 0;
+  for (int w = kWaves - 1; w >= 0; --w)
+    if (s.sums[w]) top = s.sums[w];
+  return top;
+}
+
+// Weighs the stretches, all threads: what there is up to the end of each, and the sum at temperature 1.  (Ends rise: a stretch's is the
+// sum over its wave so far, added to the waves' before.)
+__device__ __forceinline__ void weigh(Shared& s, double top, double per, bool nll, double* sum1) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t c = 0;
+  double w = 0.0, w1 = 0.0;
+  const bool both = nll && per != 1.0;
+#pragma unroll 1
+  for (int e = 0; e < kEach; ++e) {
+    const uint32_t n = Counted::count_of(s, threadIdx.x, e);
+    if (n) {
+      const uint32_t key = Counted::key(threadIdx.x, e);
+      w += n * weight_of(key, top, per);
+      if (both) w1 += n * weight_of(key, top, 1.0);
+    }
+    c += n;
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const uint32_t c2 = __shfl_up(c, off, kWave);
+    const double w2 = __shfl_up(w, off, kWave);
+    if (lane >= off) {
+      c += c2;
+      w = w2 + w;
+    }
+    if (both) w1 += __shfl_xor(w1, off, kWave);
+  }
+  __syncthreads();  // (largest_counted()'s sums have been read)
+  if (lane == 63) {
+    s.sums[wave] = c;
+    s.masses[0][wave] = w;
+    s.masses[1][wave] = w1;
+  }
+  __syncthreads();
+  uint32_t c0 = 0;
+  double w0 = 0.0, all1 = 0.0, all = 0.0;
+  for (int i = 0; i < kWaves; ++i) {
+    if (i == wave) {
+      c0 += c;
+      w0 = all + w;
+    } else if (i < wave) {
+      c0 += s.sums[i];
+    }
+    all += s.masses[0][i];
+    all1 += s.masses[1][i];
+  }
+  s.count_ends[threadIdx.x] = c0;
+  s.mass_ends[threadIdx.x] = w0;
+  *sum1 = both ? all1 : all;
+  __syncthreads();
+}
 
 // The settings of a row.
 struct Settings {
-  double tau, top_p, min_p, u;
+  double tau, per, top_p, min_p, u;  // per: 1 / tau
   uint32_t top_k;
-};
-
-struct Choice {
-  uint32_t key, kept, which;  // the token's value, and its place among the entries of that value
-  double logprob;
 };
 
 template <class Entries>
@@ -320,14 +356,14 @@ __device__ __forceinline__ Choice choose(const Entries& x, const Settings& q, bo
       return;
     }
     end = x.find(kCount, n, 0.0);
-    sum = end.mass + (double)(n - end.before) * weight_of(end.key, x.top, x.tau);
+    sum = end.mass + (double)(n - end.before) * weight_of(end.key, x.top, x.per);
   };
   cut();
   const uint32_t by_k = n;
   if (q.top_p < 1.0 && n > 1) {
     const double enough = q.top_p * sum;
     const Place p = x.find(kMassReaches, 0, enough);
-    const double more = ceil((enough - p.mass) / weight_of(p.key, x.top, x.tau));
+    const double more = ceil((enough - p.mass) / weight_of(p.key, x.top, x.per));
     const uint32_t here = more < 1.0 ? 1 : more < (double)p.here ? (uint32_t)more : p.here;
     if (p.before + here < n) n = p.before + here;
   }
@@ -344,27 +380,66 @@ __device__ __forceinline__ Choice choose(const Entries& x, const Settings& q, bo
     if (p.before >= end.before) p = end;  // (no further than the last one that is kept)
     if (p.key == end.key) here = n - end.before;
   }
-  const double steps = floor((at - p.mass) / weight_of(p.key, x.top, x.tau));
+  const double steps = floor((at - p.mass) / weight_of(p.key, x.top, x.per));
   const uint32_t which = !(steps > 0.0) ? 0 : steps < (double)here ? (uint32_t)steps : here - 1;
-  return Choice{p.key, n, which, ((double)value_of(p.key) - x.top) / x.tau - log(sum)};
+  return Choice{p.key, n, which, ((double)value_of(p.key) - x.top) * x.per - log(sum)};
 }
 
-// id of the entry `which` (in order of ids) of those of a value
+// id of the entry `which` (in order of ids) of those of a value: their ids go into a list where the counters were
 __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t which, Shared& s) {
-  if (threadIdx.x == 0) s.found = 0x7fffffff;
+  constexpr uint32_t kList = sizeof(s.counts) / sizeof(s.counts[0]);
   __syncthreads();
-  if (which == 0) {
-    each_entry(row, [&](int id, uint32_t b) {
-      if (key_of(b) == key) atomicMin(&s.found, id);
-    });
+  if (threadIdx.x == 0) {
+    s.found = 0x7fffffff;
+    s.listed = 0;
+  }
+  __syncthreads();
+  const uint32_t bits = key == 0x8000 ? 0 : key & 0x8000 ? key & 0x7fff : ~key & 0xffff, mask = bits ? 0xffff : 0x7fff;  // (-0 is 0)
+  auto one = [&](int id, uint32_t b) {
+    if ((b & mask) != bits) return;
+    if (which == 0) {
+      atomicMin(&s.found, id);
+    } else {
+      const uint32_t n = atomicAdd(&s.listed, 1u);
+      if (n < kList) s.counts[n] = (uint32_t)id;
+    }
+  };
+  const uint32_t bits2 = bits * 0x10001u, mask2 = mask * 0x10001u;
+  each_group(
+      row,
+      [&](int id, const uint4& v) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        u16x2 d[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) d[t] = __builtin_bit_cast(u16x2, (w[t] & mask2) ^ bits2);
+        const u16x2 least = __builtin_elementwise_min(__builtin_elementwise_min(d[0], d[1]), __builtin_elementwise_min(d[2], d[3]));
+        if (least[0] != 0 && least[1] != 0) return;
+#pragma unroll 1
+        for (int t = 0; t < 8; ++t) {
+          const uint32_t two = t < 4 ? (t < 2 ? w[0] : w[1]) : (t < 6 ? w[2] : w[3]);
+          one(id + t, t & 1 ? two >> 16 : two & 0xffff);
+        }
+      },
+      one);
+  __syncthreads();
+  if (which == 0) return s.found;
+  if (s.listed <= kThreads) {
+    const uint32_t n = s.listed;
+    if (threadIdx.x < n) {
+      const uint32_t mine = s.counts[threadIdx.x];
+      uint32_t below = 0;
+      for (uint32_t i = 0; i < n; ++i) below += s.counts[i] < mine;
+      if (below == which) s.found = (int32_t)mine;
+    }
     __syncthreads();
     return s.found;
   }
-  // every wave counts in a stretch of its own, and the one that has it looks again
+  // very many of them: every wave counts in a stretch of its own, and the one that has it looks again
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int each = ((row.V + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
   const int begin = wave * each < row.V ? wave * each : row.V, end = row.V - begin < each ? row.V : begin + each;
   uint32_t n = 0;
+#pragma unroll 8
   for (int i = begin + lane; i < end; i += kWave) n += key_of(row.p[i]) == key;
   n = (uint32_t)wave_sum_int((int)n);
   if (lane == 0) s.sums[wave] = n;
@@ -409,94 +484,134 @@ __device__ __attribute__((noinline)) bool by_passes(const Row row, const Setting
   __syncthreads();
   if (bad || most < kLowest) return false;
   Passes passes{row, s, most, 0, value_of(most), 0.0, 0.0};
-  passes.begin(q.tau);
+  passes.begin(q.per);
   *c = choose(passes, q, greedy);
   *sum1 = !nll ? 1.0 : q.tau == 1.0 ? passes.sum : passes.sum_at(1.0);
   *top = passes.top;
   return true;
 }
 
+// (a workgroup has one row: in a loop over rows what only threadIdx decides would be kept in registers from one to the next)
+constexpr int64_t kGrid = 65536;  // workgroups along x
 __global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
   __shared__ Shared s;
-  for (int64_t r = blockIdx.x; r < a.T; r += gridDim.x) {
-    auto put = [&](int token, double logprob, double nll, uint32_t kept, int status) {
-      if (threadIdx.x != 0) return;
-      a.token[r] = token;
-      if (a.logprob) a.logprob[r] = (float)logprob;
-      if (a.nll) a.nll[r] = (float)nll;
-      if (a.kept) a.kept[r] = (int32_t)kept;
-      if (status && a.status) atomicOr(a.status, status);
-    };
-    const double nan = __builtin_nan("");
-    if (a.mask && !a.mask[r]) {
-      put(-1, 0.0, 0.0, 0, 0);
-      continue;
-    }
-    const float tau = a.taus ? a.taus[r] : a.tau, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p;
-    const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
-    const float u = a.u[r];
-    if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
-        !(u >= 0.0f && u < 1.0f)) {
-      put(-1, nan, nan, 0, NPD_DEV_BAD_SAMPLING);
-      continue;
-    }
-    const bool greedy = tau == 0.0f;
-    const Settings q = {greedy ? 1.0 : (double)tau, top_p, min_p, u, (uint32_t)top_k};
-    const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
-
-    for (int i = threadIdx.x; i < (int)(2 * kValues + 1); i += kThreads) s.counts[i] = 0;
-    if (threadIdx.x == 0) s.big = s.odd = 0;
-    __syncthreads();
-    uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
-    each_entry(row, [&](int, uint32_t b) {
-      const uint32_t size = b & 0x7fff, i = size - kFirst;
-      if (i < kValues) {
-        atomicAdd(&s.counts[i + (b >> 15) * kValues], 1u);
-      } else if (size == 0) {
-        atomicAdd(&s.counts[2 * kValues], 1u);
-      } else if (b != 0xff80) {
-        if (b >= 0x8000 + kFirst + kValues && b < 0xff80)
-          ++big;
-        else
-          odd = 1;
-      }
-    });
-    if (big) atomicAdd(&s.big, big);
-    if (odd) s.odd = 1;
-    __syncthreads();
-    big = s.big;
-    odd = s.odd;
-    Choice c;
-    double sum1 = 1.0, top;  // of the weights at temperature 1
-    Counted counted{s};
-    counted.read();
-    // Numbers below -256 have no weight that 64 bits would show beside the largest's (2^-90 times at most 2^26 of them) where that is
-    // 64 temperatures above -256, and are none that a min-p would keep.
-    const double room = counted.top + 256.0;
-    const bool apart = room >= 64.0 && room >= 64.0 * q.tau && (q.min_p == 0.0 || room > q.tau * (1.0 - log(q.min_p)));
-    if (!odd && counted.top_key && (!big || apart)) {
-      counted.begin(q.tau);
-      c = choose(counted, q, greedy);
-      // those that are kept if nothing is cut off
-      if (c.kept == counted.all && big) c.kept = !greedy && q.min_p == 0.0 && q.top_p == 1.0 ? (q.top_k > 0 && q.top_k < counted.all + big ? q.top_k : counted.all + big) : c.kept;
-      if (a.nll) sum1 = q.tau == 1.0 ? counted.sum : counted.sum_at(1.0);
-      top = counted.top;
-    } else {
-      if (!by_passes(row, q, greedy, a.nll != nullptr, s, &c, &sum1, &top)) {
-        put(-1, nan, nan, 0, NPD_DEV_BAD_LOGITS);
-        continue;
-      }
-    }
-    const int token = find_entry(row, c.key, c.which, s);
-    put(token, c.logprob, log(sum1) + (top - (double)value_of(c.key)), c.kept, 0);
-    __syncthreads();
+  const int64_t r = (int64_t)blockIdx.y * kGrid + blockIdx.x;
+  if (r >= a.T) return;
+  auto put = [&](int token, double logprob, double nll, uint32_t kept, int status) {
+    if (threadIdx.x != 0) return;
+    a.token[r] = token;
+    if (a.logprob) a.logprob[r] = (float)logprob;
+    if (a.nll) a.nll[r] = (float)nll;
+    if (a.kept) a.kept[r] = (int32_t)kept;
+    if (status && a.status) atomicOr(a.status, status);
+  };
+  const double nan = __builtin_nan("");
+  if (a.mask && !a.mask[r]) {
+    put(-1, 0.0, 0.0, 0, 0);
+    return;
   }
+  const float tau = a.taus ? a.taus[r] : a.tau, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p;
+  const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+  const float u = a.u[r];
+  if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
+      !(u >= 0.0f && u < 1.0f)) {
+    put(-1, nan, nan, 0, NPD_DEV_BAD_SAMPLING);
+    return;
+  }
+  const bool greedy = tau == 0.0f;
+  const double t = greedy ? 1.0 : (double)tau;
+  const Settings q = {t, 1.0 / t, top_p, min_p, u, (uint32_t)top_k};
+  const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
+
+  for (int i = threadIdx.x; i < (int)(sizeof(s.counts) / 16); i += kThreads) reinterpret_cast<uint4*>(s.counts)[i] = make_uint4(0, 0, 0, 0);
+  if (threadIdx.x == 0) s.big = s.odd = 0;
+  __syncthreads();
+  uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
+  auto other = [&](uint32_t b) {
+    const uint32_t size = b & 0x7fff;
+    if (size == 0)
+      atomicAdd(&s.counts[kZero], 1u);
+    else if (size - kFirst >= kValues && b != 0xff80) {
+      if (b >= 0x8000 + kFirst + kValues && b < 0xff80)
+        ++big;
+      else
+        odd = 1;
+    }
+  };
+  // A counter's number is the entry with its sign in the lowest place, less the first one's.  What is no counter's goes to
+  // the lane's own among `kOthers` (a branch around every addition takes twice the time) and is looked at afterwards.
+  const uint32_t own = kOthers + (threadIdx.x & 63);
+  each_group(
+      row,
+      [&](int, const uint4& v) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t most = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t turned = (w[t] << 1 & 0xfffefffe) | (w[t] >> 15 & 0x00010001);
+          const u16x2 at = __builtin_bit_cast(u16x2, turned) - u16x2{(unsigned short)(2 * kFirst), (unsigned short)(2 * kFirst)};
+          const uint32_t lo = at[0], hi = at[1];
+          most = most > lo ? most : lo;
+          most = most > hi ? most : hi;
+          atomicAdd(&s.counts[lo < own ? lo : own], 1u);
+          atomicAdd(&s.counts[hi < own ? hi : own], 1u);
+        }
+        if (most < kOthers) return;
+#pragma unroll 1
+        for (int t = 0; t < 8; ++t) {
+          const uint32_t two = t < 4 ? (t < 2 ? w[0] : w[1]) : (t < 6 ? w[2] : w[3]);
+          other(t & 1 ? two >> 16 : two & 0xffff);
+        }
+      },
+      [&](int, uint32_t b) {
+        const uint32_t i = (b & 0x7fff) - kFirst;
+        if (i < kValues)
+          atomicAdd(&s.counts[2 * i + (b >> 15)], 1u);
+        else
+          other(b);
+      });
+  if (big) atomicAdd(&s.big, big);
+  if (odd) s.odd = 1;
+  __syncthreads();
+  big = s.big;
+  odd = s.odd;
+  Choice c;
+  double sum1 = 1.0, top;  // of the weights at temperature 1
+  const uint32_t top_key = largest_counted(s);
+  const double counted_top = top_key ? value_of(top_key) : 0.0;
+  // Numbers below -256 have no weight that 64 bits would show beside the largest's (2^-90 times at most 2^26 of them) where that is
+  // 64 temperatures above -256, and are none that a min-p would keep.
+  const double room = counted_top + 256.0;
+  const bool apart = room >= 64.0 && room >= 64.0 * q.tau && (q.min_p == 0.0 || room > q.tau * (1.0 - log(q.min_p)));
+  if (!odd && top_key && (!big || apart)) {
+    weigh(s, counted_top, q.per, a.nll != nullptr, &sum1);
+    if (threadIdx.x < kWave) {
+      const Counted counted{s, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
+      Choice mine = choose(counted, q, greedy);
+      if (mine.kept == counted.all && big && !greedy && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
+        const uint32_t all = counted.all + big;
+        mine.kept = q.top_k > 0 && q.top_k < all ? q.top_k : all;
+      }
+      if (threadIdx.x == 0) s.choice = mine;
+    }
+    __syncthreads();
+    c = s.choice;
+    top = counted_top;
+  } else {
+    if (!by_passes(row, q, greedy, a.nll != nullptr, s, &c, &sum1, &top)) {
+      put(-1, nan, nan, 0, NPD_DEV_BAD_LOGITS);
+      return;
+    }
+  }
+  const int token = find_entry(row, c.key, c.which, s);
+  put(token, c.logprob, log(sum1) + (top - (double)value_of(c.key)), c.kept, 0);
 }
 
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
-  return launch_kernel(sample_kernel, dim3((unsigned)(a.T < 65536 ? a.T : 65536)), dim3(kThreads), 0, stream, a);
+  const int64_t rows = a.T < kGrid ? a.T : kGrid;
+  return launch_kernel(sample_kernel, dim3((unsigned)rows, (unsigned)((a.T + kGrid - 1) / kGrid)), dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace npd
