@@ -5,8 +5,8 @@
 // bits of the sums where many entries are alike, so they are 64-bit.  That is cheap because bf16 has few values: a row's entries are
 // counted by value (whole numbers in LDS, exact in any order), and every value that occurs is weighed once, times its count.
 //
-// The 7,937 values of magnitude 2^-23 .. 2^8 and zero have a counter each; a row with an entry outside of them that may matter is
-// done by bisection over the values instead, with a pass over the row for each step.
+// The 7,936 values of magnitude 2^-23 .. 2^8 and zero have a counter each, up to 255 entries closer to zero are listed; a row with
+// more of those, or an entry beyond 2^8 that may matter, is done by bisection over the values, with a pass over the row for each step.
 #include "../../include/npd.h"
 #include "npd_device.hpp"
 #include "npd_sample.hpp"
@@ -18,6 +18,14 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 
+// threadIdx.x, of which the compiler keeps nothing from one phase of a row to the next (places and keys of eight values, spilled to
+// memory over the whole row, took longer than the phases)
+__device__ __forceinline__ int thread_of_phase() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 // bf16 bits in the order of their values: 0 and -0 alike, -inf below every number, NaN at either end
 constexpr uint32_t kLowest = 0x80, kInfinity = 0xff80;  // keys of the lowest number and of +inf
 __device__ __forceinline__ uint32_t key_of(uint32_t b) {
@@ -27,14 +35,18 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return bf16_one((uint16_t)(key & 0x8000 ? key & 0x7fff : ~key & 0xffffu));
 }
 
-// counters: 2 i + sign of the 3,968 magnitudes i, 64 that take what has none, zero
-constexpr uint32_t kFirst = (127 - 23) << 7, kValues = 31 << 7, kOthers = 2 * kValues, kZero = kOthers + kWave;
-constexpr int kEach = 8, kOwners = kValues / kEach;  // a thread has eight values; thread kOwners zero
-static_assert(2 * kOwners + 1 <= kThreads, "");
+// counters: 2 i + sign of the 3,968 magnitudes i, 64 that take what has none
+constexpr uint32_t kFirst = (127 - 23) << 7, kValues = 31 << 7, kOthers = 2 * kValues;
+constexpr int kTable = 64;  // of the exponential
+// a thread has eight values: the positive ones, what is close to zero, the negative ones
+constexpr int kEach = 8, kOwners = kValues / kEach, kNear = 256;
+static_assert(2 * kOwners + kNear / kEach == kThreads, "");
+constexpr uint32_t kBelowNear = 0x8000 - kFirst;  // key below those of what is close to zero
 
 struct Place {       // where a search over the order ended
   uint32_t key, before, here;  // the value; entries above it, entries of it
   double mass;       // of those above it
+  double weight;     // of one of them
 };
 
 struct Choice {
@@ -43,13 +55,16 @@ struct Choice {
 };
 
 struct Shared {
-  __attribute__((aligned(16))) uint32_t counts[kZero + 4];
+  __attribute__((aligned(16))) uint32_t counts[kOthers + kWave];
   double mass_ends[kThreads];
+  double table[kTable];
   uint32_t count_ends[kThreads];
   double masses[2][kWaves];
+  uint32_t near_list[kNear], near_keys[kNear], near_counts[kNear];  // as they came; in order, and how many have that value
   uint32_t sums[kWaves];
-  uint32_t big, odd, first, listed;
+  uint32_t big, odd, near, first, listed;
   int32_t found;
+  double log1;
   Choice choice;
 };
 
@@ -59,41 +74,35 @@ struct Row {
   RowSplit split;
 };
 
-// eight(id, bits of eight entries) of the row's aligned groups, kAhead of them requested while as many are looked at, and
-// one(id, bits) of the entries around them
+// eight(id, bits of eight entries) of the row's aligned groups, the next kAhead of them always requested, and one(id, bits) of the
+// entries around them.  (No load is behind a branch: the compiler would wait for all of them where paths meet.  Those behind the
+// row's end read its last group again.)
+constexpr int kAhead = 6;
 template <class E, class F>
 __device__ __forceinline__ void each_group(const Row& r, E&& eight, F&& one) {
-  constexpr int kAhead = 4;
-  const uint4* groups = reinterpret_cast<const uint4*>(r.p + r.split.head);
-  const int n = r.split.nvec;
-  int g = threadIdx.x;
-  if (g + (kAhead - 1) * kThreads < n) {
-    uint4 next[kAhead];
+  const int n = r.split.nvec, t = thread_of_phase();
+  if (n > 0) {
+    const uint4* groups = reinterpret_cast<const uint4*>(r.p + r.split.head);
+    auto load = [&](int g) { return groups[g < n ? g : n - 1]; };
+    uint4 v[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) next[u] = groups[g + u * kThreads];
+    for (int u = 0; u < kAhead; ++u) v[u] = load(t + u * kThreads);
+    int g = 0;
 #pragma unroll 1
-    for (; g + (kAhead - 1) * kThreads < n; g += kAhead * kThreads) {
-      uint4 v[kAhead];
-      const int after = g + kAhead * kThreads;
-      const bool more = after + (kAhead - 1) * kThreads < n;
+    for (; g + kAhead * kThreads <= n; g += kAhead * kThreads) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        v[u] = next[u];
-        if (more) next[u] = groups[after + u * kThreads];
+        const uint4 now = v[u];
+        v[u] = load(g + t + (u + kAhead) * kThreads);
+        eight(r.split.head + 8 * (g + t + u * kThreads), now);
       }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) eight(r.split.head + 8 * (g + u * kThreads), v[u]);
     }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (g + t + u * kThreads < n) eight(r.split.head + 8 * (g + t + u * kThreads), v[u]);
   }
-  uint4 v[kAhead - 1];
-#pragma unroll
-  for (int u = 0; u < kAhead - 1; ++u)
-    if (g + u * kThreads < n) v[u] = groups[g + u * kThreads];
-#pragma unroll
-  for (int u = 0; u < kAhead - 1; ++u)
-    if (g + u * kThreads < n) eight(r.split.head + 8 * (g + u * kThreads), v[u]);
 #pragma unroll 1
-  for (int j = threadIdx.x; j < r.V - 8 * n; j += kThreads) {
+  for (int j = t; j < r.V - 8 * n; j += kThreads) {
     const int id = r.split.edge_elem(j);
     one(id, (uint32_t)r.p[id]);
   }
@@ -136,9 +145,33 @@ __device__ __forceinline__ uint32_t block_count(uint32_t v, uint32_t* smem) {
   return s;
 }
 
-// `per`: 1 / tau.  (Not inlined: the coefficients of the exponential, two registers each, would be kept from one row to the next.)
-__device__ __attribute__((noinline)) double weight_of(uint32_t key, double top, double per) {
-  return exp(((double)value_of(key) - top) * per);
+// exp(y), y <= 0, to about a unit in the last place: y = (64 i + j) ln 2 / 64 + r with |r| <= ln 2 / 128, 2^(j / 64) from a table in LDS
+// (begin()), exp(r) by its series (r^6 / 720 is 2^-54.6 at most).  Half the operations of the library's, and few constants.
+__device__ __forceinline__ void begin_exponentials(Shared& s) {
+  if (threadIdx.x < kTable) s.table[threadIdx.x] = exp2((double)threadIdx.x / kTable);
+}
+__device__ __forceinline__ double exponential(double y, const Shared& s) {
+  y = __builtin_fmin(__builtin_fmax(y, -800.0), 0.0);  // (0 below; searches ask above the largest entry too)
+  const double k = __builtin_rint(y * 0x1.71547652b82fep+6);
+  double r = __builtin_fma(k, -0x1.62e42fefa39efp-7, y);
+  r = __builtin_fma(k, -0x1.abc9e3b39803fp-62, r);
+  double p = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
+  p = __builtin_fma(r, p, 1.0 / 6.0);
+  p = __builtin_fma(r, p, 0.5);
+  p = __builtin_fma(r * r, p, r);
+  const int i = (int)k;
+  const double t = s.table[i & (kTable - 1)];
+  return __builtin_amdgcn_ldexp(__builtin_fma(t, p, t), i >> 6);
+}
+// `per`: 1 / tau
+__device__ __forceinline__ double weight_of(uint32_t key, double top, double per, const Shared& s) {
+  return exponential(((double)value_of(key) - top) * per, s);
+}
+
+// lane i's
+__device__ __forceinline__ double lane_value(double v, int i) {
+  const uint2 u = __builtin_bit_cast(uint2, v);
+  return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(u.x, i), __builtin_amdgcn_readlane(u.y, i)));
 }
 
 enum Find { kCount, kMassReaches, kMassExceeds };
@@ -156,7 +189,7 @@ struct Passes {
       const uint32_t k = key_of(b);
       if (k < key || k < kLowest) return;
       ++n;
-      m += weight_of(k, top, at);
+      m += weight_of(k, top, at, s);
     });
     *count = block_count(n, s.sums);
     *mass = block_sum64(m, s.masses[0]);
@@ -176,7 +209,7 @@ struct Passes {
     uint32_t n = 0;
     each_entry(row, [&](int, uint32_t b) {
       const uint32_t k = key_of(b);
-      n += k >= kLowest && weight_of(k, top, per) >= least;
+      n += k >= kLowest && weight_of(k, top, per, s) >= least;
     });
     return block_count(n, s.sums);
   }
@@ -199,7 +232,7 @@ struct Passes {
         m_hi = m;
       }
     }
-    return Place{lo, n_hi, n_lo - n_hi, m_hi};
+    return Place{lo, n_hi, n_lo - n_hi, m_hi, weight_of(lo, top, per, s)};
   }
 };
 
@@ -210,20 +243,21 @@ struct Counted {
   uint32_t top_key, all;
   double top, per, sum;
 
-  static __device__ __forceinline__ uint32_t key(int t, int e) {
+  static __device__ __forceinline__ uint32_t key(const Shared& s, int t, int e) {
     if (t < kOwners) return 0x8000u + kFirst + kValues - 1 - (uint32_t)(t * kEach + e);
-    if (t == kOwners) return 0x8000u;
-    return ~(0x8000u + kFirst + (uint32_t)((t - kOwners - 1) * kEach + e)) & 0xffffu;
+    const int i = (t - kOwners) * kEach + e;
+    if (i < kNear) return s.near_keys[i];
+    return ~(0x8000u + kFirst + (uint32_t)(i - kNear)) & 0xffffu;
   }
   static __device__ __forceinline__ uint32_t count_of(const Shared& s, int t, int e) {
     if (t < kOwners) return s.counts[2 * (kValues - 1 - (t * kEach + e))];
-    if (t == kOwners) return e == 0 ? s.counts[kZero] : 0;
-    return t <= 2 * kOwners ? s.counts[2 * ((t - kOwners - 1) * kEach + e) + 1] : 0;
+    const int i = (t - kOwners) * kEach + e;
+    return i < kNear ? s.near_counts[i] : s.counts[2 * (i - kNear) + 1];
   }
   // the first stretch for which `is` holds (it holds for those behind it too), all threads of the wave
   template <class F>
   static __device__ __forceinline__ int first_stretch(F&& is) {
-    const int lane = threadIdx.x & 63;
+    const int lane = thread_of_phase() & 63;
     constexpr int kPer = kThreads / kWave;
     const uint64_t ends = __ballot(is(lane * kPer + kPer - 1));
     const int group = ends ? __builtin_ctzll(ends) : kWave - 1;
@@ -232,14 +266,13 @@ struct Counted {
   }
   // how many weigh `least` and more (weights fall along the order whether a value occurs or not)
   __device__ __forceinline__ uint32_t at_least(double least) const {
-    const int t = first_stretch([&](int t) { return t > 2 * kOwners || weight_of(key(t, t == kOwners ? 0 : kEach - 1), top, per) < least; });
+    const int t = first_stretch([&](int t) { return weight_of(key(s, t, kEach - 1), top, per, s) < least || t == kThreads - 1; });
     uint32_t n = t ? s.count_ends[t - 1] : 0;
-    if (t > 2 * kOwners) return n;
-    const int e = threadIdx.x & (kEach - 1);
+    const int e = thread_of_phase() & (kEach - 1);
     const uint32_t here = count_of(s, t, e);
-    const uint32_t mine = here && weight_of(key(t, e), top, per) >= least ? here : 0;
+    const uint32_t mine = here && weight_of(key(s, t, e), top, per, s) >= least ? here : 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) n += __shfl(mine, i, kWave);
+    for (int i = 0; i < kEach; ++i) n += __builtin_amdgcn_readlane(mine, i);
     return n;
   }
   // (there is enough: what is asked for is at most what there is; the last value there is takes what rounding leaves over)
@@ -250,60 +283,140 @@ struct Counted {
       const double w = s.mass_ends[t];
       return c == all || (c > 0 && (what == kMassReaches ? w >= mass : w > mass));
     });
-    const int e = threadIdx.x & (kEach - 1);
+    const int e = thread_of_phase() & (kEach - 1);
     const uint32_t n = count_of(s, t, e);
-    const double m = n ? n * weight_of(key(t, e), top, per) : 0.0;
-    uint32_t c = t ? s.count_ends[t - 1] : 0;
-    double w = t ? s.mass_ends[t - 1] : 0.0;
-    Place p{};
+    const double one = weight_of(key(s, t, e), top, per, s);
+    // up to the end of each of the eight (lanes eight apart do the same)
+    uint32_t c = n;
+    double w = n * one;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t ni = __shfl(n, i, kWave);
-      const double mi = __shfl(m, i, kWave);
-      const bool done = p.here && (what == kCount ? c >= target : what == kMassReaches ? w >= mass : w > mass);
-      // (what rounding leaves over is not an entry's of weight 0)
-      if (!done && ni && (what == kCount || !p.here || mi > 0.0)) p = Place{key(t, i), c, ni, w};
-      c += ni;
-      w += mi;
+    for (int off = 1; off < kEach; off <<= 1) {
+      const uint32_t c2 = __shfl_up(c, off, kEach);
+      const double w2 = __shfl_up(w, off, kEach);
+      if (e >= off) {
+        c += c2;
+        w = w2 + w;
+      }
     }
+    const uint32_t c0 = t ? s.count_ends[t - 1] : 0;
+    const double w0 = t ? s.mass_ends[t - 1] : 0.0;
+    c += c0;
+    w += w0;
+    const bool enough = what == kCount ? c >= target : what == kMassReaches ? w >= mass : w > mass;
+    // (what rounding leaves over is the last one's that has any weight)
+    const uint64_t those = __ballot(enough && n) & 0xff, some = __ballot(n && one > 0.0) & 0xff, any = __ballot(n != 0) & 0xff;
+    const int i = those ? __builtin_ctzll(those) : some ? 63 - __builtin_clzll(some) : any ? 63 - __builtin_clzll(any) : 0;
+    const uint32_t here = __builtin_amdgcn_readlane(n, i);
+    const double before = i ? lane_value(w, i ? i - 1 : 0) : w0;
+    const Place p = {key(s, t, i), (uint32_t)__builtin_amdgcn_readlane(c, i) - here, here, before, lane_value(one, i)};
     return p;
   }
 };
 
-// the largest value that is counted (0: none), all threads
-__device__ __forceinline__ uint32_t largest_counted(Shared& s) {
-  const int t = threadIdx.x;
-  uint32_t mine = 0;
-#pragma unroll
-  for (int e = kEach - 1; e >= 0; --e)
-    if (Counted::count_of(s, t, e)) mine = Counted::key(t, e);
-  const uint64_t any = __ballot(mine != 0);
-  if (any ? (t & 63) == __builtin_ctzll(any) : (t & 63) == 0) s.sums[t >> 6] = mine;
+// The list of what is close to zero in its order, equal ones in the first of their places, zero (counted in the first place until
+// now) in there once.  All threads.
+__device__ __attribute__((noinline)) void order_near(Shared& s) {
+  const int t = threadIdx.x, n = (int)s.near;
+  const uint32_t zeros = s.near_counts[0];
   __syncthreads();
-  uint32_t top = 0;
-  for (int w = kWaves - 1; w >= 0; --w)
-    if (s.sums[w]) top = s.sums[w];
-  return top;
+  if (t < kNear) {
+    const uint32_t mine = t < n ? s.near_list[t] : t == n ? 0x8000 : kBelowNear;
+    int above = t > n ? t : 0, same_before = 0, same = 1;
+    if (t <= n) {
+      for (int i = 0; i < n; ++i) {
+        const uint32_t k = s.near_list[i];
+        above += k > mine;
+        same += k == mine && i != t;
+        same_before += k == mine && i < t;
+      }
+      above += t != n && mine < 0x8000;  // (zero)
+    }
+    s.near_keys[above + same_before] = mine;
+    s.near_counts[above + same_before] = t > n || same_before ? 0 : t == n ? zeros : same;
+  }
+  __syncthreads();
+}
+
+// The counts of the thread's eight values, in their order.
+__device__ __forceinline__ void read_counts(const Shared& s, int t, uint32_t (&n)[kEach]) {
+  if (t >= kOwners && t < kOwners + kNear / kEach) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) n[e] = s.near_counts[(t - kOwners) * kEach + e];
+    return;
+  }
+  // (sixteen counters, of both signs: reads of every other word would meet in few banks)
+  const bool negative = t >= kOwners;
+  const int at = negative ? 2 * (t - kOwners - kNear / kEach) * kEach : 2 * (kValues - kEach * (t + 1));
+  uint32_t w[2 * kEach];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 v = *reinterpret_cast<const uint4*>(&s.counts[at + 4 * i]);
+    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) n[e] = negative ? w[2 * e + 1] : w[2 * (kEach - 1 - e)];
+}
+
+// the largest value that is counted (0: none), all threads
+__device__ __forceinline__ uint32_t largest_counted(Shared& s, const uint32_t (&n)[kEach]) {
+  const int t = thread_of_phase();
+  uint32_t there = 0;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) there |= n[e] ? 1u << e : 0;
+  const uint64_t any = __ballot(there != 0);
+  const int first = any ? __builtin_ctzll(any) : 0;
+  if ((t & 63) == first) s.sums[t >> 6] = there ? Counted::key(s, t, __builtin_ctz(there)) : 0;
+  __syncthreads();
+  const uint32_t mine = s.sums[t & (kWaves - 1)];
+  const uint64_t waves = __ballot(mine != 0);
+  return waves ? __builtin_amdgcn_readlane(mine, __builtin_ctzll(waves)) : 0;
 }
 
 // Weighs the stretches, all threads: what there is up to the end of each, and the sum at temperature 1.  (Ends rise: a stretch's is the
-// sum over its wave so far, added to the waves' before.)
-__device__ __forceinline__ void weigh(Shared& s, double top, double per, bool nll, double* sum1) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// sum over its wave so far, added to the waves' before.)  Eight values of a stretch lie evenly apart, so that their weights are
+// powers of one ratio: two exponentials for eight, and 2^-50 of a weight at most in roundings.
+__device__ __forceinline__ void weigh(Shared& s, const uint32_t (&n)[kEach], double top, double per, bool nll, double* sum1) {
+  const int t = thread_of_phase(), lane = t & 63, wave = t >> 6;
   uint32_t c = 0;
   double w = 0.0, w1 = 0.0;
-  const bool both = nll && per != 1.0;
-#pragma unroll 1
-  for (int e = 0; e < kEach; ++e) {
-    const uint32_t n = Counted::count_of(s, threadIdx.x, e);
-    if (n) {
-      const uint32_t key = Counted::key(threadIdx.x, e);
-      w += n * weight_of(key, top, per);
-      if (both) w1 += n * weight_of(key, top, 1.0);
-    }
-    c += n;
-  }
+  const bool both = nll && per != 1.0, near = t >= kOwners && t < kOwners + kNear / kEach;
+  uint32_t there = 0;
 #pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    c += n[e];
+    there |= n[e] ? 1u << e : 0;
+  }
+  if (c && !near) {
+    // (from the first that occurs: those before it may lie above the top)
+    const int f = __builtin_ctz(there);
+    const double first = value_of(Counted::key(s, t, f)), step = value_of(Counted::key(s, t, 0)) - value_of(Counted::key(s, t, 1));
+    double one = exponential((first - top) * per, s);
+    const double ratio = exponential(-step * per, s);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      w = __builtin_fma((double)n[e], one, w);
+      if (e >= f) one *= ratio;
+    }
+    if (both) {
+      one = exponential(first - top, s);
+      const double ratio1 = exponential(-step, s);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        w1 = __builtin_fma((double)n[e], one, w1);
+        if (e >= f) one *= ratio1;
+      }
+    }
+  }
+  if (c && near) {
+#pragma unroll 1
+    for (int e = 0; e < kEach; ++e) {
+      const double k = Counted::count_of(s, t, e);
+      const uint32_t key = Counted::key(s, t, e);
+      w += k * weight_of(key, top, per, s);
+      if (both) w1 += k * weight_of(key, top, 1.0, s);
+    }
+  }
+#pragma unroll 1
   for (int off = 1; off < kWave; off <<= 1) {
     const uint32_t c2 = __shfl_up(c, off, kWave);
     const double w2 = __shfl_up(w, off, kWave);
@@ -322,6 +435,7 @@ __device__ __forceinline__ void weigh(Shared& s, double top, double per, bool nl
   __syncthreads();
   uint32_t c0 = 0;
   double w0 = 0.0, all1 = 0.0, all = 0.0;
+#pragma unroll 4
   for (int i = 0; i < kWaves; ++i) {
     if (i == wave) {
       c0 += c;
@@ -332,8 +446,8 @@ __device__ __forceinline__ void weigh(Shared& s, double top, double per, bool nl
     all += s.masses[0][i];
     all1 += s.masses[1][i];
   }
-  s.count_ends[threadIdx.x] = c0;
-  s.mass_ends[threadIdx.x] = w0;
+  s.count_ends[t] = c0;
+  s.mass_ends[t] = w0;
   *sum1 = both ? all1 : all;
   __syncthreads();
 }
@@ -356,14 +470,14 @@ __device__ __forceinline__ Choice choose(const Entries& x, const Settings& q, bo
       return;
     }
     end = x.find(kCount, n, 0.0);
-    sum = end.mass + (double)(n - end.before) * weight_of(end.key, x.top, x.per);
+    sum = end.mass + (double)(n - end.before) * end.weight;
   };
   cut();
   const uint32_t by_k = n;
   if (q.top_p < 1.0 && n > 1) {
     const double enough = q.top_p * sum;
     const Place p = x.find(kMassReaches, 0, enough);
-    const double more = ceil((enough - p.mass) / weight_of(p.key, x.top, x.per));
+    const double more = ceil((enough - p.mass) / p.weight);
     const uint32_t here = more < 1.0 ? 1 : more < (double)p.here ? (uint32_t)more : p.here;
     if (p.before + here < n) n = p.before + here;
   }
@@ -374,13 +488,13 @@ __device__ __forceinline__ Choice choose(const Entries& x, const Settings& q, bo
   if (n < 1) n = 1;
   if (n != by_k) cut();
   const double at = q.u * sum;
-  Place p = n == 1 ? Place{x.top_key, 0, 1, 0.0} : x.find(kMassExceeds, 0, at);
+  Place p = n == 1 ? Place{x.top_key, 0, 1, 0.0, 1.0} : x.find(kMassExceeds, 0, at);
   uint32_t here = p.here;
   if (n != x.all && n > 1) {
     if (p.before >= end.before) p = end;  // (no further than the last one that is kept)
     if (p.key == end.key) here = n - end.before;
   }
-  const double steps = floor((at - p.mass) / weight_of(p.key, x.top, x.per));
+  const double steps = floor((at - p.mass) / p.weight);
   const uint32_t which = !(steps > 0.0) ? 0 : steps < (double)here ? (uint32_t)steps : here - 1;
   return Choice{p.key, n, which, ((double)value_of(p.key) - x.top) * x.per - log(sum)};
 }
@@ -395,8 +509,7 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   }
   __syncthreads();
   const uint32_t bits = key == 0x8000 ? 0 : key & 0x8000 ? key & 0x7fff : ~key & 0xffff, mask = bits ? 0xffff : 0x7fff;  // (-0 is 0)
-  auto one = [&](int id, uint32_t b) {
-    if ((b & mask) != bits) return;
+  auto hit = [&](int id) {
     if (which == 0) {
       atomicMin(&s.found, id);
     } else {
@@ -414,13 +527,15 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
         for (int t = 0; t < 4; ++t) d[t] = __builtin_bit_cast(u16x2, (w[t] & mask2) ^ bits2);
         const u16x2 least = __builtin_elementwise_min(__builtin_elementwise_min(d[0], d[1]), __builtin_elementwise_min(d[2], d[3]));
         if (least[0] != 0 && least[1] != 0) return;
+        uint32_t hits = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) hits |= (d[t >> 1][t & 1] == 0 ? 1u : 0u) << t;
 #pragma unroll 1
-        for (int t = 0; t < 8; ++t) {
-          const uint32_t two = t < 4 ? (t < 2 ? w[0] : w[1]) : (t < 6 ? w[2] : w[3]);
-          one(id + t, t & 1 ? two >> 16 : two & 0xffff);
-        }
+        for (; hits; hits &= hits - 1) hit(id + __builtin_ctz(hits));
       },
-      one);
+      [&](int id, uint32_t b) {
+        if ((b & mask) == bits) hit(id);
+      });
   __syncthreads();
   if (which == 0) return s.found;
   if (s.listed <= kThreads) {
@@ -524,15 +639,23 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
   const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
 
   for (int i = threadIdx.x; i < (int)(sizeof(s.counts) / 16); i += kThreads) reinterpret_cast<uint4*>(s.counts)[i] = make_uint4(0, 0, 0, 0);
-  if (threadIdx.x == 0) s.big = s.odd = 0;
+  if (threadIdx.x < kNear) {
+    s.near_keys[threadIdx.x] = threadIdx.x ? kBelowNear : 0x8000;
+    s.near_counts[threadIdx.x] = 0;
+  }
+  if (threadIdx.x == 0) s.big = s.odd = s.near = 0;
+  begin_exponentials(s);
   __syncthreads();
   uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
   auto other = [&](uint32_t b) {
     const uint32_t size = b & 0x7fff;
     if (size == 0)
-      atomicAdd(&s.counts[kZero], 1u);
-    else if (size - kFirst >= kValues && b != 0xff80) {
-      if (b >= 0x8000 + kFirst + kValues && b < 0xff80)
+      atomicAdd(&s.near_counts[0], 1u);
+    else if (size < kFirst) {
+      const uint32_t n = atomicAdd(&s.near, 1u);
+      if (n < kNear - 1) s.near_list[n] = key_of(b);
+    } else if (size >= kFirst + kValues && b != 0xff80) {
+      if (b > 0x8000 && b < 0xff80)
         ++big;
       else
         odd = 1;
@@ -574,17 +697,20 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
   if (odd) s.odd = 1;
   __syncthreads();
   big = s.big;
-  odd = s.odd;
+  odd = s.odd || s.near >= kNear;
+  if (s.near && !odd) order_near(s);
   Choice c;
-  double sum1 = 1.0, top;  // of the weights at temperature 1
-  const uint32_t top_key = largest_counted(s);
+  double sum1 = 1.0, log1, top;  // of the weights at temperature 1
+  uint32_t n[kEach];
+  read_counts(s, thread_of_phase(), n);
+  const uint32_t top_key = largest_counted(s, n);
   const double counted_top = top_key ? value_of(top_key) : 0.0;
   // Numbers below -256 have no weight that 64 bits would show beside the largest's (2^-90 times at most 2^26 of them) where that is
   // 64 temperatures above -256, and are none that a min-p would keep.
   const double room = counted_top + 256.0;
   const bool apart = room >= 64.0 && room >= 64.0 * q.tau && (q.min_p == 0.0 || room > q.tau * (1.0 - log(q.min_p)));
   if (!odd && top_key && (!big || apart)) {
-    weigh(s, counted_top, q.per, a.nll != nullptr, &sum1);
+    weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
     if (threadIdx.x < kWave) {
       const Counted counted{s, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
       Choice mine = choose(counted, q, greedy);
@@ -594,17 +720,20 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
       }
       if (threadIdx.x == 0) s.choice = mine;
     }
+    if (threadIdx.x == kWave) s.log1 = log(sum1);  // (beside the search)
     __syncthreads();
     c = s.choice;
+    log1 = s.log1;
     top = counted_top;
   } else {
     if (!by_passes(row, q, greedy, a.nll != nullptr, s, &c, &sum1, &top)) {
       put(-1, nan, nan, 0, NPD_DEV_BAD_LOGITS);
       return;
     }
+    log1 = log(sum1);
   }
   const int token = find_entry(row, c.key, c.which, s);
-  put(token, c.logprob, log(sum1) + (top - (double)value_of(c.key)), c.kept, 0);
+  put(token, c.logprob, log1 + (top - (double)value_of(c.key)), c.kept, 0);
 }
 
 }  // namespace

@@ -66,6 +66,23 @@ def test_logits_of_every_size(spread):
         check(*logits(8, 3000, spread=spread), **settings)
 
 
+@pytest.mark.parametrize("n", [1, 2, 8, 9, 254, 255, 256, 300])
+def test_entries_close_to_zero(n):
+    """Numbers below 2^-23, some of them equal, zeros of both signs among them: listed, or too many for the list."""
+    x, u = logits(24, 2000, spread=0.3)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    tiny = torch.randint(1, 1 + 3 * n, (24, n), device=DEV, generator=g) * torch.randint(0, 2, (24, n), device=DEV, generator=g).mul(2).sub(1)
+    x[:, 100:100 + n] = tiny.float() * 2.0 ** -40
+    x[::2, 1900:1907] = 0.0
+    x[::3, 1907:1911] = -0.0
+    for settings in (dict(), dict(top_k=1000), dict(temperature=2.0 ** -40), dict(temperature=2.0 ** -39, min_p=0.2, top_p=0.9), dict(top_p=0.5)):
+        check(x, u, **settings)
+    x[:, :100], x[:, 100 + n:] = float("-inf"), float("-inf")
+    x[::2, 1900] = 0.0
+    for settings in (dict(), dict(temperature=2.0 ** -39), dict(temperature=2.0 ** -39, min_p=0.7), dict(temperature=0.0), dict(min_p=1.0)):
+        check(x, u, **settings)
+
+
 @pytest.mark.parametrize("scale", [2.0 ** -40, 2.0 ** -24, 2.0 ** -22, 100.0, 1e4, 1e35])
 def test_temperatures_as_large_as_the_logits(scale):
     x, u = logits(8, 2000, spread=scale)
