@@ -36,12 +36,21 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* smem) {
   }
 }
 
+// Values [d, d + 8) of a row, 0 behind its end.  WHOLE: rows are whole groups of eight (what ends of groups take otherwise, in code and
+// registers, costs such rows 20 %).
+template <bool WHOLE>
+__device__ __forceinline__ uint4 read8(const uint16_t* row, int d, int cols) {
+  if constexpr (!WHOLE) return load8_of(row, d, cols);
+  const uint4 v = load8(row + (d < cols ? d : 0));
+  return d < cols ? v : make_uint4(0, 0, 0, 0);
+}
 // values [d, d + 8) of a row, those behind its end are left as they are
+template <bool WHOLE>
 __device__ __forceinline__ void store8_of(uint16_t* row, int d, int cols, const float (&v)[8]) {
   const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-  if (d + 8 <= cols) {
+  if (WHOLE ? d < cols : d + 8 <= cols) {
     store8(row + d, w);
-  } else {
+  } else if constexpr (!WHOLE) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int t = 0; t < 8; ++t)
@@ -51,7 +60,15 @@ __device__ __forceinline__ void store8_of(uint16_t* row, int d, int cols, const 
 
 constexpr uint32_t kOnes = 0x3f803f80u;  // two bf16 ones
 
-template <int TH, int G>
+// What stays in registers, for a row or for all rows of a workgroup, stays packed: the compiler would keep what is unpacked once, in
+// twice the registers (norm_grad_kernel<64, 4> 256 of them, a wave per SIMD).
+template <int G>
+__device__ __forceinline__ void stay_packed(uint4 (&w)[G]) {
+#pragma unroll
+  for (int u = 0; u < G; ++u) asm volatile("" : "+v"(w[u].x), "+v"(w[u].y), "+v"(w[u].z), "+v"(w[u].w));
+}
+
+template <int TH, int G, bool WHOLE>
 __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
   __shared__ float smem[norm_block<TH>() / kWave];
   constexpr int kRows = norm_block<TH>() / TH;  // a workgroup's at a time
@@ -59,15 +76,17 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
   uint4 w[G], b[G];
 #pragma unroll
   for (int u = 0; u < G; ++u) {
-    w[u] = a.w ? load8_of(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
-    b[u] = a.b ? load8_of(a.b, at + 8 * TH * u, a.D) : make_uint4(0, 0, 0, 0);
+    w[u] = a.w ? read8<WHOLE>(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
+    b[u] = a.b ? read8<WHOLE>(a.b, at + 8 * TH * u, a.D) : make_uint4(0, 0, 0, 0);
   }
   const float per = 1.0f / (float)a.D;
   for (int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / TH; p < a.T; p += (int64_t)gridDim.x * kRows) {
     const uint16_t* row = a.x + p * a.x_stride;
+    stay_packed(w);
+    stay_packed(b);
     uint4 x[G];
 #pragma unroll
-    for (int u = 0; u < G; ++u) x[u] = load8_of(row, at + 8 * TH * u, a.D);
+    for (int u = 0; u < G; ++u) x[u] = read8<WHOLE>(row, at + 8 * TH * u, a.D);
     float mean = 0.0f;
     if (!a.rms) {
       float s[1] = {0.0f};
@@ -80,6 +99,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
       row_sums<TH, 1>(s, smem);
       mean = s[0] * per;
     }
+    stay_packed(x);
     float s[1] = {0.0f};
 #pragma unroll
     for (int u = 0; u < G; ++u) {
@@ -87,11 +107,12 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
       unpack8(x[u], v);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const float d = at + 8 * TH * u + t < a.D ? v[t] - mean : 0.0f;
+        const float d = (WHOLE ? at + 8 * TH * u : at + 8 * TH * u + t) < a.D ? v[t] - mean : 0.0f;
         s[0] = __builtin_fmaf(d, d, s[0]);
       }
     }
     row_sums<TH, 1>(s, smem);
+    stay_packed(x);
     const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
     if (threadIdx.x % TH == 0) {
       if (a.mean) a.mean[p] = mean;
@@ -106,13 +127,13 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
       unpack8(b[u], bv);
 #pragma unroll
       for (int t = 0; t < 8; ++t) v[t] = __builtin_fmaf((v[t] - mean) * rstd, wv[t], bv[t]);
-      store8_of(out, at + 8 * TH * u, a.D, v);
+      store8_of<WHOLE>(out, at + 8 * TH * u, a.D, v);
     }
   }
 }
 
 // HELD: the workgroup's sums over its rows for the parameters' gradients stay in registers, and go to its piece at the end.
-template <int TH, int G, bool HELD>
+template <int TH, int G, bool HELD, bool WHOLE>
 __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArgs a) {
   __shared__ float smem[2 * norm_block<TH>() / kWave];
   __shared__ float joined[HELD && TH == kWave ? 2 * TH * 8 * G : 1];
@@ -120,16 +141,17 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
   const int at = (threadIdx.x % TH) * 8;
   uint4 w[G];
 #pragma unroll
-  for (int u = 0; u < G; ++u) w[u] = a.w ? load8_of(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
+  for (int u = 0; u < G; ++u) w[u] = a.w ? read8<WHOLE>(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
   float dw[HELD ? G : 1][8] = {}, db[HELD ? G : 1][8] = {};
   const float per = 1.0f / (float)a.D;
   for (int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / TH; p < a.T; p += (int64_t)gridDim.x * kRows) {
     const uint16_t *grow = a.g + p * a.g_stride, *xrow = a.x + p * a.x_stride;
+    stay_packed(w);
     uint4 g[G], x[G];
 #pragma unroll
     for (int u = 0; u < G; ++u) {
-      g[u] = load8_of(grow, at + 8 * TH * u, a.D);  // (0 behind the end: no part in any sum)
-      x[u] = load8_of(xrow, at + 8 * TH * u, a.D);
+      g[u] = read8<WHOLE>(grow, at + 8 * TH * u, a.D);  // (0 behind the end: no part in any sum)
+      x[u] = read8<WHOLE>(xrow, at + 8 * TH * u, a.D);
     }
     const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
     float s[2] = {0.0f, 0.0f};
@@ -152,6 +174,9 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
     }
     if (!a.dx) continue;
     row_sums<TH, 2>(s, smem);
+    stay_packed(g);
+    stay_packed(x);
+    stay_packed(w);
     const float along = s[0] * per, flat = a.rms ? 0.0f : s[1] * per;
     uint16_t* out = a.dx + p * a.dx_stride;
 #pragma unroll
@@ -165,7 +190,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
         const float n = (xv[t] - mean) * rstd;
         gv[t] = __builtin_fmaf(-n, along, gv[t] * wv[t] - flat) * rstd;
       }
-      store8_of(out, at + 8 * TH * u, a.D, gv);
+      store8_of<WHOLE>(out, at + 8 * TH * u, a.D, gv);
     }
   }
   if constexpr (HELD) {
@@ -175,7 +200,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
       for (int r = 0; r < kRows; ++r) {
         if (threadIdx.x / TH == r) {
 #pragma unroll
-          for (int u = 0; u < G; ++u)
+          for (int u = 0; u < G; ++u) {
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
               const int i = (u * 8 + t) * TH + (threadIdx.x & 63);
@@ -185,6 +210,8 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
               joined[i] = dw[u][t];
               joined[G * 8 * TH + i] = db[u][t];
             }
+            asm volatile("" ::: "memory");  // (a group's sums at a time)
+          }
         }
         __syncthreads();
       }
@@ -197,7 +224,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         const int d = at + 8 * TH * u + t;
-        if (d >= a.D) break;
+        if ((WHOLE ? d - t : d) >= a.D) break;
         if (a.dw) pw[d] = dw[u][t];
         if (a.db) pb[d] = db[u][t];
       }
@@ -238,22 +265,28 @@ __global__ __launch_bounds__(kNormThreads) void norm_columns_kernel(NormGradArgs
   }
 }
 
-// Joins the pieces: 64 columns to a workgroup, a wave has every sixteenth piece of them.
-constexpr int kJoinThreads = 1024;
+// Joins the pieces: 32 columns to a workgroup, a half wave has every 32nd piece of them.
+constexpr int kJoinThreads = 1024, kJoinColumns = 32;
 __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormGradArgs a) {
-  constexpr int kWaves = kJoinThreads / kWave;
-  __shared__ float joined[kWaves][kWave];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * kWave + lane;
+  constexpr int kSlots = kJoinThreads / kJoinColumns;
+  __shared__ float joined[kSlots][kJoinColumns];
+  const int c = threadIdx.x % kJoinColumns, slot = threadIdx.x / kJoinColumns, d = blockIdx.x * kJoinColumns + c;
   const bool bias = blockIdx.y == 1 || !a.dw;
-  const float* pieces = bias ? a.db_pieces : a.dw_pieces;
-  float s = 0.0f;
-  if (d < a.D)
-    for (int i = wave; i < a.pieces; i += kWaves) s += pieces[(int64_t)i * a.D + d];
-  joined[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && d < a.D) {
+  const float* pieces = (bias ? a.db_pieces : a.dw_pieces) + (d < a.D ? d : a.D - 1);
+  constexpr int kMost = kNormPieces / kSlots;
+  float v[kMost], s = 0.0f;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) s += joined[w][lane];
+  for (int i = 0; i < kMost; ++i) {
+    const int piece = slot + i * kSlots;
+    v[i] = pieces[(int64_t)(piece < a.pieces ? piece : 0) * a.D];  // (all requested together)
+  }
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) s += slot + i * kSlots < a.pieces ? v[i] : 0.0f;
+  joined[slot][c] = s;
+  __syncthreads();
+  if (threadIdx.x < kJoinColumns && d < a.D) {
+#pragma unroll
+    for (int i = 1; i < kSlots; ++i) s += joined[i][c];
     uint16_t* out = bias ? a.db : a.dw;
     out[d] = one_bf16(a.accumulate ? s + bf16_one(out[d]) : s);
   }
@@ -263,7 +296,8 @@ template <int TH, int G>
 hipError_t launch_rows(const NormArgs& a, hipStream_t stream) {
   constexpr int kRows = norm_block<TH>() / TH;
   const int64_t blocks = (a.T + kRows - 1) / kRows;
-  return launch_kernel(norm_kernel<TH, G>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(norm_block<TH>()), 0, stream, a);
+  return launch_kernel(a.D % 8 == 0 ? norm_kernel<TH, G, true> : norm_kernel<TH, G, false>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)),
+                       dim3(norm_block<TH>()), 0, stream, a);
 }
 
 template <int TH, int G>
@@ -271,11 +305,15 @@ hipError_t launch_grad(const NormGradArgs& a, hipStream_t stream) {
   constexpr int kRows = norm_block<TH>() / TH;
   const int64_t blocks = (a.T + kRows - 1) / kRows;
   const dim3 block(norm_block<TH>());
+  const bool whole = a.D % 8 == 0;
   if constexpr (TH * 8 * G <= kNormHeldWidth) {
-    if (a.dw || a.db) return launch_kernel(norm_grad_kernel<TH, G, true>, dim3((unsigned)a.pieces), block, 0, stream, a);
+    if (a.dw || a.db)
+      return launch_kernel(whole ? norm_grad_kernel<TH, G, true, true> : norm_grad_kernel<TH, G, true, false>, dim3((unsigned)a.pieces), block, 0,
+                           stream, a);
   }
   if (!a.dx) return hipSuccess;
-  return launch_kernel(norm_grad_kernel<TH, G, false>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), block, 0, stream, a);
+  return launch_kernel(whole ? norm_grad_kernel<TH, G, false, true> : norm_grad_kernel<TH, G, false, false>,
+                       dim3((unsigned)(blocks < 65536 ? blocks : 65536)), block, 0, stream, a);
 }
 
 }  // namespace
@@ -311,7 +349,7 @@ hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t stream) {
     const hipError_t c = launch_kernel(norm_columns_kernel, dim3((unsigned)(a.D + 511) / 512, (unsigned)a.pieces), dim3(kNormThreads), 0, stream, a);
     if (c != hipSuccess) return c;
   }
-  return launch_kernel(norm_join_kernel, dim3((unsigned)(a.D + 63) / 64, a.dw && a.db ? 2 : 1), dim3(kJoinThreads), 0, stream, a);
+  return launch_kernel(norm_join_kernel, dim3((unsigned)(a.D + kJoinColumns - 1) / kJoinColumns, a.dw && a.db ? 2 : 1), dim3(kJoinThreads), 0, stream, a);
 }
 
 }  // namespace npd
