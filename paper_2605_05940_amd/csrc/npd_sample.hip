@@ -8,7 +8,7 @@
 // The 7,936 values of magnitude 2^-23 .. 2^8 and zero have a counter each, up to 255 entries closer to zero are listed; a row with
 // more of those, or an entry beyond 2^8 that may matter, is done by bisection over the values, with a pass over the row for each step.
 #include "../../include/npd.h"
-#include "npd_device.hpp"
+#include "npd_head_gemm.hpp"
 #include "npd_sample.hpp"
 
 namespace npd {
@@ -538,12 +538,18 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
       });
   __syncthreads();
   if (which == 0) return s.found;
-  if (s.listed <= kThreads) {
-    const uint32_t n = s.listed;
-    if (threadIdx.x < n) {
+  const uint32_t listed = s.listed;
+  if (listed <= kThreads) {
+    if (threadIdx.x < 4) s.counts[listed + threadIdx.x] = 0xffffffffu;  // (the list in fours)
+    __syncthreads();
+    if (threadIdx.x < listed) {
       const uint32_t mine = s.counts[threadIdx.x];
       uint32_t below = 0;
-      for (uint32_t i = 0; i < n; ++i) below += s.counts[i] < mine;
+#pragma unroll 4
+      for (uint32_t i = 0; i < listed; i += 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(&s.counts[i]);
+        below += (v.x < mine) + (v.y < mine) + (v.z < mine) + (v.w < mine);
+      }
       if (below == which) s.found = (int32_t)mine;
     }
     __syncthreads();
@@ -551,11 +557,22 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   }
   // very many of them: every wave counts in a stretch of its own, and the one that has it looks again
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int each = ((row.V + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
-  const int begin = wave * each < row.V ? wave * each : row.V, end = row.V - begin < each ? row.V : begin + each;
+  const int groups = (row.V + 7) / 8, each = (groups + kWaves - 1) / kWaves;
+  const int begin = wave * each < groups ? wave * each : groups, end = groups - begin < each ? groups : begin + each;
+  auto hits_of = [&](int g) {  // which of eight entries
+    const uint4 v = load8_of(row.p, 8 * g, row.V);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t hits = 0;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const uint32_t x = t & 1 ? w[t >> 1] >> 16 : w[t >> 1] & 0xffff;
+      hits |= ((x & mask) == bits && 8 * g + t < row.V ? 1u : 0u) << t;
+    }
+    return hits;
+  };
   uint32_t n = 0;
-#pragma unroll 8
-  for (int i = begin + lane; i < end; i += kWave) n += key_of(row.p[i]) == key;
+#pragma unroll 1
+  for (int g = begin + lane; g < end; g += kWave) n += __popc(hits_of(g));
   n = (uint32_t)wave_sum_int((int)n);
   if (lane == 0) s.sums[wave] = n;
   __syncthreads();
@@ -563,12 +580,22 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   for (int w = 0; w < wave; ++w) before += s.sums[w];
   if (which >= before && which - before < n) {
     uint32_t left = which - before;
-    for (int i = begin; i < end; i += kWave) {
-      const bool is = i + lane < end && key_of(row.p[i + lane]) == key;
-      const uint64_t all = __ballot(is);
-      const uint32_t here = (uint32_t)__popcll(all);
+#pragma unroll 1
+    for (int g = begin; g < end; g += kWave) {
+      uint32_t hits = g + lane < end ? hits_of(g + lane) : 0;
+      uint32_t upto = __popc(hits);
+      const uint32_t mine = upto;
+#pragma unroll 1
+      for (int off = 1; off < kWave; off <<= 1) {
+        const uint32_t o = __shfl_up(upto, off, kWave);
+        if (lane >= off) upto += o;
+      }
+      const uint32_t here = __shfl(upto, kWave - 1, kWave);
       if (left < here) {
-        if (is && (uint32_t)__popcll(all & ((1ull << lane) - 1)) == left) s.found = i + lane;
+        if (left >= upto - mine && left < upto) {
+          for (uint32_t skip = left - (upto - mine); skip; --skip) hits &= hits - 1;
+          s.found = 8 * (g + lane) + __builtin_ctz(hits);
+        }
         break;
       }
       left -= here;

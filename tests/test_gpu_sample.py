@@ -98,6 +98,17 @@ def test_few_values_and_many_ties():
         check(x, u, **settings)
 
 
+@pytest.mark.parametrize("V,offset", [(1024, 0), (1025, 1), (5003, 3), (20000, 0), (151936, 0)])
+@pytest.mark.parametrize("value", [0.0, -1.5, 2.0 ** -30, 300.0])
+def test_rows_of_equal_entries(V, offset, value):
+    """The list of the ids of a value is as long as a list may be, longer, and far longer."""
+    x, u = logits(7, V, offset=offset)
+    x.fill_(value)
+    x[3:, ::7] = value - 1
+    check(x, u)
+    check(x, u, top_k=V // 2, top_p=0.9)
+
+
 def test_zeros_of_either_sign_are_equal():
     x = torch.zeros((6, 300), dtype=torch.bfloat16, device=DEV)
     x[:, ::2] = -0.0
