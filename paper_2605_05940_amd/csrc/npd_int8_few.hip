@@ -118,11 +118,13 @@ __device__ __forceinline__ i32x4 load16_of(const int8_t* row, int d, int cols) {
   return i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
 
+constexpr int kTokenColumns = 32;
+
 // The end of a workgroup's PART columns, whose sums lie in LDS as [row][PART]: a wave per row, PART / 64 columns per lane.
-template <bool CAP, int PART>
+template <int PART>
 __device__ __forceinline__ void finish_columns(const Int8Args& a, const int* x) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const SoftCap soft(CAP ? a.cap : 1.0f);
+  const SoftCap soft(a.cap != 0.0f ? a.cap : 1.0f);
   constexpr int N = PART < kWave ? 1 : PART / kWave;
   if (PART < kWave && lane >= PART) return;
   const int n = blockIdx.x * PART + N * lane;
@@ -140,7 +142,7 @@ __device__ __forceinline__ void finish_columns(const Int8Args& a, const int* x) 
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       y[e] = __builtin_fmaf((float)x[m * PART + N * lane + e] * hs, scale[e], bias[e]);
-      if constexpr (CAP) y[e] = soft.cap * soft.tanh_of(y[e]);
+      if (a.cap != 0.0f) y[e] = soft.cap * soft.tanh_of(y[e]);  // uniform
     }
     uint16_t* out = a.out + m * a.out_stride + n;
     if (N == 2 && n + 2 <= a.V) {
@@ -152,93 +154,75 @@ __device__ __forceinline__ void finish_columns(const Int8Args& a, const int* x) 
   }
 }
 
-// Up to 4 NT rows: v_mfma_i32_4x4x4_16b_i8 as 16 pieces of k of the same four columns and four rows, added up at the end, so that one
-// load of a wave is 256 consecutive bytes of each of four rows of the weights, read past the caches.  Waves begin at different places
-// of their rows and wrap around (rows of a power of two of bytes would else be read out of few memory channels).
-//
-// PART 128: a wave has 32 columns of its own.  32: the four waves have the same ones and every fourth block of k, added up at the end.
-template <int NT, int PART, bool CAP>
-__global__ __launch_bounds__(kHeadThreads, NT == 1 ? 5 : 4) void int8_tokens_kernel(Int8Args a) {
-  constexpr int kWaves = kHeadThreads / kWave, G = 8, kShare = PART == 4 * G ? kWaves : 1;
-  static_assert(PART == 4 * G * kWaves / kShare, "");
-  __shared__ __attribute__((aligned(16))) int x[kShare][4 * NT][PART];
+// Up to four rows: v_mfma_i32_4x4x4_16b_i8 as 16 pieces of k of the same four columns and four rows, added up at the end, so that one
+// load of a wave is 256 consecutive bytes of each of four rows of the weights, read past the caches; the four waves of a workgroup
+// have the same 32 columns and every fourth block of k.  Workgroups begin at different places of their rows and wrap around (rows of
+// a power of two of bytes would else be read out of few memory channels).
+__global__ __launch_bounds__(kHeadThreads, 5) void int8_tokens_kernel(Int8Args a) {
+  constexpr int kWaves = kHeadThreads / kWave, G = 8;
+  constexpr int kBlock = 256;  // bytes of k per load
+  __shared__ __attribute__((aligned(16))) int x[kWaves][4][kTokenColumns];
+  static_assert(kTokenColumns == 4 * G && 4 * kTokenColumns <= kHeadThreads, "a thread per sum");
   typedef int words __attribute__((ext_vector_type(4), aligned(1)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 3, b = lane >> 2;
-  constexpr int kBlock = 256;  // bytes of k per load
   const int blocks = a.D / kBlock, tail = blocks * kBlock + 16 * b;
-  const int first = kShare > 1 ? wave : 0, mine = (blocks - first + kShare - 1) / kShare;  // blocks first, first + kShare ..
-  const int c0 = kShare > 1 ? 0 : wave * 4 * G;  // of the workgroup's columns
-  const int8_t *h[NT], *w[G];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int m = 4 * t + i;
-    h[t] = a.h + (m < a.T ? m : a.T - 1) * a.h_stride;
-  }
+  const int mine = (blocks - wave + kWaves - 1) / kWaves;  // blocks wave, wave + 4 ..
+  const int8_t* h = a.h + (i < a.T ? i : a.T - 1) * a.h_stride;
+  const int8_t* w[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    const int v = blockIdx.x * PART + c0 + 4 * g + i;
+    const int v = blockIdx.x * kTokenColumns + 4 * g + i;
     w[g] = a.w + (int64_t)(v < a.V ? v : a.V - 1) * a.w_stride;
   }
-  i32x4 acc[G][NT];
+  i32x4 acc[G];
 #pragma unroll
-  for (int g = 0; g < G; ++g)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[g][t] = i32x4{0, 0, 0, 0};
-  auto multiply = [&](const i32x4 (&wv)[G], const i32x4 (&hv)[NT]) {
+  for (int g = 0; g < G; ++g) acc[g] = i32x4{0, 0, 0, 0};
+  auto multiply = [&](const i32x4 (&wv)[G], const i32x4& hv) {
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[g][t] = __builtin_amdgcn_mfma_i32_4x4x4i8(wv[g][e], hv[t][e], acc[g][t], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) acc[g] = __builtin_amdgcn_mfma_i32_4x4x4i8(wv[g][e], hv[e], acc[g], 0, 0, 0);
   };
   int at = mine > 0 ? (int)((blockIdx.x * 4 + wave) % (unsigned)mine) : 0;
   for (int n = 0; n < mine; ++n) {
-    const int d = (first + at * kShare) * kBlock + 16 * b;
+    const int d = (wave + at * kWaves) * kBlock + 16 * b;
     at = at + 1 == mine ? 0 : at + 1;
-    i32x4 wv[G], hv[NT];
+    i32x4 wv[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) wv[g] = __builtin_nontemporal_load(reinterpret_cast<const words*>(w[g] + d));
-#pragma unroll
-    for (int t = 0; t < NT; ++t) hv[t] = load16(h[t] + d);
+    const i32x4 hv = load16(h + d);
+    __builtin_amdgcn_sched_barrier(0);  // (all requested before the first is waited for: 151,936 x 2,048 52.4 us, in the compiler's order 56.3)
     multiply(wv, hv);
   }
-  if (tail - 16 * b < a.D && (kShare == 1 || wave == kWaves - 1)) {  // uniform (the last wave has the fewest blocks)
-    i32x4 wv[G], hv[NT];
+  if (tail - 16 * b < a.D && wave == kWaves - 1) {  // uniform (the last wave has the fewest blocks)
+    i32x4 wv[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) wv[g] = load16_of(w[g], tail, a.D);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) hv[t] = load16_of(h[t], tail, a.D);
-    multiply(wv, hv);
+    multiply(wv, load16_of(h, tail, a.D));
   }
-  // acc[g][t][e] of lane (b, i): column 4 g + e, row 4 t + i, piece b of k
+  // acc[g][e] of lane (b, i): column 4 g + e, row i, piece b of k
 #pragma unroll
-  for (int g = 0; g < G; ++g)
+  for (int g = 0; g < G; ++g) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int off = 4; off < kWave; off <<= 1)
 #pragma unroll
-      for (int off = 4; off < kWave; off <<= 1)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[g][t][e] += __shfl_xor(acc[g][t][e], off, kWave);
-      if (b == g) *reinterpret_cast<i32x4*>(&x[kShare > 1 ? wave : 0][4 * t + i][c0 + 4 * g]) = acc[g][t];
-    }
+      for (int e = 0; e < 4; ++e) acc[g][e] += __shfl_xor(acc[g][e], off, kWave);
+    if (b == g) *reinterpret_cast<i32x4*>(&x[wave][i][4 * g]) = acc[g];
+  }
   __syncthreads();
-  if constexpr (kShare > 1) {
-    static_assert(4 * NT * PART <= kHeadThreads, "a thread per sum");
-    const int t = threadIdx.x;
-    if (t < 4 * NT * PART) {
-      int* sum = &x[0][0][0] + t;
+  const int t = threadIdx.x;
+  if (t < 4 * kTokenColumns) {
+    int* sum = &x[0][0][0] + t;
 #pragma unroll
-      for (int u = 1; u < kShare; ++u) *sum += sum[u * 4 * NT * PART];
-    }
-    __syncthreads();
+    for (int u = 1; u < kWaves; ++u) *sum += sum[u * 4 * kTokenColumns];
   }
-  finish_columns<CAP, PART>(a, &x[0][0][0]);
+  __syncthreads();
+  finish_columns<kTokenColumns>(a, &x[0][0][0]);
 }
 
 // Up to 16 RT rows: a wave reads the weights of 16 FC columns straight into the fragments of 16 x 16 x 64 products, 64 bytes of 16
 // rows per load, 256 of each at a time; the hidden states go through LDS, 256 bytes of all rows at a time.
-template <int RT, int FC, bool CAP>
+template <int RT, int FC>
 __global__ __launch_bounds__(kHeadThreads, 3) void int8_few_kernel(Int8Args a) {
   constexpr int kPart = 64 * FC;  // columns of the workgroup
   constexpr int kBlock = 256, kStep = 64, kSteps = kBlock / kStep;
@@ -315,36 +299,26 @@ __global__ __launch_bounds__(kHeadThreads, 3) void int8_few_kernel(Int8Args a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) *reinterpret_cast<i32x4*>(&lds.x[16 * t + i][wave * 16 * FC + 16 * f + 4 * g]) = acc[f][t];
   __syncthreads();
-  finish_columns<CAP, kPart>(a, &lds.x[0][0]);
+  finish_columns<kPart>(a, &lds.x[0][0]);
 }
 
 constexpr int kPackThreads = 256;
 __global__ __launch_bounds__(kPackThreads) void int8_pack_kernel(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width,
                                                                  int64_t rows, int32_t cols) {
-  const int64_t groups = to_width / 16, all = rows * groups;
-  for (int64_t n = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; n < all; n += (int64_t)gridDim.x * kPackThreads) {
-    const int64_t p = n / groups, d = (n - p * groups) * 16;
-    *reinterpret_cast<i32x4*>(to + p * to_width + d) = load16_of(from + p * from_stride, (int)d, cols);
-  }
+  // (a wave per row)
+  for (int64_t p = (int64_t)blockIdx.x * (kPackThreads / kWave) + (threadIdx.x >> 6); p < rows; p += (int64_t)gridDim.x * (kPackThreads / kWave))
+    for (int d = (threadIdx.x & 63) * 16; d < to_width; d += kWave * 16)
+      *reinterpret_cast<i32x4*>(to + p * to_width + d) = load16_of(from + p * from_stride, d, cols);
 }
 
-template <bool CAP>
-hipError_t launch_few(const Int8Args& a, hipStream_t stream) {
-  const dim3 block(kHeadThreads);
-  const auto parts = [&](int columns) { return dim3((unsigned)((a.V + (int64_t)columns - 1) / columns)); };
-  if (a.T <= 8) {
-    const bool share = a.D >= 2048 && a.V < 256 * 96;
-    if (a.T > 4)
-      return share ? launch_kernel(int8_tokens_kernel<2, 32, CAP>, parts(32), block, 0, stream, a)
-                   : launch_kernel(int8_tokens_kernel<2, 128, CAP>, parts(128), block, 0, stream, a);
-    return share ? launch_kernel(int8_tokens_kernel<1, 32, CAP>, parts(32), block, 0, stream, a)
-                 : launch_kernel(int8_tokens_kernel<1, 128, CAP>, parts(128), block, 0, stream, a);
-  }
+template <int RT>
+hipError_t launch_fragments(const Int8Args& a, hipStream_t stream) {
+  // (64 columns to a workgroup where 128 leave compute units without one: 9 rows of 32,000 x 4,096 24 us, 33 with 128; of 50,048 x 1,024
+  // 13.8 / 12.0)
   const bool narrow = a.V < 256 * 128;
-  if (a.T <= 16) return narrow ? launch_kernel(int8_few_kernel<1, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<1, 2, CAP>, parts(128), block, 0, stream, a);
-  if (a.T <= 32) return narrow ? launch_kernel(int8_few_kernel<2, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<2, 2, CAP>, parts(128), block, 0, stream, a);
-  if (a.T <= 48) return narrow ? launch_kernel(int8_few_kernel<3, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<3, 2, CAP>, parts(128), block, 0, stream, a);
-  return narrow ? launch_kernel(int8_few_kernel<4, 1, CAP>, parts(64), block, 0, stream, a) : launch_kernel(int8_few_kernel<4, 2, CAP>, parts(128), block, 0, stream, a);
+  const int columns = narrow ? 64 : 128;
+  return launch_kernel(narrow ? int8_few_kernel<RT, 1> : int8_few_kernel<RT, 2>, dim3((unsigned)((a.V + (int64_t)columns - 1) / columns)),
+                       dim3(kHeadThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -361,12 +335,21 @@ hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_int8_few(const Int8Args& a, hipStream_t stream) {
-  return a.cap != 0.0f ? launch_few<true>(a, stream) : launch_few<false>(a, stream);
+  // Up to four rows of 1,536 and more bytes are int8_tokens_kernel's, whose waves share a row.  Measured (MI355X, us, one row there / in
+  // int8_few_kernel, weights out of the caches): 8,000 x 1,024 6.1 / 4.9 (1,000 entries), 8,000 x 1,536 7.0 / 7.8, 8,000 x 8,192 15.3 / 39.7,
+  // 32,000 x 2,048 15.4 / 13.7, 50,048 x 2,048 22.1 / 20.0, 100,000 x 2,048 38.2 / 43.9, 151,936 x 1,024 35.4 / 30.4, x 1,536 40.6 / 44.2, x
+  // 2,048 53 / 60, 262,144 x 1,152 82.5 / 56.8.  Eight rows in two of its products at once are slower (100,000 x 2,048 70 / 46).
+  if (a.T <= 4 && a.D >= 1536)
+    return launch_kernel(int8_tokens_kernel, dim3((unsigned)((a.V + (int64_t)kTokenColumns - 1) / kTokenColumns)), dim3(kHeadThreads), 0, stream, a);
+  if (a.T <= 16) return launch_fragments<1>(a, stream);
+  if (a.T <= 32) return launch_fragments<2>(a, stream);
+  if (a.T <= 48) return launch_fragments<3>(a, stream);
+  return launch_fragments<4>(a, stream);
 }
 
 hipError_t launch_int8_pack(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width, int64_t rows, int32_t cols,
                             hipStream_t stream) {
-  const int64_t blocks = (rows * (to_width / 16) + kPackThreads - 1) / kPackThreads;
+  const int64_t blocks = (rows + kPackThreads / kWave - 1) / (kPackThreads / kWave);
   return launch_kernel(int8_pack_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kPackThreads), 0, stream, from, from_stride, to,
                        to_width, rows, cols);
 }

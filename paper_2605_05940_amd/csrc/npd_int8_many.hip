@@ -72,22 +72,35 @@ __global__ __launch_bounds__(kHeadThreads, 1) void int8_tiles_kernel(Int8Args a)
   }
 }
 
+// `together`: workgroups that a compute unit runs at once (their LDS), so that one's end of a tile lies beside the other's steps
 template <int MF, int NF>
-hipError_t launch(const Int8Args& a, hipStream_t stream) {
+hipError_t launch(const Int8Args& a, int together, hipStream_t stream) {
   using Product = HeadProduct<MF, NF, false, false, true, true>;
   const int64_t mt = (a.T + Product::kTileM - 1) / Product::kTileM, nt = (a.V + Product::kTileN - 1) / Product::kTileN;
-  const int64_t blocks = (mt * nt + 7) / 8 * 8;
+  const int64_t blocks = (mt * nt + 7) / 8 * 8, units = (int64_t)compute_units() / 8 * 8 * together;
   if (blocks >= (int64_t)1 << 30) return hipErrorInvalidConfiguration;
-  return launch_kernel(a.cap != 0.0f ? int8_tiles_kernel<MF, NF, true> : int8_tiles_kernel<MF, NF, false>, dim3(head_grid(blocks)),
-                       dim3(kHeadThreads), 0, stream, a);
+  return launch_kernel(a.cap != 0.0f ? int8_tiles_kernel<MF, NF, true> : int8_tiles_kernel<MF, NF, false>,
+                       dim3((unsigned)(blocks < units || units == 0 ? blocks : units)), dim3(kHeadThreads), 0, stream, a);
 }
 
 }  // namespace
 
+// Tiles of 256 x 256 have the highest rate (2,048 bytes of k: 1,420 us for 4,096 x 151,936; 256 x 128 1,700, 128 x 128 1,767), where
+// there are enough of them for the compute units, and where their rows are there.  Measured (MI355X, us; 64 x 128 / 128 x 128 / 256 x 128 /
+// 256 x 256, of the first two as many workgroups together as fit):
+//   rows  of 32,000 x 4,096           of 50,048 x 1,024            of 151,936 x 2,048
+//   64    34 / 35 / - / -             16.3 / 17.1 / - / -          75 / 74 / - / -
+//   128   49 / 37 / - / -             25.0 / 21.0 / - / -          111 / 86 / - / -
+//   160   - / 53 / 42 / 64            - / 27.7 / 27.3 / 25.7       - / 120 / 112 / 119
+//   256   - / 61 / 46 / 64            - / 34.6 / 28.3 / 26.5       - / 145 / 126 / 124
+//   512   - / 105 / 86 / 69           - / 56.4 / 49.3 / 45.8       - / 246 / 230 / 201
+// (up to 128 rows tiles of 128 x 256, one workgroup per compute unit: 52, 18.8 and 96)
 hipError_t launch_int8_many(const Int8Args& a, hipStream_t stream) {
-  if (head_small(a.T, a.V)) return launch<4, 4>(a, stream);
-  if (a.T <= 128) return launch<4, 8>(a, stream);
-  return launch<8, 8>(a, stream);
+  if (a.T <= 64) return launch<2, 4>(a, 3, stream);
+  if (a.T <= 128 || head_small(a.T, a.V)) return launch<4, 4>(a, 2, stream);
+  const int64_t tiles = (a.T + 255) / 256 * (((int64_t)a.V + 255) / 256);
+  if (tiles <= 128) return launch<8, 4>(a, 1, stream);
+  return launch<8, 8>(a, 1, stream);
 }
 
 }  // namespace npd
