@@ -158,7 +158,7 @@ __device__ __forceinline__ void finish_columns(const Int8Args& a, const int* x) 
 // load of a wave is 256 consecutive bytes of each of four rows of the weights, read past the caches; the four waves of a workgroup
 // have the same 32 columns and every fourth block of k.  Workgroups begin at different places of their rows and wrap around (rows of
 // a power of two of bytes would else be read out of few memory channels).
-__global__ __launch_bounds__(kHeadThreads, 5) void int8_tokens_kernel(Int8Args a) {
+__global__ __launch_bounds__(kHeadThreads, 4) void int8_tokens_kernel(Int8Args a) {
   constexpr int kWaves = kHeadThreads / kWave, G = 8;
   constexpr int kBlock = 256;  // bytes of k per load
   __shared__ __attribute__((aligned(16))) int x[kWaves][4][kTokenColumns];
