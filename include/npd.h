@@ -626,12 +626,17 @@ typedef struct {
  *   dev_status  int32 [1] or NULL: a setting or random number out of range (NPD_DEV_BAD_SAMPLING), NaN, +inf or nothing but
  *               -inf among a row's logits (NPD_DEV_BAD_LOGITS) give token -1, NaN and kept 0
  *
- * Weights and their sums are 64-bit; nothing depends on the order in which a row is read: reproducible.  No workspace.
+ *   workspace  device, npd_sample_workspace_bytes(desc) bytes, 256-byte aligned (else NPD_ERR_WORKSPACE), as for the head's calls:
+ *               calls of few rows share a row among several workgroups through it.  With NULL or fewer bytes they do not, and are slower
+ *
+ * Weights and their sums are 64-bit; nothing depends on the order in which a row is read, nor on the workspace: reproducible.
  */
 npd_status npd_sample_tokens(const npd_sample_desc* desc, const void* logits, const float* uniform,
                              const uint8_t* loss_mask, const float* temperature, const int32_t* top_k, const float* top_p,
                              const float* min_p, int32_t* token, float* logprob, float* nll, int32_t* kept,
-                             int32_t* dev_status, void* stream);
+                             int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream);
+/* Host call; 0 is a legal answer (rows enough for every compute unit) and what an invalid desc gets. */
+size_t npd_sample_workspace_bytes(const npd_sample_desc* desc);
 
 #ifdef __cplusplus
 }

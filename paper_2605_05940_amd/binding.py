@@ -37,7 +37,7 @@ EXPORTS = ("npd_version", "npd_status_string", "npd_workspace_bytes", "npd_kd_lo
            "npd_kept_workspace_bytes", "npd_kd_loss_fwd_bwd_kept", "npd_head_workspace_bytes",
            "npd_head_workspace_bytes_preferred", "npd_head_loss_fwd_bwd", "npd_head_logits", "npd_head_logits_bwd",
            "npd_layer_norm", "npd_layer_norm_bwd", "npd_layer_norm_workspace_bytes", "npd_quantize_rows", "npd_head_logits_int8",
-           "npd_sample_tokens")
+           "npd_sample_tokens", "npd_sample_workspace_bytes")
 
 
 class NpdError(RuntimeError):
@@ -146,7 +146,8 @@ def load() -> ctypes.CDLL:
                   "npd_layer_norm_workspace_bytes": (size, [ctypes.POINTER(NormDesc)]),
                   "npd_quantize_rows": (ctypes.c_int, [i64, i32, i64, i64] + [_vp] * 4),
                   "npd_head_logits_int8": (ctypes.c_int, [ctypes.POINTER(HeadDesc)] + [_vp] * 7 + [size, _vp]),
-                  "npd_sample_tokens": (ctypes.c_int, [ctypes.POINTER(SampleDesc)] + [_vp] * 13)}
+                  "npd_sample_tokens": (ctypes.c_int, [ctypes.POINTER(SampleDesc)] + [_vp] * 13 + [size, _vp]),
+                  "npd_sample_workspace_bytes": (size, [ctypes.POINTER(SampleDesc)])}
         for name, (result, arguments) in around.items():
             if here or hasattr(L, name):
                 getattr(L, name).restype = result
@@ -718,25 +719,33 @@ def npd_head_logits_int8(hidden: torch.Tensor, hidden_scale: torch.Tensor, weigh
     _check(L.npd_head_logits_int8(*args, ws, n, _stream()))
 
 
+def npd_sample_workspace_bytes(n_tokens: int, vocab: int) -> int:
+    """Bytes of workspace with which ``npd_sample_tokens`` shares the rows of a call of few among several workgroups (0: it does not)."""
+    return int(load().npd_sample_workspace_bytes(ctypes.byref(SampleDesc(n_tokens, _width32(vocab), _width32(vocab), 0, 1.0, 0, 1.0, 0.0))))
+
+
 def npd_sample_tokens(logits: torch.Tensor, uniform: torch.Tensor, *, tokens_out: torch.Tensor, temperature=1.0, top_k=0,
                       top_p=1.0, min_p=0.0, loss_mask: Optional[torch.Tensor] = None, logprob_out: Optional[torch.Tensor] = None,
                       nll_out: Optional[torch.Tensor] = None, kept_out: Optional[torch.Tensor] = None,
-                      dev_status: Optional[torch.Tensor] = None) -> None:
+                      dev_status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """Enqueue the drawing of a token from every row of bf16 logits by the random numbers ``uniform`` in [0, 1) (see
     ``npd_sample_tokens`` in npd.h).  ``temperature``, ``top_p``, ``min_p`` (numbers, or fp32 tensors of one per row) and ``top_k``
     (int32) truncate the distribution; 0 or None for no ``top_k``, 1 for no ``top_p``, 0 for no ``min_p``, temperature 0 for the largest
-    logit."""
+    logit.  ``workspace``: a uint8 tensor (``npd_sample_workspace_bytes``; a smaller one is not used); without it the call takes a block
+    from torch's allocator for as long as it is being enqueued."""
     T, V = logits.shape
     top_k = 0 if top_k is None else top_k
     settings = (temperature, top_k, top_p, min_p)
     rows = [s if isinstance(s, torch.Tensor) else None for s in settings]
     numbers = [n if r is None else 0 for n, r in zip(settings, rows)]
-    _on_current_device(logits, uniform, tokens_out, *rows, loss_mask, logprob_out, nll_out, kept_out, dev_status)
-    desc = SampleDesc(T, _pitch(logits), _width32(V), 0, numbers[0], max(-1, _width32(numbers[1])), numbers[2], numbers[3])
+    _on_current_device(logits, uniform, tokens_out, *rows, loss_mask, logprob_out, nll_out, kept_out, dev_status, workspace)
+    desc = ctypes.byref(SampleDesc(T, _pitch(logits), _width32(V), 0, numbers[0], max(-1, _width32(numbers[1])), numbers[2], numbers[3]))
     f32, i32 = torch.float32, torch.int32
-    _check(load().npd_sample_tokens(
-        ctypes.byref(desc), _matrix("logits", logits, (T, V)), _array("uniform", uniform, T, f32),
-        _array("loss_mask", loss_mask, T, torch.uint8), _array("temperature", rows[0], T, f32), _array("top_k", rows[1], T, i32),
-        _array("top_p", rows[2], T, f32), _array("min_p", rows[3], T, f32), _array("tokens_out", tokens_out, T, i32),
-        _array("logprob_out", logprob_out, T, f32), _array("nll_out", nll_out, T, f32), _array("kept_out", kept_out, T, i32),
-        _array("dev_status", dev_status, 1, i32), _stream()))
+    args = (desc, _matrix("logits", logits, (T, V)), _array("uniform", uniform, T, f32),
+            _array("loss_mask", loss_mask, T, torch.uint8), _array("temperature", rows[0], T, f32), _array("top_k", rows[1], T, i32),
+            _array("top_p", rows[2], T, f32), _array("min_p", rows[3], T, f32), _array("tokens_out", tokens_out, T, i32),
+            _array("logprob_out", logprob_out, T, f32), _array("nll_out", nll_out, T, f32), _array("kept_out", kept_out, T, i32),
+            _array("dev_status", dev_status, 1, i32))
+    L = load()
+    _block, ws, n = _given_or_own(workspace, lambda: L.npd_sample_workspace_bytes(desc))
+    _check(L.npd_sample_tokens(*args, ws, n, _stream()))

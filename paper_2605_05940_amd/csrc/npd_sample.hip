@@ -605,10 +605,18 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   return s.found;
 }
 
-// A row by passes over it (not inlined: the registers of the rows that are counted are the ones that matter); false: not a row to
-// draw from.
-__device__ __attribute__((noinline)) bool by_passes(const Row row, const Settings q, bool greedy, bool nll, Shared& s, Choice* c, double* sum1,
-                                                    double* top) {
+// A row's outputs.
+__device__ __forceinline__ void put(const SampleArgs& a, int64_t r, int token, double logprob, double nll, uint32_t kept, int status) {
+  if (threadIdx.x != 0) return;
+  a.token[r] = token;
+  if (a.logprob) a.logprob[r] = (float)logprob;
+  if (a.nll) a.nll[r] = (float)nll;
+  if (a.kept) a.kept[r] = (int32_t)kept;
+  if (status && a.status) atomicOr(a.status, status);
+}
+
+// A row by passes over it.  (Not inlined: the registers of the rows that are counted are the ones that matter.)
+__device__ __attribute__((noinline)) void draw_by_passes(const SampleArgs a, int64_t r, const Row row, const Settings q, bool greedy, Shared& s) {
   uint32_t most = 0, bad = 0;
   each_entry(row, [&](int, uint32_t b) {
     const uint32_t k = key_of(b);
@@ -624,55 +632,32 @@ __device__ __attribute__((noinline)) bool by_passes(const Row row, const Setting
   most = s.first;
   bad = s.odd;
   __syncthreads();
-  if (bad || most < kLowest) return false;
+  if (bad || most < kLowest) {
+    put(a, r, -1, __builtin_nan(""), __builtin_nan(""), 0, NPD_DEV_BAD_LOGITS);
+    return;
+  }
   Passes passes{row, s, most, 0, value_of(most), 0.0, 0.0};
   passes.begin(q.per);
-  *c = choose(passes, q, greedy);
-  *sum1 = !nll ? 1.0 : q.tau == 1.0 ? passes.sum : passes.sum_at(1.0);
-  *top = passes.top;
-  return true;
+  const Choice c = choose(passes, q, greedy);
+  const double sum1 = !a.nll ? 1.0 : q.tau == 1.0 ? passes.sum : passes.sum_at(1.0);
+  const int token = find_entry(row, c.key, c.which, s);
+  put(a, r, token, c.logprob, log(sum1) + (passes.top - (double)value_of(c.key)), c.kept, 0);
 }
 
 // (a workgroup has one row: in a loop over rows what only threadIdx decides would be kept in registers from one to the next)
 constexpr int64_t kGrid = 65536;  // workgroups along x
-__global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
-  __shared__ Shared s;
-  const int64_t r = (int64_t)blockIdx.y * kGrid + blockIdx.x;
-  if (r >= a.T) return;
-  auto put = [&](int token, double logprob, double nll, uint32_t kept, int status) {
-    if (threadIdx.x != 0) return;
-    a.token[r] = token;
-    if (a.logprob) a.logprob[r] = (float)logprob;
-    if (a.nll) a.nll[r] = (float)nll;
-    if (a.kept) a.kept[r] = (int32_t)kept;
-    if (status && a.status) atomicOr(a.status, status);
-  };
-  const double nan = __builtin_nan("");
-  if (a.mask && !a.mask[r]) {
-    put(-1, 0.0, 0.0, 0, 0);
-    return;
-  }
-  const float tau = a.taus ? a.taus[r] : a.tau, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p;
-  const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
-  const float u = a.u[r];
-  if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
-      !(u >= 0.0f && u < 1.0f)) {
-    put(-1, nan, nan, 0, NPD_DEV_BAD_SAMPLING);
-    return;
-  }
-  const bool greedy = tau == 0.0f;
-  const double t = greedy ? 1.0 : (double)tau;
-  const Settings q = {t, 1.0 / t, top_p, min_p, u, (uint32_t)top_k};
-  const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
 
+__device__ __forceinline__ void begin_counts(Shared& s) {
   for (int i = threadIdx.x; i < (int)(sizeof(s.counts) / 16); i += kThreads) reinterpret_cast<uint4*>(s.counts)[i] = make_uint4(0, 0, 0, 0);
   if (threadIdx.x < kNear) {
     s.near_keys[threadIdx.x] = threadIdx.x ? kBelowNear : 0x8000;
     s.near_counts[threadIdx.x] = 0;
   }
   if (threadIdx.x == 0) s.big = s.odd = s.near = 0;
-  begin_exponentials(s);
-  __syncthreads();
+}
+
+// Counts a row's entries; zero in the first of near_counts, what else is closer to zero than the counters' in near_list.
+__device__ __forceinline__ void count_entries(const Row& row, Shared& s) {
   uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
   auto other = [&](uint32_t b) {
     const uint32_t size = b & 0x7fff;
@@ -723,11 +708,117 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
   if (big) atomicAdd(&s.big, big);
   if (odd) s.odd = 1;
   __syncthreads();
-  big = s.big;
-  odd = s.odd || s.near >= kNear;
+}
+
+// Rows of calls that have few of them are counted in parts, by a workgroup each.  What a part leaves in the workspace:
+struct Part {
+  uint32_t counts[kOthers];
+  uint32_t zeros, near, big, odd;
+  uint32_t near_list[kNear];
+};
+static_assert(sizeof(Part) == kSamplePartBytes, "");
+
+// entries [first, end) of a row are its part i
+struct Span {
+  int first, end;
+};
+__device__ __forceinline__ Span part_of(int V, int parts, int i) {
+  const int each = ((V + parts - 1) / parts + 7) / 8 * 8;
+  const int first = i * each < V ? i * each : V;
+  return Span{first, V - first < each ? V : first + each};
+}
+__device__ __forceinline__ Row row_part(const uint16_t* p, const Span& at) {
+  const int n = at.end - at.first;
+  return Row{p + at.first, n, row_split(p + at.first, n, true)};
+}
+
+__global__ __launch_bounds__(kThreads, 8) void sample_count_kernel(SampleArgs a) {
+  __shared__ Shared s;
+  const int64_t r = blockIdx.y;
+  if (a.mask && !a.mask[r]) return;
+  begin_counts(s);
+  __syncthreads();
+  count_entries(row_part(a.x + r * a.stride, part_of(a.V, a.parts, blockIdx.x)), s);
+  Part& part = reinterpret_cast<Part*>(a.workspace)[r * a.parts + blockIdx.x];
+  for (int i = threadIdx.x; i < (int)kOthers / 4; i += kThreads) reinterpret_cast<uint4*>(part.counts)[i] = reinterpret_cast<uint4*>(s.counts)[i];
+  if (threadIdx.x < kNear) part.near_list[threadIdx.x] = s.near_list[threadIdx.x];
+  if (threadIdx.x == 0) {
+    part.zeros = s.near_counts[0];
+    part.near = s.near;
+    part.big = s.big;
+    part.odd = s.odd;
+  }
+}
+
+// The counts of a row out of those of its parts, all threads.
+__device__ __forceinline__ void join_parts(const Part* parts, int n, Shared& s) {
+  for (int i = threadIdx.x; i < (int)kOthers / 4; i += kThreads) {
+    uint4 sum = make_uint4(0, 0, 0, 0);
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const uint4 v = reinterpret_cast<const uint4*>(parts[p].counts)[i];
+      sum = make_uint4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+    }
+    reinterpret_cast<uint4*>(s.counts)[i] = sum;
+  }
+  uint32_t zeros = 0, near = 0, big = 0, odd = 0;
+#pragma unroll 4
+  for (int p = 0; p < n; ++p) {
+    zeros += parts[p].zeros;
+    const uint32_t here = parts[p].near;
+    if (near + here < kNear && threadIdx.x < here) s.near_list[near + threadIdx.x] = parts[p].near_list[threadIdx.x];
+    near = near + here < kNear ? near + here : kNear;  // (no more than fit are looked at)
+    big += parts[p].big;
+    odd |= parts[p].odd;
+  }
+  if (threadIdx.x < kNear) {
+    s.near_keys[threadIdx.x] = threadIdx.x ? kBelowNear : 0x8000;
+    s.near_counts[threadIdx.x] = threadIdx.x ? 0 : zeros;
+  }
+  if (threadIdx.x == 0) {
+    s.near = near;
+    s.big = big;
+    s.odd = odd;
+  }
+  __syncthreads();
+}
+
+// SPLIT: the row has been counted, in parts
+template <bool SPLIT>
+__global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleArgs a) {
+  __shared__ Shared s;
+  const int64_t r = (int64_t)blockIdx.y * kGrid + blockIdx.x;
+  if (r >= a.T) return;
+  const double nan = __builtin_nan("");
+  if (a.mask && !a.mask[r]) {
+    put(a, r, -1, 0.0, 0.0, 0, 0);
+    return;
+  }
+  const float tau = a.taus ? a.taus[r] : a.tau, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p;
+  const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+  const float u = a.u[r];
+  if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
+      !(u >= 0.0f && u < 1.0f)) {
+    put(a, r, -1, nan, nan, 0, NPD_DEV_BAD_SAMPLING);
+    return;
+  }
+  const bool greedy = tau == 0.0f;
+  const double t = greedy ? 1.0 : (double)tau;
+  const Settings q = {t, 1.0 / t, top_p, min_p, u, (uint32_t)top_k};
+  const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
+  const Part* parts = SPLIT ? reinterpret_cast<const Part*>(a.workspace) + r * a.parts : nullptr;
+
+  begin_exponentials(s);
+  if constexpr (SPLIT) {
+    join_parts(parts, a.parts, s);
+  } else {
+    begin_counts(s);
+    __syncthreads();
+    count_entries(row, s);
+  }
+  const uint32_t big = s.big;
+  const bool odd = s.odd || s.near >= kNear;
   if (s.near && !odd) order_near(s);
-  Choice c;
-  double sum1 = 1.0, log1, top;  // of the weights at temperature 1
   uint32_t n[kEach];
   read_counts(s, thread_of_phase(), n);
   const uint32_t top_key = largest_counted(s, n);
@@ -736,38 +827,61 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(SampleArgs a) {
   // 64 temperatures above -256, and are none that a min-p would keep.
   const double room = counted_top + 256.0;
   const bool apart = room >= 64.0 && room >= 64.0 * q.tau && (q.min_p == 0.0 || room > q.tau * (1.0 - log(q.min_p)));
-  if (!odd && top_key && (!big || apart)) {
-    weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
-    if (threadIdx.x < kWave) {
-      const Counted counted{s, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
-      Choice mine = choose(counted, q, greedy);
-      if (mine.kept == counted.all && big && !greedy && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
-        const uint32_t all = counted.all + big;
-        mine.kept = q.top_k > 0 && q.top_k < all ? q.top_k : all;
-      }
-      if (threadIdx.x == 0) s.choice = mine;
-    }
-    if (threadIdx.x == kWave) s.log1 = log(sum1);  // (beside the search)
-    __syncthreads();
-    c = s.choice;
-    log1 = s.log1;
-    top = counted_top;
-  } else {
-    if (!by_passes(row, q, greedy, a.nll != nullptr, s, &c, &sum1, &top)) {
-      put(-1, nan, nan, 0, NPD_DEV_BAD_LOGITS);
-      return;
-    }
-    log1 = log(sum1);
+  if (odd || !top_key || (big && !apart)) {
+    draw_by_passes(a, r, row, q, greedy, s);
+    return;
   }
-  const int token = find_entry(row, c.key, c.which, s);
-  put(token, c.logprob, log1 + (top - (double)value_of(c.key)), c.kept, 0);
+  double sum1;  // of the weights at temperature 1
+  weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
+  if (threadIdx.x < kWave) {
+    const Counted counted{s, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
+    Choice mine = choose(counted, q, greedy);
+    if (mine.kept == counted.all && big && !greedy && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
+      const uint32_t all = counted.all + big;
+      mine.kept = q.top_k > 0 && q.top_k < all ? q.top_k : all;
+    }
+    if (threadIdx.x == 0) s.choice = mine;
+  }
+  if (threadIdx.x == kWave) s.log1 = log(sum1);  // (beside the search)
+  __syncthreads();
+  const Choice c = s.choice;
+  int token;
+  if constexpr (SPLIT) {
+    // the part that has the entry, where the value has a counter
+    Span where = {0, a.V};
+    uint32_t which = c.which;
+    const uint32_t bits = c.key & 0x8000 ? c.key & 0x7fff : ~c.key & 0x7fff, i = 2 * (bits - kFirst) + (c.key & 0x8000 ? 0 : 1);
+    if (bits >= kFirst) {
+      for (int p = 0; p < a.parts; ++p) {
+        const uint32_t here = parts[p].counts[i];
+        if (which < here) {
+          where = part_of(a.V, a.parts, p);
+          break;
+        }
+        which -= here;
+      }
+    }
+    token = where.first + find_entry(row_part(row.p, where), c.key, which, s);
+  } else {
+    token = find_entry(row, c.key, c.which, s);
+  }
+  put(a, r, token, c.logprob, s.log1 + (counted_top - (double)value_of(c.key)), c.kept, 0);
 }
 
 }  // namespace
 
+// As many parts as give every compute unit one and leave each 16,384 entries.
+int sample_parts(int64_t T, int32_t V) {
+  const int64_t most = 256 / T < kSampleParts ? 256 / T : kSampleParts, some = V / 16384;
+  return (int)(most < 2 || some < 2 ? 1 : most < some ? most : some);
+}
+
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
   const int64_t rows = a.T < kGrid ? a.T : kGrid;
-  return launch_kernel(sample_kernel, dim3((unsigned)rows, (unsigned)((a.T + kGrid - 1) / kGrid)), dim3(kThreads), 0, stream, a);
+  const dim3 grid((unsigned)rows, (unsigned)((a.T + kGrid - 1) / kGrid));
+  if (a.parts < 2) return launch_kernel(sample_kernel<false>, grid, dim3(kThreads), 0, stream, a);
+  const hipError_t e = launch_kernel(sample_count_kernel, dim3((unsigned)a.parts, (unsigned)a.T), dim3(kThreads), 0, stream, a);
+  return e != hipSuccess ? e : launch_kernel(sample_kernel<true>, grid, dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace npd

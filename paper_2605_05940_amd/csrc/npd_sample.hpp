@@ -23,7 +23,13 @@ struct SampleArgs {
   float *logprob, *nll;  // or null
   int32_t* kept;
   int32_t* status;
+  int32_t parts;    // of a row that workgroups count each, sample_parts(), 1: none
+  void* workspace;  // kSamplePartBytes for each part of each row
 };
+// Parts of a call's rows that workgroups of their own count, 1 where there are rows enough
+constexpr int kSampleParts = 8;
+constexpr size_t kSamplePartBytes = 4 * (7936 + 4 + 256);
+int sample_parts(int64_t T, int32_t V);
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream);
 
 }  // namespace npd

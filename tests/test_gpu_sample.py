@@ -32,6 +32,10 @@ def call(x, u, **settings):
 def check(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     got, status = call(x, u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
     assert status == 0
+    if npd.npd_sample_workspace_bytes(*x.shape):  # rows in parts, and whole: the same bit by bit
+        whole, status = call(x, u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p,
+                             workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+        assert status == 0 and all((whole[n] == got[n]).all() for n in got)
     T = x.shape[0]
 
     def setting(v):
@@ -54,7 +58,7 @@ SETTINGS = [dict(), dict(temperature=0.7), dict(temperature=0.0), dict(top_k=1),
 
 @pytest.mark.parametrize("settings", SETTINGS, ids=str)
 @pytest.mark.parametrize("T,V,offset,pad", [(1, 1, 0, 0), (5, 2, 1, 0), (9, 7, 3, 2), (40, 100, 0, 0), (33, 1000, 1, 1), (17, 4099, 0, 0),
-                                            (12, 8192, 0, 0), (10, 32001, 5, 0), (6, 50003, 0, 0), (3, 151936, 0, 64)])
+                                            (12, 8192, 0, 0), (10, 32001, 5, 0), (5, 32768, 0, 0), (2, 65537, 1, 2), (6, 50003, 0, 0), (3, 151936, 0, 64)])
 def test_against_the_definition(T, V, offset, pad, settings):
     check(*logits(T, V, offset=offset, pad=pad), **settings)
 
@@ -66,18 +70,20 @@ def test_logits_of_every_size(spread):
         check(*logits(8, 3000, spread=spread), **settings)
 
 
+@pytest.mark.parametrize("V", [2000, 40003])
 @pytest.mark.parametrize("n", [1, 2, 8, 9, 254, 255, 256, 300])
-def test_entries_close_to_zero(n):
+def test_entries_close_to_zero(n, V):
     """Numbers below 2^-23, some of them equal, zeros of both signs among them: listed, or too many for the list."""
-    x, u = logits(24, 2000, spread=0.3)
+    x, u = logits(24, V, spread=0.3)
     g = torch.Generator(device=DEV).manual_seed(n)
     tiny = torch.randint(1, 1 + 3 * n, (24, n), device=DEV, generator=g) * torch.randint(0, 2, (24, n), device=DEV, generator=g).mul(2).sub(1)
-    x[:, 100:100 + n] = tiny.float() * 2.0 ** -40
+    x[:, torch.arange(100, 100 + n) * (V // 1000) % V] = (tiny.float() * 2.0 ** -40).to(torch.bfloat16)
     x[::2, 1900:1907] = 0.0
     x[::3, 1907:1911] = -0.0
     for settings in (dict(), dict(top_k=1000), dict(temperature=2.0 ** -40), dict(temperature=2.0 ** -39, min_p=0.2, top_p=0.9), dict(top_p=0.5)):
         check(x, u, **settings)
-    x[:, :100], x[:, 100 + n:] = float("-inf"), float("-inf")
+    x.masked_fill_(x.float().abs() > 2.0 ** -23, float("-inf"))
+    x[:, 50] = torch.finfo(torch.bfloat16).tiny
     x[::2, 1900] = 0.0
     for settings in (dict(), dict(temperature=2.0 ** -39), dict(temperature=2.0 ** -39, min_p=0.7), dict(temperature=0.0), dict(min_p=1.0)):
         check(x, u, **settings)
@@ -119,7 +125,7 @@ def test_zeros_of_either_sign_are_equal():
     check(x, u, temperature=0.0)
 
 
-@pytest.mark.parametrize("V", [64, 3001, 40000])
+@pytest.mark.parametrize("V", [64, 3001, 40000, 120001])
 def test_entries_of_minus_infinity(V):
     x, u = logits(12, V)
     g = torch.Generator(device=DEV).manual_seed(8)
@@ -131,8 +137,9 @@ def test_entries_of_minus_infinity(V):
         check(x, u, **settings)
 
 
-def test_the_lowest_number_as_a_mask():
-    x, u = logits(8, 2000)
+@pytest.mark.parametrize("V", [2000, 33000])
+def test_the_lowest_number_as_a_mask(V):
+    x, u = logits(8, V)
     g = torch.Generator(device=DEV).manual_seed(9)
     x.masked_fill_(torch.rand(x.shape, device=DEV, generator=g) < 0.7, torch.finfo(torch.bfloat16).min)
     x[4:] = torch.finfo(torch.bfloat16).min  # nothing else left: equal entries
@@ -140,8 +147,9 @@ def test_the_lowest_number_as_a_mask():
         check(x, u, **settings)
 
 
-def test_numbers_below_minus_256():
-    x, u = logits(8, 1500)
+@pytest.mark.parametrize("V", [1500, 36000])
+def test_numbers_below_minus_256(V):
+    x, u = logits(8, V)
     x[:, ::3] = -400.0
     x[4:] -= 250.0  # the rest not far above
     for settings in SETTINGS + [dict(temperature=100.0), dict(top_k=1400), dict(min_p=1e-38), dict(temperature=30.0, min_p=1e-30)]:
@@ -167,8 +175,9 @@ def test_settings_of_every_row():
     check(x, u, temperature=rows["temperature"], top_k=5)
 
 
-def test_rows_that_are_not_drawn_from():
-    x, u = logits(10, 700)
+@pytest.mark.parametrize("V", [700, 50000])
+def test_rows_that_are_not_drawn_from(V):
+    x, u = logits(10, V)
     mask = torch.ones(10, dtype=torch.uint8, device=DEV)
     mask[3] = 0
     x[3] = float("nan")
@@ -180,16 +189,17 @@ def test_rows_that_are_not_drawn_from():
     assert all((got[n][others] == clean[n][others]).all() for n in got)
 
 
+@pytest.mark.parametrize("V", [900, 50000])
 @pytest.mark.parametrize("bad", ["nan", "-nan", "inf", "empty"])
-def test_logits_that_cannot_be_drawn_from(bad):
-    x, u = logits(6, 900)
+def test_logits_that_cannot_be_drawn_from(bad, V):
+    x, u = logits(6, V)
     clean, _ = call(x, u)
     if bad == "empty":
         x[2] = float("-inf")
     else:
-        x[2, 899] = float("inf") if bad == "inf" else float("nan")
+        x[2, V - 1] = float("inf") if bad == "inf" else float("nan")
         if bad == "-nan":
-            x.view(torch.int16)[2, 899] = -1
+            x.view(torch.int16)[2, V - 1] = -1
     got, status = call(x, u)
     assert status == binding.NPD_DEV_BAD_LOGITS
     assert got["tokens_out"][2] == -1 and got["kept_out"][2] == 0 and np.isnan(got["logprob_out"][2]) and np.isnan(got["nll_out"][2])
@@ -242,21 +252,22 @@ def test_offsets_beyond_32_bits():
     check(far, u, top_p=0.8)
 
 
-def test_captured_and_replayed():
-    T, V = 30, 20000
+@pytest.mark.parametrize("T,V", [(30, 20000), (3, 100000)])
+def test_captured_and_replayed(T, V):
+    ws = torch.empty(npd.npd_sample_workspace_bytes(T, V), dtype=torch.uint8, device=DEV)
     sets = [logits(T, V, seed=s) for s in range(3)]
     x, u = (t.clone() for t in sets[0])
     tau = torch.full((T,), 0.8, device=DEV)
     tokens, nll = torch.empty(T, dtype=torch.int32, device=DEV), torch.empty(T, device=DEV)
 
-    def run(x, u, tokens, nll):
-        npd.npd_sample_tokens(x, u, temperature=tau, top_k=100, top_p=0.95, tokens_out=tokens, nll_out=nll)
+    def run(x, u, tokens, nll, **how):
+        npd.npd_sample_tokens(x, u, temperature=tau, top_k=100, top_p=0.95, tokens_out=tokens, nll_out=nll, **how)
 
-    run(x, u, tokens, nll)
+    run(x, u, tokens, nll, workspace=ws)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        run(x, u, tokens, nll)
+        run(x, u, tokens, nll, workspace=ws)
     for s in (1, 0, 2, 1):
         x.copy_(sets[s][0])
         u.copy_(sets[s][1])
@@ -267,8 +278,9 @@ def test_captured_and_replayed():
         assert torch.equal(tokens, want[0]) and torch.equal(nll, want[1])
 
 
-def test_two_streams_at_once():
-    sets = [logits(50, 30000, seed=s) for s in range(2)]
+@pytest.mark.parametrize("T", [50, 5])
+def test_two_streams_at_once(T):
+    sets = [logits(T, 40000, seed=s) for s in range(2)]
     want = [call(x, u, top_p=0.9)[0] for x, u in sets]
     streams = [torch.cuda.Stream() for _ in sets]
     outs = []
@@ -276,7 +288,7 @@ def test_two_streams_at_once():
     for _ in range(3):
         for i, stream in enumerate(streams):
             with torch.cuda.stream(stream):
-                tokens = torch.empty(50, dtype=torch.int32, device=DEV)
+                tokens = torch.empty(T, dtype=torch.int32, device=DEV)
                 npd.npd_sample_tokens(*sets[i], top_p=0.9, tokens_out=tokens)
                 outs.append((i, tokens))
     torch.cuda.synchronize()
