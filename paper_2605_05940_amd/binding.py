@@ -173,6 +173,10 @@ def _load_host(L):
     kept = [getattr(L, name, None) for name in ("npd_kept_workspace_bytes", "npd_kd_loss_fwd_bwd_kept")]
     addresses = [ctypes.cast(f, _vp).value for f in entries + (kept if all(kept) else [])]
     host.bind(_raw_stream, _workspaces, tuple(addresses + [0] * (11 - len(addresses))))
+    around = [getattr(L, name, None) for name in (
+        "npd_layer_norm", "npd_layer_norm_bwd", "npd_layer_norm_workspace_bytes", "npd_quantize_rows", "npd_head_logits_int8",
+        "npd_head_workspace_bytes", "npd_sample_tokens", "npd_sample_workspace_bytes")]
+    host.bind_around_head(tuple(ctypes.cast(f, _vp).value for f in around) if all(around) else (0,) * len(around))
     return host
 
 
@@ -633,6 +637,10 @@ def npd_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, *, y_
                    mean_out: Optional[torch.Tensor] = None, rstd_out: Optional[torch.Tensor] = None) -> None:
     """Enqueue ``y_out = (x - mean) * rstd * weight + bias`` of every row of a bf16 matrix (``rms``: without the mean), and the
     row statistics that the backward pass takes (see ``npd_layer_norm`` in npd.h)."""
+    if _host is not None:
+        st = _host.layer_norm(x, weight, y_out, bias, eps, rms, mean_out, rstd_out)
+        if st >= 0:
+            return _check(st)
     T, D = x.shape
     _on_current_device(x, weight, bias, y_out, mean_out, rstd_out)
     desc = NormDesc(T, _pitch(x), _pitch(y_out), 0, _width32(D), NPD_NORM_RMS if rms else 0, eps)
@@ -664,6 +672,10 @@ def npd_layer_norm_bwd(grad_y: torch.Tensor, x: torch.Tensor, weight: Optional[t
     (see ``npd_layer_norm_bwd`` in npd.h).  ``accumulate``: the gradients of weight and bias are added to what their tensors
     hold.  ``workspace``: a uint8 tensor of at least ``npd_layer_norm_workspace_bytes`` bytes; without it the call takes a block
     from torch's allocator for as long as it is being enqueued."""
+    if _host is not None:
+        st = _host.layer_norm_bwd(grad_y, x, weight, rstd, mean, rms, grad_x, grad_weight, grad_bias, accumulate, workspace)
+        if st >= 0:
+            return _check(st)
     T, D = x.shape
     _on_current_device(grad_y, x, weight, rstd, mean, grad_x, grad_weight, grad_bias, workspace)
     desc = _norm_grad_desc(T, D, (_pitch(x), _pitch(grad_y), _pitch(grad_x)), rms, grad_x is not None, grad_weight is not None,
@@ -694,6 +706,10 @@ def npd_quantize_rows(x: torch.Tensor, *, q_out: torch.Tensor, scale_out: torch.
     """Enqueue ``scale_out = max|x| / 127`` and ``q_out = round(x / scale_out)`` of every row of a bf16 matrix, as 8-bit integers
     (see ``npd_quantize_rows`` in npd.h).  A ``q_out`` whose rows begin on multiples of 16 (a view of a wider tensor where the
     width is none) is read as it is by ``npd_head_logits_int8``."""
+    if _host is not None:
+        st = _host.quantize_rows(x, q_out, scale_out)
+        if st >= 0:
+            return _check(st)
     R, D = x.shape
     _on_current_device(x, q_out, scale_out)
     _check(load().npd_quantize_rows(R, _width32(D), _pitch(x), _pitch(q_out), _matrix("x", x, (R, D)),
@@ -706,6 +722,10 @@ def npd_head_logits_int8(hidden: torch.Tensor, hidden_scale: torch.Tensor, weigh
                          workspace: Optional[torch.Tensor] = None) -> None:
     """Enqueue ``npd_head_logits`` of 8-bit hidden states and weights with a scale for each of their rows (see
     ``npd_head_logits_int8`` in npd.h)."""
+    if _host is not None:
+        st = _host.head_logits_int8(hidden, hidden_scale, weight, weight_scale, logits_out, bias, softcap, workspace)
+        if st >= 0:
+            return _check(st)
     T, D = hidden.shape
     V = weight.shape[0]
     _on_current_device(hidden, hidden_scale, weight, weight_scale, logits_out, bias, workspace)
@@ -733,8 +753,13 @@ def npd_sample_tokens(logits: torch.Tensor, uniform: torch.Tensor, *, tokens_out
     (int32) truncate the distribution; 0 or None for no ``top_k``, 1 for no ``top_p``, 0 for no ``min_p``, temperature 0 for the largest
     logit.  ``workspace``: a uint8 tensor (``npd_sample_workspace_bytes``; a smaller one is not used); without it the call takes a block
     from torch's allocator for as long as it is being enqueued."""
-    T, V = logits.shape
     top_k = 0 if top_k is None else top_k
+    if _host is not None:
+        st = _host.sample_tokens(logits, uniform, tokens_out, temperature, top_k, top_p, min_p, loss_mask, logprob_out, nll_out, kept_out,
+                                 dev_status, workspace)
+        if st >= 0:
+            return _check(st)
+    T, V = logits.shape
     settings = (temperature, top_k, top_p, min_p)
     rows = [s if isinstance(s, torch.Tensor) else None for s in settings]
     numbers = [n if r is None else 0 for n, r in zip(settings, rows)]

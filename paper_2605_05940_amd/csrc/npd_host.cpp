@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <utility>
 #include <vector>
 
 #include "../../include/npd.h"
@@ -36,6 +37,18 @@ struct Entry {
   decltype(&npd_kept_workspace_bytes) kept_bytes;  // null with a library that has no calls on kept records
   decltype(&npd_kd_loss_fwd_bwd_kept) kd_kept;
 };
+// The operators around the head; all null with a library that has none of them.
+struct AroundHead {
+  decltype(&npd_layer_norm) norm;
+  decltype(&npd_layer_norm_bwd) norm_bwd;
+  decltype(&npd_layer_norm_workspace_bytes) norm_bytes;
+  decltype(&npd_quantize_rows) quantize;
+  decltype(&npd_head_logits_int8) int8;
+  decltype(&npd_head_workspace_bytes) head_bytes;
+  decltype(&npd_sample_tokens) sample;
+  decltype(&npd_sample_workspace_bytes) sample_bytes;
+};
+AroundHead around;                    // written by bind_around_head(), likewise
 Entry lib;                            // written by bind() under the interpreter lock, before any call
 PyObject* raw_stream = nullptr;       // torch's current raw stream of a device index
 PyObject* workspaces = nullptr;       // the buffers it keeps, by device index
@@ -372,6 +385,210 @@ PyObject* policy_lag(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Tensors of a call of the operators around the head: as above, and on the device that the kernels run on.
+struct Call {
+  const c10::DeviceIndex device = current_device().index();
+  const at::Tensor* tensor(PyObject* o) const {
+    const at::Tensor* t = ::tensor(o);
+    if (t && t->get_device() != device) throw NotPlain();
+    return t;
+  }
+  const at::Tensor& required(PyObject* o) const {
+    const at::Tensor* t = tensor(o);
+    if (!t) throw NotPlain();
+    return *t;
+  }
+  template <class T>
+  T* array(PyObject* o, int64_t n, at::ScalarType type) const {
+    tensor(o);
+    return array_of<T>(o, n, type);
+  }
+  // a matrix of rows of consecutive values, of `rows` by `cols`, and its pitch
+  void* matrix(PyObject* o, int64_t rows, int64_t cols, at::ScalarType type, int64_t* pitch) const {
+    const at::Tensor* t = tensor(o);
+    if (!t) {
+      *pitch = 0;
+      return nullptr;
+    }
+    if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (cols > 1 && t->stride(1) != 1)) throw NotPlain();
+    *pitch = rows > 1 ? t->stride(0) : cols;
+    return pointer(t, type);
+  }
+  // rows and columns of what a call is about
+  std::pair<int64_t, int64_t> sizes(PyObject* o) const {
+    const at::Tensor& t = required(o);
+    if (t.dim() != 2 || t.size(0) < 1 || t.size(1) < 1 || t.size(1) > 0x7fffffffLL) throw NotPlain();
+    return {t.size(0), t.size(1)};
+  }
+};
+// the caller's workspace, or a block of this call (held through it)
+struct Workspace {
+  at::Tensor own;
+  void* p = nullptr;
+  size_t bytes = 0;
+  Workspace(const at::Tensor* given, size_t need) {
+    if (given) {
+      if (!given->is_contiguous()) throw NotPlain();
+      p = given->data_ptr();
+      bytes = given->nbytes();
+    } else if (need) {
+      own = scratch(need);
+      p = own.data_ptr();
+      bytes = need;
+    }
+  }
+};
+
+// (x, weight, y_out, bias, eps, rms, mean_out, rstd_out)
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 8 || !around.norm) return PyLong_FromLong(-1);
+  return guarded([&]() -> int {
+    const Call c;
+    const auto [T, D] = c.sizes(a[0]);
+    npd_norm_desc d{};
+    d.n_tokens = T;
+    d.width = (int32_t)D;
+    d.flags = flag(a[5]) ? NPD_NORM_RMS : 0u;
+    d.eps = (float)number(a[4]);
+    void* const x = c.matrix(a[0], T, D, at::kBFloat16, &d.x_stride);
+    void* const y = c.matrix(a[2], T, D, at::kBFloat16, &d.y_stride);
+    return call(around.norm, &d, x, c.array<void>(a[1], D, at::kBFloat16), c.array<void>(a[3], D, at::kBFloat16), y,
+                c.array<float>(a[6], T, at::kFloat), c.array<float>(a[7], T, at::kFloat), current_stream());
+  });
+}
+
+// (grad_y, x, weight, rstd, mean, rms, grad_x, grad_weight, grad_bias, accumulate, workspace)
+PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11 || !around.norm_bwd) return PyLong_FromLong(-1);
+  return guarded([&]() -> int {
+    const Call c;
+    const auto [T, D] = c.sizes(a[1]);
+    npd_norm_desc d{};
+    d.n_tokens = T;
+    d.width = (int32_t)D;
+    d.flags = (flag(a[5]) ? NPD_NORM_RMS : 0u) | (a[6] != Py_None ? NPD_NORM_GRAD_X : 0u) | (a[7] != Py_None ? NPD_NORM_GRAD_WEIGHT : 0u) |
+              (a[8] != Py_None ? NPD_NORM_GRAD_BIAS : 0u) | (flag(a[9]) ? NPD_NORM_ACCUMULATE : 0u);
+    void* const g = c.matrix(a[0], T, D, at::kBFloat16, &d.y_stride);
+    void* const x = c.matrix(a[1], T, D, at::kBFloat16, &d.x_stride);
+    void* const gx = c.matrix(a[6], T, D, at::kBFloat16, &d.grad_x_stride);
+    void* const w = c.array<void>(a[2], D, at::kBFloat16);
+    float* const mean = c.array<float>(a[4], T, at::kFloat);
+    float* const rstd = c.array<float>(a[3], T, at::kFloat);
+    void* const gw = c.array<void>(a[7], D, at::kBFloat16);
+    void* const gb = c.array<void>(a[8], D, at::kBFloat16);
+    const Workspace ws(c.tensor(a[10]), a[10] == Py_None ? around.norm_bytes(&d) : 0);
+    return call(around.norm_bwd, &d, g, x, w, mean, rstd, gx, gw, gb, ws.p, ws.bytes, current_stream());
+  });
+}
+
+// (x, q_out, scale_out)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 3 || !around.quantize) return PyLong_FromLong(-1);
+  return guarded([&]() -> int {
+    const Call c;
+    const auto [R, D] = c.sizes(a[0]);
+    int64_t x_stride, q_stride;
+    void* const x = c.matrix(a[0], R, D, at::kBFloat16, &x_stride);
+    int8_t* const q = static_cast<int8_t*>(c.matrix(a[1], R, D, at::kChar, &q_stride));
+    return call(around.quantize, R, (int32_t)D, x_stride, q_stride, x, q, c.array<float>(a[2], R, at::kFloat), current_stream());
+  });
+}
+
+// (hidden, hidden_scale, weight, weight_scale, logits_out, bias, softcap, workspace)
+PyObject* head_logits_int8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 8 || !around.int8) return PyLong_FromLong(-1);
+  return guarded([&]() -> int {
+    const Call c;
+    const auto [T, D] = c.sizes(a[0]);
+    const int64_t V = c.required(a[2]).dim() == 2 ? c.required(a[2]).size(0) : 0;
+    if (V < 1 || V > 0x7fffffffLL) throw NotPlain();
+    npd_head_desc d{};
+    d.n_tokens = T;
+    d.vocab = (int32_t)V;
+    d.width = (int32_t)D;
+    d.tau = 1.0f;
+    d.softcap = (float)number(a[6]);
+    int8_t* const h = static_cast<int8_t*>(c.matrix(a[0], T, D, at::kChar, &d.hidden_stride));
+    int8_t* const w = static_cast<int8_t*>(c.matrix(a[2], V, D, at::kChar, &d.weight_stride));
+    void* const out = c.matrix(a[4], T, V, at::kBFloat16, &d.logits_stride);
+    d.flags = (((uintptr_t)h | (uintptr_t)w) & 15) != 0 ? NPD_HEAD_UNALIGNED : 0u;
+    float* const hs = c.array<float>(a[1], T, at::kFloat);
+    float* const wscale = c.array<float>(a[3], V, at::kFloat);
+    void* const bias = c.array<void>(a[5], V, at::kBFloat16);
+    const Workspace ws(c.tensor(a[7]), a[7] == Py_None ? around.head_bytes(&d, NPD_HEAD_LOGITS_INT8) : 0);
+    return call(around.int8, &d, h, hs, w, wscale, bias, out, ws.p, ws.bytes, current_stream());
+  });
+}
+
+// (logits, uniform, tokens_out, temperature, top_k, top_p, min_p, loss_mask, logprob_out, nll_out, kept_out, dev_status, workspace)
+PyObject* sample_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 13 || !around.sample) return PyLong_FromLong(-1);
+  return guarded([&]() -> int {
+    const Call c;
+    const auto [T, V] = c.sizes(a[0]);
+    npd_sample_desc d{};
+    d.n_tokens = T;
+    d.vocab = (int32_t)V;
+    d.top_p = 1.0f;
+    // a number for all rows, or a tensor of one for each
+    auto setting = [&](PyObject* o, float* value) -> float* {
+      if (THPVariable_Check(o)) return c.array<float>(o, T, at::kFloat);
+      *value = (float)number(o);
+      return nullptr;
+    };
+    void* const x = c.matrix(a[0], T, V, at::kBFloat16, &d.logits_stride);
+    float* const tau = setting(a[3], &d.temperature);
+    int32_t* k = nullptr;
+    if (THPVariable_Check(a[4]))
+      k = c.array<int32_t>(a[4], T, at::kInt);
+    else
+      d.top_k = (int32_t)whole(a[4]);
+    float* const top_p = setting(a[5], &d.top_p);
+    float* const min_p = setting(a[6], &d.min_p);
+    float* const u = c.array<float>(a[1], T, at::kFloat);
+    int32_t* const token = c.array<int32_t>(a[2], T, at::kInt);
+    uint8_t* const mask = c.array<uint8_t>(a[7], T, at::kByte);
+    float* const logprob = c.array<float>(a[8], T, at::kFloat);
+    float* const nll = c.array<float>(a[9], T, at::kFloat);
+    int32_t* const kept = c.array<int32_t>(a[10], T, at::kInt);
+    int32_t* const status = c.array<int32_t>(a[11], 1, at::kInt);
+    const Workspace ws(c.tensor(a[12]), a[12] == Py_None ? around.sample_bytes(&d) : 0);
+    return call(around.sample, &d, x, u, mask, tau, k, top_p, min_p, token, logprob, nll, kept, status, ws.p, ws.bytes, current_stream());
+  });
+}
+
+// bind_around_head(addresses): in the order of AroundHead, all 0 with a library without them
+PyObject* bind_around_head(PyObject*, PyObject* args) {
+  PyObject* addresses;
+  if (!PyArg_ParseTuple(args, "O!", &PyTuple_Type, &addresses)) return nullptr;
+  constexpr int kEntries = 8;
+  void* p[kEntries];
+  bool some = false, all = true;
+  if (PyTuple_GET_SIZE(addresses) != kEntries) {
+    PyErr_SetString(PyExc_ValueError, "8 addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < kEntries; ++i) {
+    p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(addresses, i));
+    if (!p[i] && PyErr_Occurred()) return nullptr;
+    some |= p[i] != nullptr;
+    all &= p[i] != nullptr;
+  }
+  if (some != all) {
+    PyErr_SetString(PyExc_ValueError, "a null address");
+    return nullptr;
+  }
+  around.norm = reinterpret_cast<decltype(around.norm)>(p[0]);
+  around.norm_bwd = reinterpret_cast<decltype(around.norm_bwd)>(p[1]);
+  around.norm_bytes = reinterpret_cast<decltype(around.norm_bytes)>(p[2]);
+  around.quantize = reinterpret_cast<decltype(around.quantize)>(p[3]);
+  around.int8 = reinterpret_cast<decltype(around.int8)>(p[4]);
+  around.head_bytes = reinterpret_cast<decltype(around.head_bytes)>(p[5]);
+  around.sample = reinterpret_cast<decltype(around.sample)>(p[6]);
+  around.sample_bytes = reinterpret_cast<decltype(around.sample_bytes)>(p[7]);
+  Py_RETURN_NONE;
+}
+
 // bind(raw_stream, workspaces, addresses): `addresses` of libnpd's entry points in the order of Entry; 0 for both of the last two:
 // a library without them
 PyObject* bind(PyObject*, PyObject* args) {
@@ -417,6 +634,12 @@ PyMethodDef methods[] = {
     {"delta_ifd", reinterpret_cast<PyCFunction>(delta_ifd), METH_FASTCALL, nullptr},
     {"teacher_topk", reinterpret_cast<PyCFunction>(teacher_topk), METH_FASTCALL, nullptr},
     {"policy_lag", reinterpret_cast<PyCFunction>(policy_lag), METH_FASTCALL, nullptr},
+    {"bind_around_head", bind_around_head, METH_VARARGS, nullptr},
+    {"layer_norm", reinterpret_cast<PyCFunction>(layer_norm), METH_FASTCALL, nullptr},
+    {"layer_norm_bwd", reinterpret_cast<PyCFunction>(layer_norm_bwd), METH_FASTCALL, nullptr},
+    {"quantize_rows", reinterpret_cast<PyCFunction>(quantize_rows), METH_FASTCALL, nullptr},
+    {"head_logits_int8", reinterpret_cast<PyCFunction>(head_logits_int8), METH_FASTCALL, nullptr},
+    {"sample_tokens", reinterpret_cast<PyCFunction>(sample_tokens), METH_FASTCALL, nullptr},
     {"release", release, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "npd_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -185,3 +185,76 @@ def test_the_norms_backward_pass_is_captured_beside_an_eager_graph():
         assert torch.equal(gx, want[0]) and torch.equal(gw, want[1])
     alive.backward()
     assert x.grad is not None and w.grad is not None
+
+
+def _calls(seed=0):
+    """Every wrapper's call with each of its arguments: (call, outputs)."""
+    T, V, D = 70, 600, 130
+    weight, norm, g = model(V, D, seed)
+    f = dict(device=DEV)
+    x = torch.randn((T, D), device=DEV, generator=g).to(torch.bfloat16)
+    bias = torch.randn(V, device=DEV, generator=g).to(torch.bfloat16)
+    y, mean, rstd = torch.empty_like(x), torch.empty(T, **f), torch.empty(T, **f)
+    gx, gw, gb = torch.empty_like(x), torch.ones_like(norm), torch.ones_like(norm)
+    q, scale = torch.empty((T, D), dtype=torch.int8, **f), torch.empty(T, **f)
+    wq, wscale = torch.empty((V, D), dtype=torch.int8, **f), torch.empty(V, **f)
+    logits = torch.empty((T, V), dtype=torch.bfloat16, **f)
+    tokens, kept, status = (torch.zeros(n, dtype=torch.int32, **f) for n in (T, T, 1))
+    logprob, nll = torch.empty(T, **f), torch.empty(T, **f)
+    u, r = torch.rand(T, device=DEV, generator=g), torch.rand(T, device=DEV, generator=g)
+    mask = (r < 0.9).to(torch.uint8)
+    ws = [torch.empty(1 << 20, dtype=torch.uint8, **f) for _ in range(3)]
+    own = dict(temperature=0.5 + r, top_k=(50 * r).to(torch.int32), top_p=1 - 0.2 * r, min_p=0.1 * r)
+    return [
+        (lambda: npd.npd_layer_norm(x, norm, bias=norm, eps=1e-4, y_out=y, mean_out=mean, rstd_out=rstd), [y, mean, rstd]),
+        (lambda: npd.npd_layer_norm(x, y_out=y, rms=True, rstd_out=rstd), [y, rstd]),
+        (lambda: npd.npd_layer_norm_bwd(y, x, norm, mean=mean, rstd=rstd, grad_x=gx, grad_weight=gw, grad_bias=gb, accumulate=True), [gx, gw, gb]),
+        (lambda: npd.npd_layer_norm_bwd(y, x, rstd=rstd, rms=True, grad_weight=gw, workspace=ws[0]), [gw]),
+        (lambda: npd.npd_quantize_rows(x, q_out=q, scale_out=scale), [q, scale]),
+        (lambda: npd.npd_quantize_rows(weight, q_out=wq, scale_out=wscale), [wq, wscale]),
+        (lambda: npd.npd_head_logits_int8(q, scale, wq, wscale, bias=bias, softcap=20.0, logits_out=logits), [logits]),
+        (lambda: npd.npd_head_logits_int8(q, scale, wq, wscale, logits_out=logits, workspace=ws[1]), [logits]),
+        (lambda: npd.npd_sample_tokens(logits, u, tokens_out=tokens, temperature=0.7, top_k=20, top_p=0.9, min_p=0.01, loss_mask=mask,
+                                       logprob_out=logprob, nll_out=nll, kept_out=kept, dev_status=status), [tokens, logprob, nll, kept, status]),
+        (lambda: npd.npd_sample_tokens(logits, u, tokens_out=tokens, logprob_out=logprob, kept_out=kept, workspace=ws[2], **own),
+         [tokens, logprob, kept]),
+        (lambda: npd.npd_sample_tokens(logits, u, tokens_out=tokens, top_k=None, kept_out=kept), [tokens, kept]),
+    ]
+
+
+def test_native_and_python_marshalling_make_the_same_calls(monkeypatch):
+    assert binding._host is not None
+    native, python = [], []
+    for call, outputs in _calls():
+        call()
+        native.append([t.clone() for t in outputs])
+    monkeypatch.setattr(binding, "_host", None)
+    for call, outputs in _calls():
+        call()
+        python.append([t.clone() for t in outputs])
+    for a, b in zip(native, python):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("host", [True, False])
+def test_refusals_are_the_same_with_either(host, monkeypatch):
+    if not host:
+        monkeypatch.setattr(binding, "_host", None)
+    x, f = torch.zeros((4, 40), dtype=torch.bfloat16, device=DEV), torch.zeros(4, device=DEV)
+    q, i = torch.zeros((4, 40), dtype=torch.int8, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    for call in (lambda: npd.npd_layer_norm(x, y_out=x), lambda: npd.npd_layer_norm(x, y_out=x.clone(), eps=-1.0),
+                 lambda: npd.npd_layer_norm_bwd(x, x, rstd=f, rms=True), lambda: npd.npd_layer_norm_bwd(x, x, rstd=f, grad_x=x.clone()),
+                 lambda: npd.npd_quantize_rows(x, q_out=x.view(torch.int8)[:, :40], scale_out=f),
+                 lambda: npd.npd_head_logits_int8(q, f, q, f, logits_out=x[:, :4], softcap=float("nan")),
+                 lambda: npd.npd_sample_tokens(x, f, tokens_out=i, temperature=-1.0), lambda: npd.npd_sample_tokens(x, f, tokens_out=i, top_k=-1),
+                 lambda: npd.npd_sample_tokens(x, f, tokens_out=f.view(torch.int32))):
+        with pytest.raises(binding.NpdError):
+            call()
+    for call in (lambda: npd.npd_layer_norm(x.float(), y_out=x.clone()), lambda: npd.npd_layer_norm(x, y_out=x.clone()[:, :39]),
+                 lambda: npd.npd_layer_norm(x.t(), y_out=x.t()), lambda: npd.npd_layer_norm(x, f, y_out=x.clone()),
+                 lambda: npd.npd_quantize_rows(x, q_out=i, scale_out=f), lambda: npd.npd_quantize_rows(x, q_out=q, scale_out=f[:3]),
+                 lambda: npd.npd_head_logits_int8(q, f, x, f, logits_out=x[:, :4].clone()),
+                 lambda: npd.npd_sample_tokens(x, i, tokens_out=i), lambda: npd.npd_sample_tokens(x, f, tokens_out=i, top_p=i),
+                 lambda: npd.npd_sample_tokens(x, f.cpu(), tokens_out=i)):
+        with pytest.raises(ValueError):
+            call()
