@@ -74,7 +74,7 @@ struct Row {
   RowSplit split;
 };
 
-// eight(id, bits of eight entries) of the row's aligned groups, the next kAhead of them always requested, and one(id, bits) of the
+// eight(g, bits of eight entries) of the row's aligned groups, the next kAhead of them always requested, and one(id, bits) of the
 // entries around them.  (No load is behind a branch: the compiler would wait for all of them where paths meet.  Those behind the
 // row's end read its last group again.)
 constexpr int kAhead = 6;
@@ -94,12 +94,12 @@ __device__ __forceinline__ void each_group(const Row& r, E&& eight, F&& one) {
       for (int u = 0; u < kAhead; ++u) {
         const uint4 now = v[u];
         v[u] = load(g + t + (u + kAhead) * kThreads);
-        eight(r.split.head + 8 * (g + t + u * kThreads), now);
+        eight(g + t + u * kThreads, now);
       }
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (g + t + u * kThreads < n) eight(r.split.head + 8 * (g + t + u * kThreads), v[u]);
+      if (g + t + u * kThreads < n) eight(g + t + u * kThreads, v[u]);
   }
 #pragma unroll 1
   for (int j = t; j < r.V - 8 * n; j += kThreads) {
@@ -108,12 +108,34 @@ __device__ __forceinline__ void each_group(const Row& r, E&& eight, F&& one) {
   }
 }
 
+// A counter also says where its value occurs if it does once: the lower bits count, the others add up the numbers of the places (2^shift
+// groups) of those that are counted.  Rows of 2^19 entries and more have no bits left for that.
+struct Places {
+  uint32_t mask;  // of the count
+  int shift;
+  bool there;
+};
+constexpr int kCountBits = 19;
+constexpr uint32_t kAround = (1u << (32 - kCountBits)) - 1;  // the place of the entries around the groups
+// `longest`: entries of the row, of one in parts those of its first part, so that all have the same bits
+__device__ __forceinline__ Places places_of(const Row& r, int longest) {
+  const int n = r.split.nvec;
+  Places p;
+  p.there = longest < 1 << kCountBits;
+  p.mask = p.there ? (1u << kCountBits) - 1 : 0xffffffffu;
+  const int over = 32 - (32 - kCountBits) - __builtin_clz((unsigned)n | 1);  // bits of n beyond those of a place
+  p.shift = over > 0 ? over : 0;
+  if ((uint32_t)(n >> p.shift) >= kAround) ++p.shift;
+  return p;
+}
+
 // f(id, bits) of the row's entries
 template <class F>
 __device__ __forceinline__ void each_entry(const Row& r, F&& f) {
   each_group(
       r,
-      [&](int id, const uint4& v) {
+      [&](int g, const uint4& v) {
+        const int id = r.split.head + 8 * g;
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -240,6 +262,7 @@ struct Passes {
 // is up to the end of each stretch is in LDS; one wave searches there.
 struct Counted {
   Shared& s;
+  uint32_t mask;  // Places::mask
   uint32_t top_key, all;
   double top, per, sum;
 
@@ -249,10 +272,10 @@ struct Counted {
     if (i < kNear) return s.near_keys[i];
     return ~(0x8000u + kFirst + (uint32_t)(i - kNear)) & 0xffffu;
   }
-  static __device__ __forceinline__ uint32_t count_of(const Shared& s, int t, int e) {
-    if (t < kOwners) return s.counts[2 * (kValues - 1 - (t * kEach + e))];
+  static __device__ __forceinline__ uint32_t count_of(const Shared& s, uint32_t mask, int t, int e) {
+    if (t < kOwners) return s.counts[2 * (kValues - 1 - (t * kEach + e))] & mask;
     const int i = (t - kOwners) * kEach + e;
-    return i < kNear ? s.near_counts[i] : s.counts[2 * (i - kNear) + 1];
+    return i < kNear ? s.near_counts[i] : s.counts[2 * (i - kNear) + 1] & mask;
   }
   // the first stretch for which `is` holds (it holds for those behind it too), all threads of the wave
   template <class F>
@@ -269,7 +292,7 @@ struct Counted {
     const int t = first_stretch([&](int t) { return weight_of(key(s, t, kEach - 1), top, per, s) < least || t == kThreads - 1; });
     uint32_t n = t ? s.count_ends[t - 1] : 0;
     const int e = thread_of_phase() & (kEach - 1);
-    const uint32_t here = count_of(s, t, e);
+    const uint32_t here = count_of(s, mask, t, e);
     const uint32_t mine = here && weight_of(key(s, t, e), top, per, s) >= least ? here : 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) n += __builtin_amdgcn_readlane(mine, i);
@@ -284,7 +307,7 @@ struct Counted {
       return c == all || (c > 0 && (what == kMassReaches ? w >= mass : w > mass));
     });
     const int e = thread_of_phase() & (kEach - 1);
-    const uint32_t n = count_of(s, t, e);
+    const uint32_t n = count_of(s, mask, t, e);
     const double one = weight_of(key(s, t, e), top, per, s);
     // up to the end of each of the eight (lanes eight apart do the same)
     uint32_t c = n;
@@ -338,7 +361,7 @@ __device__ __attribute__((noinline)) void order_near(Shared& s) {
 }
 
 // The counts of the thread's eight values, in their order.
-__device__ __forceinline__ void read_counts(const Shared& s, int t, uint32_t (&n)[kEach]) {
+__device__ __forceinline__ void read_counts(const Shared& s, uint32_t mask, int t, uint32_t (&n)[kEach]) {
   if (t >= kOwners && t < kOwners + kNear / kEach) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) n[e] = s.near_counts[(t - kOwners) * kEach + e];
@@ -354,7 +377,7 @@ __device__ __forceinline__ void read_counts(const Shared& s, int t, uint32_t (&n
     w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
   }
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) n[e] = negative ? w[2 * e + 1] : w[2 * (kEach - 1 - e)];
+  for (int e = 0; e < kEach; ++e) n[e] = (negative ? w[2 * e + 1] : w[2 * (kEach - 1 - e)]) & mask;
 }
 
 // the largest value that is counted (0: none), all threads
@@ -410,7 +433,7 @@ __device__ __forceinline__ void weigh(Shared& s, const uint32_t (&n)[kEach], dou
   if (c && near) {
 #pragma unroll 1
     for (int e = 0; e < kEach; ++e) {
-      const double k = Counted::count_of(s, t, e);
+      const double k = s.near_counts[(t - kOwners) * kEach + e];
       const uint32_t key = Counted::key(s, t, e);
       w += k * weight_of(key, top, per, s);
       if (both) w1 += k * weight_of(key, top, 1.0, s);
@@ -520,7 +543,8 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   const uint32_t bits2 = bits * 0x10001u, mask2 = mask * 0x10001u;
   each_group(
       row,
-      [&](int id, const uint4& v) {
+      [&](int g, const uint4& v) {
+        const int id = row.split.head + 8 * g;
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         u16x2 d[4];
 #pragma unroll
@@ -605,6 +629,28 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   return s.found;
 }
 
+// id of the entry of a value that occurs once, at a place
+__device__ __forceinline__ int find_place(const Row& row, uint32_t key, uint32_t place, int shift, Shared& s) {
+  const int t = thread_of_phase();
+  if (place == kAround) {
+    if (t < row.V - 8 * row.split.nvec) {
+      const int id = row.split.edge_elem(t);
+      if (key_of(row.p[id]) == key) s.found = id;
+    }
+  } else {
+    const int g = (int)(place << shift) + t;
+    if (t < 1 << shift && g < row.split.nvec) {
+      const uint4 v = reinterpret_cast<const uint4*>(row.p + row.split.head)[g];
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (key_of(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffff) == key) s.found = row.split.head + 8 * g + e;
+    }
+  }
+  __syncthreads();
+  return s.found;
+}
+
 // A row's outputs.
 __device__ __forceinline__ void put(const SampleArgs& a, int64_t r, int token, double logprob, double nll, uint32_t kept, int status) {
   if (threadIdx.x != 0) return;
@@ -657,7 +703,7 @@ __device__ __forceinline__ void begin_counts(Shared& s) {
 }
 
 // Counts a row's entries; zero in the first of near_counts, what else is closer to zero than the counters' in near_list.
-__device__ __forceinline__ void count_entries(const Row& row, Shared& s) {
+__device__ __forceinline__ void count_entries(const Row& row, int longest, Shared& s) {
   uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
   auto other = [&](uint32_t b) {
     const uint32_t size = b & 0x7fff;
@@ -676,9 +722,11 @@ __device__ __forceinline__ void count_entries(const Row& row, Shared& s) {
   // A counter's number is the entry with its sign in the lowest place, less the first one's.  What is no counter's goes to
   // the lane's own among `kOthers` (a branch around every addition takes twice the time) and is looked at afterwards.
   const uint32_t own = kOthers + (threadIdx.x & 63);
+  const Places places = places_of(row, longest);
   each_group(
       row,
-      [&](int, const uint4& v) {
+      [&](int g, const uint4& v) {
+        const uint32_t unit = 1u + (places.there ? (uint32_t)(g >> places.shift) << kCountBits : 0u);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         uint32_t most = 0;
 #pragma unroll
@@ -688,8 +736,8 @@ __device__ __forceinline__ void count_entries(const Row& row, Shared& s) {
           const uint32_t lo = at[0], hi = at[1];
           most = most > lo ? most : lo;
           most = most > hi ? most : hi;
-          atomicAdd(&s.counts[lo < own ? lo : own], 1u);
-          atomicAdd(&s.counts[hi < own ? hi : own], 1u);
+          atomicAdd(&s.counts[lo < own ? lo : own], unit);
+          atomicAdd(&s.counts[hi < own ? hi : own], unit);
         }
         if (most < kOthers) return;
 #pragma unroll 1
@@ -701,7 +749,7 @@ __device__ __forceinline__ void count_entries(const Row& row, Shared& s) {
       [&](int, uint32_t b) {
         const uint32_t i = (b & 0x7fff) - kFirst;
         if (i < kValues)
-          atomicAdd(&s.counts[2 * i + (b >> 15)], 1u);
+          atomicAdd(&s.counts[2 * i + (b >> 15)], 1u + (places.there ? kAround << kCountBits : 0u));
         else
           other(b);
       });
@@ -738,7 +786,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_count_kernel(SampleArgs a)
   if (a.mask && !a.mask[r]) return;
   begin_counts(s);
   __syncthreads();
-  count_entries(row_part(a.x + r * a.stride, part_of(a.V, a.parts, blockIdx.x)), s);
+  count_entries(row_part(a.x + r * a.stride, part_of(a.V, a.parts, blockIdx.x)), part_of(a.V, a.parts, 0).end, s);
   Part& part = reinterpret_cast<Part*>(a.workspace)[r * a.parts + blockIdx.x];
   for (int i = threadIdx.x; i < (int)kOthers / 4; i += kThreads) reinterpret_cast<uint4*>(part.counts)[i] = reinterpret_cast<uint4*>(s.counts)[i];
   if (threadIdx.x < kNear) part.near_list[threadIdx.x] = s.near_list[threadIdx.x];
@@ -751,13 +799,13 @@ __global__ __launch_bounds__(kThreads, 8) void sample_count_kernel(SampleArgs a)
 }
 
 // The counts of a row out of those of its parts, all threads.
-__device__ __forceinline__ void join_parts(const Part* parts, int n, Shared& s) {
+__device__ __forceinline__ void join_parts(const Part* parts, int n, uint32_t mask, Shared& s) {
   for (int i = threadIdx.x; i < (int)kOthers / 4; i += kThreads) {
     uint4 sum = make_uint4(0, 0, 0, 0);
 #pragma unroll 4
     for (int p = 0; p < n; ++p) {
       const uint4 v = reinterpret_cast<const uint4*>(parts[p].counts)[i];
-      sum = make_uint4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+      sum = make_uint4(sum.x + (v.x & mask), sum.y + (v.y & mask), sum.z + (v.z & mask), sum.w + (v.w & mask));
     }
     reinterpret_cast<uint4*>(s.counts)[i] = sum;
   }
@@ -808,19 +856,21 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
   const Part* parts = SPLIT ? reinterpret_cast<const Part*>(a.workspace) + r * a.parts : nullptr;
 
+  const int longest = SPLIT ? part_of(a.V, a.parts, 0).end : a.V;
   begin_exponentials(s);
   if constexpr (SPLIT) {
-    join_parts(parts, a.parts, s);
+    join_parts(parts, a.parts, places_of(row, longest).mask, s);
   } else {
     begin_counts(s);
     __syncthreads();
-    count_entries(row, s);
+    count_entries(row, a.V, s);
   }
   const uint32_t big = s.big;
   const bool odd = s.odd || s.near >= kNear;
   if (s.near && !odd) order_near(s);
+  const uint32_t mask = SPLIT ? 0xffffffffu : places_of(row, longest).mask;  // (joined, they are counts alone)
   uint32_t n[kEach];
-  read_counts(s, thread_of_phase(), n);
+  read_counts(s, mask, thread_of_phase(), n);
   const uint32_t top_key = largest_counted(s, n);
   const double counted_top = top_key ? value_of(top_key) : 0.0;
   // Numbers below -256 have no weight that 64 bits would show beside the largest's (2^-90 times at most 2^26 of them) where that is
@@ -834,7 +884,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   double sum1;  // of the weights at temperature 1
   weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
   if (threadIdx.x < kWave) {
-    const Counted counted{s, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
+    const Counted counted{s, mask, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
     Choice mine = choose(counted, q, greedy);
     if (mine.kept == counted.all && big && !greedy && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
       const uint32_t all = counted.all + big;
@@ -845,26 +895,31 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   if (threadIdx.x == kWave) s.log1 = log(sum1);  // (beside the search)
   __syncthreads();
   const Choice c = s.choice;
-  int token;
-  if constexpr (SPLIT) {
-    // the part that has the entry, where the value has a counter
-    Span where = {0, a.V};
-    uint32_t which = c.which;
-    const uint32_t bits = c.key & 0x8000 ? c.key & 0x7fff : ~c.key & 0x7fff, i = 2 * (bits - kFirst) + (c.key & 0x8000 ? 0 : 1);
-    if (bits >= kFirst) {
+  // what there is about the value where it has a counter; of a row in parts the part that has the entry
+  Row where = row;
+  int first = 0;
+  uint32_t which = c.which, here = 0;
+  const uint32_t bits = c.key & 0x8000 ? c.key & 0x7fff : ~c.key & 0x7fff, i = 2 * (bits - kFirst) + (c.key & 0x8000 ? 0 : 1);
+  if (bits >= kFirst) {
+    if constexpr (SPLIT) {
+      const uint32_t part_mask = places_of(row, longest).mask;
       for (int p = 0; p < a.parts; ++p) {
-        const uint32_t here = parts[p].counts[i];
-        if (which < here) {
-          where = part_of(a.V, a.parts, p);
+        here = parts[p].counts[i];
+        if (which < (here & part_mask)) {
+          const Span span = part_of(a.V, a.parts, p);
+          first = span.first;
+          where = row_part(row.p, span);
           break;
         }
-        which -= here;
+        which -= here & part_mask;
       }
+    } else {
+      here = s.counts[i];
     }
-    token = where.first + find_entry(row_part(row.p, where), c.key, which, s);
-  } else {
-    token = find_entry(row, c.key, c.which, s);
   }
+  const Places places = places_of(where, longest);
+  const bool once = places.there && (here & places.mask) == 1;
+  const int token = first + (once ? find_place(where, c.key, here >> kCountBits, places.shift, s) : find_entry(where, c.key, which, s));
   put(a, r, token, c.logprob, s.log1 + (counted_top - (double)value_of(c.key)), c.kept, 0);
 }
 

@@ -96,6 +96,35 @@ def test_temperatures_as_large_as_the_logits(scale):
     check(x, u, temperature=float(np.float32(scale)), top_k=100, top_p=0.9, min_p=0.01)
 
 
+@pytest.mark.parametrize("V,offset", [(40, 3), (2000, 1), (8191, 0), (65535, 5), (65600, 0), (524280, 2), (524287, 0), (524288, 0), (600001, 1),
+                                      (4300003, 3)])
+def test_the_entry_wherever_it_is(V, offset):
+    """A value that occurs once, at the ends of the row, of its parts and of what is looked at together, and another that does twice."""
+    T = 40
+    g = torch.Generator(device=DEV).manual_seed(V)
+    memory = torch.full((offset + T * V + 8,), 1e4, dtype=torch.bfloat16, device=DEV)
+    x = memory[offset:offset + T * V].view(T, V)
+    x.copy_((0.5 * torch.randn((T, V), device=DEV, generator=g)).clamp(-2, 2))
+    places = [0, 1, 5, 7, 8, 9, V - 1, V - 2, V - 8, V - 9, V // 2, V // 3, V // 8, V // 8 - 1, V // 8 // 8 * 8, 16383 % V, 16384 % V, 24575 % V,
+              24576 % V, 49151 % V, 49152 % V] + torch.randint(0, V, (T,), device=DEV, generator=g).tolist()
+    rows = torch.arange(T, device=DEV)
+    at = torch.tensor(places[:T], device=DEV)
+    x[rows, at] = 30.0                                   # all the weight there is
+    u = torch.rand(T, device=DEV, generator=g)
+    for how in (dict(), dict(workspace=torch.empty(256, dtype=torch.uint8, device=DEV))):
+        tokens = torch.empty(T, dtype=torch.int32, device=DEV)
+        for few in (T, 2):
+            npd.npd_sample_tokens(x[:few], u[:few], temperature=0.5, tokens_out=tokens[:few], **how)
+            assert torch.equal(tokens[:few].long(), at[:few])
+    also = (at + 1 + torch.randint(0, V - 1, (T,), device=DEV, generator=g)) % V
+    x[rows, also] = 30.0
+    want = torch.where(u < 0.5, torch.minimum(at, also), torch.maximum(at, also))
+    for few in (T, 2):
+        tokens = torch.empty(few, dtype=torch.int32, device=DEV)
+        npd.npd_sample_tokens(x[:few], u[:few], temperature=0.5, tokens_out=tokens)
+        assert torch.equal(tokens.long(), want[:few])
+
+
 def test_few_values_and_many_ties():
     """Bf16 logits of two bits: every draw ends among equal entries, and in the middle of them what is kept ends."""
     x, u = logits(64, 5000, spread=1.0)
