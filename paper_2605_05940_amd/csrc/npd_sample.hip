@@ -129,21 +129,22 @@ __device__ __forceinline__ Places places_of(const Row& r, int longest) {
   return p;
 }
 
-// f(id, bits) of the row's entries
+// bits of the row's entries, for rows by passes: in little code (a function whose branches reach further than 128 KB takes the registers
+// of its return address for them, and whether the compiler has saved those is chance)
 template <class F>
 __device__ __forceinline__ void each_entry(const Row& r, F&& f) {
-  each_group(
-      r,
-      [&](int g, const uint4& v) {
-        const int id = r.split.head + 8 * g;
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          f(id + 2 * t, w[t] & 0xffff);
-          f(id + 2 * t + 1, w[t] >> 16);
-        }
-      },
-      f);
+  const uint4* groups = reinterpret_cast<const uint4*>(r.p + r.split.head);
+#pragma unroll 1
+  for (int g = threadIdx.x; g < r.split.nvec; g += kThreads) {
+    const uint4 v = groups[g];
+#pragma unroll 1
+    for (int t = 0; t < 8; ++t) {
+      const uint32_t two = t < 4 ? (t < 2 ? v.x : v.y) : (t < 6 ? v.z : v.w);
+      f(t & 1 ? two >> 16 : two & 0xffff);
+    }
+  }
+#pragma unroll 1
+  for (int j = threadIdx.x; j < r.V - 8 * r.split.nvec; j += kThreads) f((uint32_t)r.p[r.split.edge_elem(j)]);
 }
 
 // in wave order, so that every thread has the same sum
@@ -204,10 +205,10 @@ struct Passes {
   Shared& s;
   uint32_t top_key, all;
   double top, per, sum;
-  __device__ __forceinline__ void from(uint32_t key, double at, uint32_t* count, double* mass) const {
+  __device__ __attribute__((noinline)) void from(uint32_t key, double at, uint32_t* count, double* mass) const {
     uint32_t n = 0;
     double m = 0.0;
-    each_entry(row, [&](int, uint32_t b) {
+    each_entry(row, [&](uint32_t b) {
       const uint32_t k = key_of(b);
       if (k < key || k < kLowest) return;
       ++n;
@@ -229,7 +230,7 @@ struct Passes {
   // how many weigh `least` and more
   __device__ __forceinline__ uint32_t at_least(double least) const {
     uint32_t n = 0;
-    each_entry(row, [&](int, uint32_t b) {
+    each_entry(row, [&](uint32_t b) {
       const uint32_t k = key_of(b);
       n += k >= kLowest && weight_of(k, top, per, s) >= least;
     });
@@ -664,7 +665,7 @@ __device__ __forceinline__ void put(const SampleArgs& a, int64_t r, int token, d
 // A row by passes over it.  (Not inlined: the registers of the rows that are counted are the ones that matter.)
 __device__ __attribute__((noinline)) void draw_by_passes(const SampleArgs a, int64_t r, const Row row, const Settings q, bool greedy, Shared& s) {
   uint32_t most = 0, bad = 0;
-  each_entry(row, [&](int, uint32_t b) {
+  each_entry(row, [&](uint32_t b) {
     const uint32_t k = key_of(b);
     most = most > k ? most : k;
     bad |= k >= kInfinity || k < 0x7f;  // (0x7f: -inf)
