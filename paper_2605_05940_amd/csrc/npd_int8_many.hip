@@ -10,6 +10,9 @@ template <int MF, int NF, bool CAP>
 __global__ __launch_bounds__(kHeadThreads, 1) void int8_tiles_kernel(Int8Args a) {
   using Product = HeadProduct<MF, NF, false, false, true, true>;
   __shared__ __attribute__((aligned(1024))) char lds[Product::kLds];
+  // a wave's factors and biases: requested with a tile's first step, in LDS when its sums are there (no barrier: they are the wave's own)
+  constexpr int kColumns = 16 * NF, kRows = 16 * MF, kC = (kColumns + kWave - 1) / kWave, kR = (kRows + kWave - 1) / kWave;
+  __shared__ __attribute__((aligned(16))) float factors[kHeadThreads / kWave][2][kColumns], of_rows[kHeadThreads / kWave][kR * kWave];
   const int rows = (int)a.T;
   const int mt = (rows + Product::kTileM - 1) / Product::kTileM, nt = (a.V + Product::kTileN - 1) / Product::kTileN;
   HeadTile tile = head_tile(blockIdx.x, mt, nt);
@@ -29,31 +32,47 @@ __global__ __launch_bounds__(kHeadThreads, 1) void int8_tiles_kernel(Int8Args a)
     for (int i = 0; i < MF; ++i)
 #pragma unroll
       for (int j = 0; j < NF; ++j) x.acc[i][j] = i32x4{0, 0, 0, 0};
+    float ws[kC], bias[kC], hs[kR];
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const int n = columns + c * kWave + lane, v = n < a.V ? n : a.V - 1;
+      ws[c] = a.w_scale[v];
+      bias[c] = a.bias ? bf16_one(a.bias[v]) : 0.0f;
+    }
+#pragma unroll
+    for (int c = 0; c < kR; ++c) {
+      const int64_t m = mw - (lane & 15) + c * kWave + lane;
+      hs[c] = a.h_scale[m < rows ? m : rows - 1];
+    }
     x.run(q, w, next.there, (int64_t)next.m * Product::kTileM, (int64_t)next.n * Product::kTileN, 0, K, lds);
     tile = next;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      factors[wave][0][c * kWave + lane] = ws[c];
+      factors[wave][1][c * kWave + lane] = bias[c];
+    }
+#pragma unroll
+    for (int c = 0; c < kR; ++c) of_rows[wave][c * kWave + lane] = hs[c];
 
     const SoftCap soft(CAP ? a.cap : 1.0f);
-    float hs[MF];
-#pragma unroll
-    for (int i = 0; i < MF; ++i) hs[i] = a.h_scale[mw + 16 * i < rows ? mw + 16 * i : 0];
 #pragma unroll
     for (int j = 0; j < NF; j += 2) {
       __builtin_amdgcn_sched_barrier(0);  // (eight columns' scales at a time: the fragments of the next tile are in registers already)
-      const int n = nw + 16 * j;
-      float ws[8], bias[8];
+      const int n = nw + 16 * j, at = n - columns;
+      f32x4 f[2], g[2];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int v = n + t < a.V ? n + t : a.V - 1;
-        ws[t] = a.w_scale[v];
-        bias[t] = a.bias ? bf16_one(a.bias[v]) : 0.0f;
+      for (int t = 0; t < 2; ++t) {
+        f[t] = *reinterpret_cast<const f32x4*>(&factors[wave][0][at + 4 * t]);
+        g[t] = *reinterpret_cast<const f32x4*>(&factors[wave][1][at + 4 * t]);
       }
 #pragma unroll
       for (int i = 0; i < MF; ++i) {
         const int64_t m = mw + 16 * i;
+        const float by = of_rows[wave][16 * i + (lane & 15)];
         float y[8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-          y[t] = __builtin_fmaf((float)x.acc[i][j + (t >> 2)][t & 3] * hs[i], ws[t], bias[t]);
+          y[t] = __builtin_fmaf((float)x.acc[i][j + (t >> 2)][t & 3] * by, f[t >> 2][t & 3], g[t >> 2][t & 3]);
           if constexpr (CAP) y[t] = soft.cap * soft.tanh_of(y[t]);
         }
         if (m >= rows) continue;
