@@ -37,7 +37,7 @@ Plan make_plan(const npd_head_desc& d) {
   Plan p;
   p.padded = (d.width + 15) / 16 * 16;
   const bool odd = d.width % 16 != 0 || (d.flags & NPD_HEAD_UNALIGNED);
-  // (64 rows of 50,048 x 1,024 take 20.9 us in the kernels that read weights at any alignment, 16.3 in tiles; 17 rows 14.7 and 14.0, of
+  // (64 rows of 50,048 x 1,024 take 20.9 us in the kernels that read weights at any alignment, 15.9 in tiles; 17 rows 14.7 and 14.0, of
   // 151,936 x 2,048 61.5 and 65.7)
   p.few = d.n_tokens <= (odd || d.hidden_stride % 16 != 0 || d.weight_stride % 16 != 0 ? kHeadFewRows : kHeadFewRows / 2);
   p.pack_h = !p.few && (odd || d.hidden_stride % 16 != 0);

@@ -37,6 +37,8 @@ __device__ __forceinline__ uint2 quantize8(const uint4& x, int down, float top, 
   return make_uint2(w[0], w[1]);
 }
 
+// A row lies in the registers of TH threads from its one read.  Bytes bound it: 151,936 x 2,048 172 us (5.4 TB/s, two thirds of them
+// reads).
 template <int TH, int G>
 __global__ __launch_bounds__(quantize_block<TH>()) void quantize_kernel(QuantizeArgs a) {
   __shared__ uint32_t tops[quantize_block<TH>() / kWave];
@@ -156,8 +158,9 @@ __device__ __forceinline__ void finish_columns(const Int8Args& a, const int* x) 
 
 // Up to four rows: v_mfma_i32_4x4x4_16b_i8 as 16 pieces of k of the same four columns and four rows, added up at the end, so that one
 // load of a wave is 256 consecutive bytes of each of four rows of the weights, read past the caches; the four waves of a workgroup
-// have the same 32 columns and every fourth block of k.  Workgroups begin at different places of their rows and wrap around (rows of
-// a power of two of bytes would else be read out of few memory channels).
+// have the same 32 columns and every fourth block of k.  The weights' bytes bound it: 151,936 x 2,048 49.3 us (6.3 TB/s).  Workgroups
+// begin at different places of their rows and wrap around (rows of a power of two of bytes would else be read out of few memory
+// channels).
 __global__ __launch_bounds__(kHeadThreads, 4) void int8_tokens_kernel(Int8Args a) {
   constexpr int kWaves = kHeadThreads / kWave, G = 8;
   constexpr int kBlock = 256;  // bytes of k per load
@@ -221,7 +224,8 @@ __global__ __launch_bounds__(kHeadThreads, 4) void int8_tokens_kernel(Int8Args a
 }
 
 // Up to 16 RT rows: a wave reads the weights of 16 FC columns straight into the fragments of 16 x 16 x 64 products, 64 bytes of 16
-// rows per load, 256 of each at a time; the hidden states go through LDS, 256 bytes of all rows at a time.
+// rows per load, 256 of each at a time; the hidden states go through LDS, 256 bytes of all rows at a time.  9 rows of 151,936 x 2,048
+// take 60 us (5.2 TB/s), of 50,048 x 1,024 12.0.
 template <int RT, int FC>
 __global__ __launch_bounds__(kHeadThreads, 3) void int8_few_kernel(Int8Args a) {
   constexpr int kPart = 64 * FC;  // columns of the workgroup

@@ -1,5 +1,8 @@
 // Logits of a head in 8-bit integers, many rows: tiles of the matrix cores' whole-number products (exact), scaled, biased and capped
 // in fp32 and rounded to bf16 once before they leave the registers.
+//
+// A step of 64 bytes of k takes the matrix cores as long as one of 32 bf16 values, so a tile has half the steps and its end weighs
+// twice: with the scales loaded there 4,096 x 151,936 x 2,048 took 1,450 us, with them waiting in LDS 1,264.
 #include "npd_int8.hpp"
 #include "npd_softcap.hpp"
 
@@ -105,23 +108,22 @@ hipError_t launch(const Int8Args& a, int together, hipStream_t stream) {
 
 }  // namespace
 
-// Tiles of 256 x 256 have the highest rate (2,048 bytes of k: 1,420 us for 4,096 x 151,936; 256 x 128 1,700, 128 x 128 1,767), where
-// there are enough of them for the compute units, and where their rows are there.  Measured (MI355X, us; 64 x 128 / 128 x 128 / 256 x 128 /
-// 256 x 256, of the first two as many workgroups together as fit):
-//   rows  of 32,000 x 4,096           of 50,048 x 1,024            of 151,936 x 2,048
-//   64    34 / 35 / - / -             16.3 / 17.1 / - / -          75 / 74 / - / -
-//   128   49 / 37 / - / -             25.0 / 21.0 / - / -          111 / 86 / - / -
-//   160   - / 53 / 42 / 64            - / 27.7 / 27.3 / 25.7       - / 120 / 112 / 119
-//   256   - / 61 / 46 / 64            - / 34.6 / 28.3 / 26.5       - / 145 / 126 / 124
-//   512   - / 105 / 86 / 69           - / 56.4 / 49.3 / 45.8       - / 246 / 230 / 201
-// (up to 128 rows tiles of 128 x 256, one workgroup per compute unit: 52, 18.8 and 96)
+// Tiles of 256 x 256 have the highest rate (4,096 x 151,936 x 2,048 1,264 us, 2,020 TOPS; 256 x 128 1,706, 128 x 128 1,850), where there are
+// enough of them for the compute units, and where their rows are there.  Measured (MI355X, us; 64 x 128 / 128 x 128 / 256 x 128 / 256 x 256, of
+// the first two as many workgroups together as fit):
+//   rows  of 32,000 x 4,096             of 50,048 x 1,024              of 151,936 x 2,048
+//   64    32.9 / 33.9 / - / -           15.9 / 16.9 / - / -            74.5 / 75.6 / - / -
+//   128   49 / 35.4 / 39.4 / 53.5       25.0 / 19.2 / 24.3 / 26.6      111 / 87.3 / 101.5 / 106.6
+//   160   - / 49.9 / 42.2 / 58.4        - / 26.0 / 25.7 / 27.0         - / 115 / 104 / 108
+//   256   - / 56.1 / 46.0 / 59.3        - / 32.4 / 28.2 / 28.4         - / 136 / 115 / 114
+//   333   - / 73.5 / 68.8 / 61.4        - / 35.9 / 43.2 / 43.9         - / 176 / 178 / 157
+//   512   - / 101 / 85 / 65             - / 51.8 / 51.4 / 46.1         - / 240 / 219 / 172
 hipError_t launch_int8_many(const Int8Args& a, hipStream_t stream) {
   if (a.T <= 64) return launch<2, 4>(a, 3, stream);
   if (a.T <= 128 || head_small(a.T, a.V)) return launch<4, 4>(a, 2, stream);
   const int64_t tiles = (a.T + 255) / 256 * (((int64_t)a.V + 255) / 256);
-  // (up to 384 rows fill three tiles of 128, two of 256 by three quarters: 333 x 50,003 x 1,008, capped, 58 us in the former, 70; but
-  // 32,000 x 4,096 80 and 66)
-  if (a.T > 256 && a.T <= 384 && a.D <= 2048) return launch<4, 4>(a, 2, stream);
+  // (up to 384 rows fill three tiles of 128, two of 256 by three quarters; with a short k that decides: 333 x 50,003 x 1,008, capped, 54 / 60)
+  if (a.T > 256 && a.T <= 384 && a.D <= 1024) return launch<4, 4>(a, 2, stream);
   if (tiles <= 128) return launch<8, 4>(a, 1, stream);
   return launch<8, 8>(a, 1, stream);
 }

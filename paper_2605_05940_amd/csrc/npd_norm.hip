@@ -1,6 +1,10 @@
 // Layer norm, forward and backward, and its form without a mean (npd_norm.hpp).  A row lies in the registers of TH threads, G groups
 // of eight values each, from its one read to its one write; its sums are taken over what is there (the mean first, then the squares of
-// what is left: the difference of two large sums is never formed).  Bytes bound it.
+// what is left: the difference of two large sums is never formed).
+//
+// Bytes bound it.  Measured (MI355X, 32,768 x 2,048): forward 48.4 us (5.5 TB/s), backward with both parameters' gradients 82.8 (4.9 TB/s;
+// torch's copy of 4 GiB reaches 4.7), of which joining the 512 pieces of those is 4.  With what is unpacked kept in registers, and so one
+// or two waves per SIMD, 56.8 and 110.  One row of 2,048 3.6 us.
 #include "../../include/npd.h"
 #include "npd_head_gemm.hpp"
 #include "npd_norm.hpp"
