@@ -350,7 +350,8 @@ hipError_t launch_norm_grad(const NormGradArgs& a, hipStream_t stream) {
                                       : launch_grad<1024, 8>(a, stream);
   if (e != hipSuccess || !(a.dw || a.db)) return e;
   if (a.D > kNormHeldWidth) {
-    const hipError_t c = launch_kernel(norm_columns_kernel, dim3((unsigned)(a.D + 511) / 512, (unsigned)a.pieces), dim3(kNormThreads), 0, stream, a);
+    const dim3 grid((unsigned)(a.D + 511) / 512, (unsigned)a.pieces);
+    const hipError_t c = launch_kernel(norm_columns_kernel, grid, dim3(kNormThreads), 0, stream, a);
     if (c != hipSuccess) return c;
   }
   return launch_kernel(norm_join_kernel, dim3((unsigned)(a.D + kJoinColumns - 1) / kJoinColumns, a.dw && a.db ? 2 : 1), dim3(kJoinThreads), 0, stream, a);

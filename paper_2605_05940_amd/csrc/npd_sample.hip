@@ -710,6 +710,9 @@ __device__ __forceinline__ void begin_counts(Shared& s) {
   if (threadIdx.x == 0) s.big = s.odd = s.near = 0;
 }
 
+// an entry with its sign in the lowest place: the first that has a counter, and -inf less that
+constexpr unsigned short kTurnedFirst = 2 * kFirst, kTurnedForbidden = 0xff01 - kTurnedFirst;
+
 // Counts a row's entries; zero in the first of near_counts, what else is closer to zero than the counters' in near_list.
 __device__ __forceinline__ void count_entries(const Row& row, int longest, Shared& s) {
   uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
@@ -736,18 +739,27 @@ __device__ __forceinline__ void count_entries(const Row& row, int longest, Share
       [&](int g, const uint4& v) {
         const uint32_t unit = 1u + (places.there ? (uint32_t)(g >> places.shift) << kCountBits : 0u);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        u16x2 at[4];
         uint32_t most = 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const uint32_t turned = (w[t] << 1 & 0xfffefffe) | (w[t] >> 15 & 0x00010001);
-          const u16x2 at = __builtin_bit_cast(u16x2, turned) - u16x2{(unsigned short)(2 * kFirst), (unsigned short)(2 * kFirst)};
-          const uint32_t lo = at[0], hi = at[1];
+          at[t] = __builtin_bit_cast(u16x2, turned) - u16x2{kTurnedFirst, kTurnedFirst};
+          const uint32_t lo = at[t][0], hi = at[t][1];
           most = most > lo ? most : lo;
           most = most > hi ? most : hi;
           atomicAdd(&s.counts[lo < own ? lo : own], unit);
           atomicAdd(&s.counts[hi < own ? hi : own], unit);
         }
         if (most < kOthers) return;
+        // (-inf is nothing: rows in which some entries are forbidden come here with every group)
+        u16x2 some = {0, 0};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const u16x2 forbidden = {kTurnedForbidden, kTurnedForbidden}, one = {1, 1};
+          some = __builtin_elementwise_max(some, at[t] * __builtin_elementwise_min(at[t] ^ forbidden, one));
+        }
+        if (some[0] < kOthers && some[1] < kOthers) return;
 #pragma unroll 1
         for (int t = 0; t < 8; ++t) {
           const uint32_t two = t < 4 ? (t < 2 ? w[0] : w[1]) : (t < 6 ? w[2] : w[3]);

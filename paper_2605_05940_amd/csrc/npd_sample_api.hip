@@ -54,7 +54,8 @@ extern "C" npd_status npd_sample_tokens(const npd_sample_desc* desc, const void*
   const size_t bytes = sample_bytes(d);
   const bool split = workspace && bytes > 0 && workspace_bytes >= bytes;
   if (split && misaligned(workspace, 256)) return NPD_ERR_WORKSPACE;
-  const Range out[6] = {opt_range(split ? workspace : nullptr, bytes), range_of(token, n), opt_range(logprob, n), opt_range(nll, n), opt_range(kept, n), opt_range(dev_status, 4)};
+  const Range out[6] = {opt_range(split ? workspace : nullptr, bytes),
+                        range_of(token, n), opt_range(logprob, n), opt_range(nll, n), opt_range(kept, n), opt_range(dev_status, 4)};
   if (any_alias(in, 7, out, 6)) return NPD_ERR_ALIAS;
   SampleArgs a{};
   a.T = T;
