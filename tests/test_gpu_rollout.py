@@ -56,7 +56,7 @@ class Rollout:
         return [t.clone() for t in (self.logits, self.tokens, self.nll, self.logprob, self.kept)]
 
 
-@pytest.mark.parametrize("T,V,D", [(1, 40000, 512), (7, 3000, 200), (70, 1000, 1000), (300, 5000, 64)])
+@pytest.mark.parametrize("T,V,D", [(1, 100000, 512), (7, 3000, 200), (70, 1000, 1000), (300, 5000, 64)])
 def test_a_step_of_a_rollout(T, V, D):
     weight, norm, g = model(V, D)
     x = torch.randn((T, D), device=DEV, generator=g).to(torch.bfloat16)
@@ -86,7 +86,7 @@ def test_a_step_of_a_rollout(T, V, D):
 @pytest.mark.parametrize("T", [1, 40, 130])
 def test_captured_steps(T):
     """Two steps captured with buffers of their own, replayed with other inputs, side by side, and with eager steps between."""
-    V, D = 33000, 300
+    V, D = 99000, 300
     weight, norm, g = model(V, D)
     sets = [(torch.randn((T, D), device=DEV, generator=g).to(torch.bfloat16), torch.rand(T, device=DEV, generator=g)) for _ in range(3)]
     mask = torch.ones(T, dtype=torch.uint8, device=DEV)

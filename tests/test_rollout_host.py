@@ -235,10 +235,10 @@ def test_sample_refusals(lib):
 
 def test_sample_workspace(lib):
     size = npd.npd_sample_workspace_bytes
-    assert size(T, V) == size(1, 32767) == size(129, 1 << 20) == size(0, 100) == size(1, 1 << 40) == 0
+    assert size(T, V) == size(1, 98303) == size(86, 1 << 20) == size(0, 100) == size(1, 1 << 40) == 0
     part = 4 * (7936 + 4 + 256)
-    assert size(1, 32768) == 2 * part and size(1, 1 << 26) == 8 * part and size(128, 1 << 18) == 256 * part and size(40, 151936) == 240 * part
-    d = sample_desc(n_tokens=4, vocab=50000, logits_stride=50000)
+    assert size(1, 98304) == 3 * part and size(1, 1 << 26) == 8 * part and size(85, 1 << 18) == 255 * part and size(40, 151936) == 160 * part
+    d = sample_desc(n_tokens=4, vocab=100000, logits_stride=100000)
     need = lib.npd_sample_workspace_bytes(d)
     assert need == 12 * part
     assert sample(lib, d, need, ws=ARGS["ws"] + 128) == E_WS
