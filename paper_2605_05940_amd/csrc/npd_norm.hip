@@ -101,7 +101,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
         s[0] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
       }
       row_sums<TH, 1>(s, smem);
-      mean = s[0] * per;
+      mean = s[0] / (float)a.D;  // (rounded once: a row of equal values, whose sums are exact, has its mean exactly)
     }
     stay_packed(x);
     float s[1] = {0.0f};

@@ -3,7 +3,7 @@
 Tolerances, from the arithmetic alone: B = 2^-8 is the largest relative error of a rounding to bf16, u = 2^-24 of one to fp32.
 
   mean    a thread adds up to 64 values, a wave and a workgroup 6 + 16 more: fewer than K = 100 dependent roundings on sums of at
-          most sum |x|, then the factor 1 / D (two):  dm = (K + 2) u sum |x| / D
+          most sum |x|, then the division by D:  dm = (K + 2) u sum |x| / D
   var     every difference is off by dm and a rounding, squares and their sum by K more:
           dv = 2 (dm + u |mean|) sum |d| / D + (K + 6) u var + dm^2
   rstd    relative: dr = dv / (2 (var + eps)) + 4 u  (sum with eps, root, reciprocal)
@@ -191,6 +191,21 @@ def test_rows_of_equal_values_and_of_zeros():
     got = run_forward(x, w, b, 1e-5, False)
     for name, want in norm64(x, w, b, 1e-5, False).items():
         check(got[name], want, name)
+
+
+@pytest.mark.parametrize("D", [1, 3, 49, 100, 999, 1000, 2047, 2048, 5001, 8191, 20001, 32767, 65535, 65536])
+def test_rows_of_equal_values_have_their_mean_exactly(D):
+    """Their sums are whole multiples (16 bits) of 8 bits, exact in fp32: the mean is the value, and nothing is left of the row but the
+    bias, however large the value is beside eps."""
+    values = torch.tensor([2.5, -1000.0, 1.0078125, 30208.0, -3e30, 1e-30, 255.0, -0.3340], device=DEV).to(torch.bfloat16)
+    x = values[:, None].repeat(1, D)
+    w, b = torch.full((D,), 1.5, dtype=torch.bfloat16, device=DEV), torch.randn(D, device=DEV).to(torch.bfloat16)
+    got = run_forward(x, w, b, 1e-5, False)
+    assert torch.equal(got["mean"], values.float())
+    assert torch.equal(got["y"], b.expand_as(x))
+    check(got["rstd"], norm64(x, w, b, 1e-5, False)["rstd"], "rstd")
+    got = run_forward(x, w, b, 0.0, False)
+    assert bool(got["rstd"].isinf().all()) and bool(got["y"].isnan().all())
 
 
 def test_a_row_that_is_not_finite_keeps_to_itself():
