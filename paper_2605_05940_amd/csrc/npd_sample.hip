@@ -14,6 +14,8 @@
 // the token's id 1 to 8); one row of 262,144 in eight parts 21.5, whole 32; 2,048 rows of 151,936 greedy 160 (3.9 TB/s), untruncated 206:
 // where the token's value occurs more than once its row is read again.  4,096 rows of 1,000 take 112: rows that short are not what this
 // is made for.  Workgroups of 512 threads, three to a compute unit, are 8 to 13 % faster for those, and 16 % slower for 48 rows of 50,003.
+#include <stddef.h>
+
 #include "../../include/npd.h"
 #include "npd_head_gemm.hpp"
 #include "npd_sample.hpp"
@@ -58,20 +60,20 @@ struct Place {       // where a search over the order ended
 
 struct Choice {
   uint32_t key, kept, which;  // the token's value, and its place among the entries of that value
-  double logprob;
+  double logit, sum;          // less the largest one, over tau; of the weights of what is kept
 };
 
 struct Shared {
   __attribute__((aligned(16))) uint32_t counts[kOthers + kWave];
-  double mass_ends[kThreads];
+  double mass_ends[kThreads + 1];  // of the stretches before
   double table[kTable];
-  uint32_t count_ends[kThreads];
+  uint32_t count_ends[kThreads + 1];
   double masses[2][kWaves];
   uint32_t near_list[kNear], near_keys[kNear], near_counts[kNear];  // as they came; in order, and how many have that value
   uint32_t sums[kWaves];
   uint32_t big, odd, near, first, listed;
   int32_t found;
-  double log1;
+  double logs[2];  // of the sums: of what is kept, at temperature 1
   Choice choice;
 };
 
@@ -204,6 +206,29 @@ __device__ __forceinline__ double lane_value(double v, int i) {
   return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(u.x, i), __builtin_amdgcn_readlane(u.y, i)));
 }
 
+// sums up to each lane, over rows of N lanes (8: the first eight alone are right); no LDS is waited for
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ uint32_t shifted(uint32_t v) {  // (lanes that nothing is shifted into: 0)
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, ROWS, 0xf, false);
+}
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ double shifted(double v) {
+  const uint2 u = __builtin_bit_cast(uint2, v);
+  return __builtin_bit_cast(double, make_uint2(shifted<CONTROL, ROWS>(u.x), shifted<CONTROL, ROWS>(u.y)));
+}
+template <int N, class T>
+__device__ __forceinline__ T sums_to(T v) {
+  v += shifted<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
+  v += shifted<0x112, 0xf>(v);
+  v += shifted<0x114, 0xf>(v);
+  if constexpr (N > 8) v += shifted<0x118, 0xf>(v);
+  if constexpr (N > 16) {
+    v += shifted<0x142, 0xa>(v);  // row_bcast:15, into the odd rows, then :31
+    v += shifted<0x143, 0xc>(v);
+  }
+  return v;
+}
+
 enum Find { kCount, kMassReaches, kMassExceeds };
 
 // A row by passes over it: counts and masses of its entries from a value on, and the value at which they reach something.
@@ -267,80 +292,69 @@ struct Passes {
 };
 
 // A row whose entries are counted.  Stretches of eight values, in their order, were weighed by a thread each (weigh()), and what there
-// is up to the end of each stretch is in LDS; one wave searches there.
+// is before each stretch is in LDS; one wave searches there, whose lanes have what there is up to the end of every sixteenth.  (One
+// wave's instructions are the time: places and keys are chosen, not branched to.)
 struct Counted {
   Shared& s;
   uint32_t mask;  // Places::mask
   uint32_t top_key, all;
   double top, per, sum;
+  uint32_t ends;
+  double mass_ends;
 
   static __device__ __forceinline__ uint32_t key(const Shared& s, int t, int e) {
-    if (t < kOwners) return 0x8000u + kFirst + kValues - 1 - (uint32_t)(t * kEach + e);
     const int i = (t - kOwners) * kEach + e;
-    if (i < kNear) return s.near_keys[i];
-    return ~(0x8000u + kFirst + (uint32_t)(i - kNear)) & 0xffffu;
+    const uint32_t near = s.near_keys[i < 0 ? 0 : i < kNear ? i : kNear - 1];
+    const uint32_t positive = 0x8000u + kFirst + kValues - 1 - (uint32_t)(t * kEach + e), negative = 0x7fffu - kFirst - (uint32_t)(i - kNear);
+    return t < kOwners ? positive : i < kNear ? near : negative;
   }
   static __device__ __forceinline__ uint32_t count_of(const Shared& s, uint32_t mask, int t, int e) {
-    if (t < kOwners) return s.counts[2 * (kValues - 1 - (t * kEach + e))] & mask;
+    constexpr int kNearCounts = (int)(offsetof(Shared, near_counts) / 4);
+    static_assert(offsetof(Shared, counts) == 0, "");
     const int i = (t - kOwners) * kEach + e;
-    return i < kNear ? s.near_counts[i] : s.counts[2 * (i - kNear) + 1] & mask;
+    const int positive = 2 * ((int)kValues - 1 - (t * kEach + e)), negative = 2 * (i - kNear) + 1;
+    const int at = t < kOwners ? positive : i < kNear ? kNearCounts + i : negative;
+    return reinterpret_cast<const uint32_t*>(&s)[at] & mask;  // (the mask has all bits of any count that may be there)
   }
-  // the first stretch for which `is` holds (it holds for those behind it too), all threads of the wave
-  template <class F>
-  static __device__ __forceinline__ int first_stretch(F&& is) {
-    const int lane = thread_of_phase() & 63;
-    constexpr int kPer = kThreads / kWave;
-    const uint64_t ends = __ballot(is(lane * kPer + kPer - 1));
-    const int group = ends ? __builtin_ctzll(ends) : kWave - 1;
-    const uint64_t in = __ballot(is(group * kPer + (lane < kPer ? lane : kPer - 1)));
-    return group * kPer + (in ? __builtin_ctzll(in) : kPer - 1);
+  static constexpr int kPer = kThreads / kWave;
+  // the first of the stretches for which it holds (it does for those behind it too), from lanes' answers for the ends of sixteen each,
+  // then for those sixteen
+  static __device__ __forceinline__ int first_lane(bool is, int none) {
+    const uint64_t lanes = __ballot(is);
+    return lanes ? __builtin_ctzll(lanes) : none;
   }
   // how many weigh `least` and more (weights fall along the order whether a value occurs or not)
   __device__ __forceinline__ uint32_t at_least(double least) const {
-    const int t = first_stretch([&](int t) { return weight_of(key(s, t, kEach - 1), top, per, s) < least || t == kThreads - 1; });
-    uint32_t n = t ? s.count_ends[t - 1] : 0;
-    const int e = thread_of_phase() & (kEach - 1);
+    const int lane = thread_of_phase() & 63;
+    const auto below = [&](uint32_t k) { return weight_of(k, top, per, s) < least; };
+    const int group = first_lane(below(key(s, lane * kPer + kPer - 1, kEach - 1)) || lane == kWave - 1, kWave - 1);
+    const int in = lane < kPer ? lane : kPer - 1;
+    const int t = group * kPer + first_lane(below(key(s, group * kPer + in, kEach - 1)) || in == kPer - 1, kPer - 1);
+    const int e = lane & (kEach - 1);
     const uint32_t here = count_of(s, mask, t, e);
-    const uint32_t mine = here && weight_of(key(s, t, e), top, per, s) >= least ? here : 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) n += __builtin_amdgcn_readlane(mine, i);
-    return n;
+    const uint32_t mine = sums_to<kEach>(below(key(s, t, e)) ? 0 : here);
+    return s.count_ends[t] + __builtin_amdgcn_readlane(mine, kEach - 1);
   }
   // (there is enough: what is asked for is at most what there is; the last value there is takes what rounding leaves over)
   __device__ __forceinline__ Place find(Find what, uint32_t target, double mass) const {
-    const int t = first_stretch([&](int t) {
-      const uint32_t c = s.count_ends[t];
-      if (what == kCount) return c >= target;
-      const double w = s.mass_ends[t];
-      return c == all || (c > 0 && (what == kMassReaches ? w >= mass : w > mass));
-    });
-    const int e = thread_of_phase() & (kEach - 1);
-    const uint32_t n = count_of(s, mask, t, e);
-    const double one = weight_of(key(s, t, e), top, per, s);
-    // up to the end of each of the eight (lanes eight apart do the same)
-    uint32_t c = n;
-    double w = n * one;
-#pragma unroll
-    for (int off = 1; off < kEach; off <<= 1) {
-      const uint32_t c2 = __shfl_up(c, off, kEach);
-      const double w2 = __shfl_up(w, off, kEach);
-      if (e >= off) {
-        c += c2;
-        w = w2 + w;
-      }
-    }
-    const uint32_t c0 = t ? s.count_ends[t - 1] : 0;
-    const double w0 = t ? s.mass_ends[t - 1] : 0.0;
-    c += c0;
-    w += w0;
-    const bool enough = what == kCount ? c >= target : what == kMassReaches ? w >= mass : w > mass;
+    const auto reached = [&](double w) { return what == kMassReaches ? w >= mass : w > mass; };
+    const auto is = [&](uint32_t c, double w) { return what == kCount ? c >= target : c == all || (c > 0 && reached(w)); };
+    const int lane = thread_of_phase() & 63, in = lane < kPer ? lane : kPer - 1, e = lane & (kEach - 1);
+    const int group = first_lane(is(ends, mass_ends), kWave - 1), at = group * kPer + in + 1;
+    const int t = group * kPer + first_lane(is(s.count_ends[at], what == kCount ? 0.0 : s.mass_ends[at]), kPer - 1);
+    const uint32_t n = count_of(s, mask, t, e), k = key(s, t, e);
+    const uint32_t c0 = s.count_ends[t];
+    const double w0 = s.mass_ends[t], one = weight_of(k, top, per, s);
+    // up to the end of each of the eight (the first eight lanes')
+    const uint32_t c = c0 + sums_to<kEach>(n);
+    const double w = w0 + sums_to<kEach>(n * one);
     // (what rounding leaves over is the last one's that has any weight)
-    const uint64_t those = __ballot(enough && n) & 0xff, some = __ballot(n && one > 0.0) & 0xff, any = __ballot(n != 0) & 0xff;
-    const int i = those ? __builtin_ctzll(those) : some ? 63 - __builtin_clzll(some) : any ? 63 - __builtin_clzll(any) : 0;
+    const uint32_t those = (uint32_t)__ballot(n && (what == kCount ? c >= target : reached(w))) & 0xff;
+    const uint32_t some = (uint32_t)__ballot(n && one > 0.0) & 0xff, any = (uint32_t)__ballot(n != 0) & 0xff;
+    const int last = 31 - __builtin_clz((some ? some : any) | 1), i = those ? __builtin_ctz(those) : last;
     const uint32_t here = __builtin_amdgcn_readlane(n, i);
-    const double before = i ? lane_value(w, i ? i - 1 : 0) : w0;
-    const Place p = {key(s, t, i), (uint32_t)__builtin_amdgcn_readlane(c, i) - here, here, before, lane_value(one, i)};
-    return p;
+    const double before = lane_value(w, i ? i - 1 : 0);
+    return Place{(uint32_t)__builtin_amdgcn_readlane(k, i), (uint32_t)__builtin_amdgcn_readlane(c, i) - here, here, i ? before : w0, lane_value(one, i)};
   }
 };
 
@@ -368,6 +382,9 @@ __device__ __attribute__((noinline)) void order_near(Shared& s) {
   __syncthreads();
 }
 
+// (of two elements of an array the compiler would choose the place, and then the element by comparing that to each)
+__device__ __forceinline__ uint32_t either(bool first, uint32_t a, uint32_t b) { return first ? a : b; }
+
 // The counts of the thread's eight values, in their order.
 __device__ __forceinline__ void read_counts(const Shared& s, uint32_t mask, int t, uint32_t (&n)[kEach]) {
   if (t >= kOwners && t < kOwners + kNear / kEach) {
@@ -375,17 +392,27 @@ __device__ __forceinline__ void read_counts(const Shared& s, uint32_t mask, int 
     for (int e = 0; e < kEach; ++e) n[e] = s.near_counts[(t - kOwners) * kEach + e];
     return;
   }
-  // (sixteen counters, of both signs: reads of every other word would meet in few banks)
+  // (sixteen counters, of both signs: reads of every other word would meet in few banks.  Those of four lanes at the same sixteenth of
+  // 256 bytes would too, so each four of the lanes begin at another quarter of their sixteen.)
   const bool negative = t >= kOwners;
-  const int at = negative ? 2 * (t - kOwners - kNear / kEach) * kEach : 2 * (kValues - kEach * (t + 1));
-  uint32_t w[2 * kEach];
+  const int at = negative ? 2 * (t - kOwners - kNear / kEach) * kEach : 2 * (kValues - kEach * (t + 1)), turn = t >> 2 & 3;
+  uint32_t w[kEach];  // of the sign
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint4 v = *reinterpret_cast<const uint4*>(&s.counts[at + 4 * i]);
-    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    const uint4 v = *reinterpret_cast<const uint4*>(&s.counts[at + 4 * ((i + turn) & 3)]);
+    w[2 * i] = negative ? v.y : v.x;
+    w[2 * i + 1] = negative ? v.w : v.z;
   }
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) n[e] = (negative ? w[2 * e + 1] : w[2 * (kEach - 1 - e)]) & mask;
+  for (int by = 1; by < 4; by <<= 1) {  // quarter i is (i + turn) & 3: turned back
+    uint32_t o[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) o[i] = either(turn & by, w[(i - 2 * by) & (kEach - 1)], w[i]);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) w[i] = o[i];
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) n[e] = either(negative, w[e], w[kEach - 1 - e]) & mask;
 }
 
 // the largest value that is counted (0: none), all threads
@@ -403,8 +430,8 @@ __device__ __forceinline__ uint32_t largest_counted(Shared& s, const uint32_t (&
   return waves ? __builtin_amdgcn_readlane(mine, __builtin_ctzll(waves)) : 0;
 }
 
-// Weighs the stretches, all threads: what there is up to the end of each, and the sum at temperature 1.  (Ends rise: a stretch's is the
-// sum over its wave so far, added to the waves' before.)  Eight values of a stretch lie evenly apart, so that their weights are
+// Weighs the stretches, all threads: what there is up to the end of each (the sum over its wave so far, added to the waves' before), and
+// the sum at temperature 1.  Eight values of a stretch lie evenly apart, so that their weights are
 // powers of one ratio: two exponentials for eight, and 2^-50 of a weight at most in roundings.
 __device__ __forceinline__ void weigh(Shared& s, const uint32_t (&n)[kEach], double top, double per, bool nll, double* sum1) {
   const int t = thread_of_phase(), lane = t & 63, wave = t >> 6;
@@ -420,7 +447,10 @@ __device__ __forceinline__ void weigh(Shared& s, const uint32_t (&n)[kEach], dou
   if (c && !near) {
     // (from the first that occurs: those before it may lie above the top)
     const int f = __builtin_ctz(there);
-    const double first = value_of(Counted::key(s, t, f)), step = value_of(Counted::key(s, t, 0)) - value_of(Counted::key(s, t, 1));
+    const bool negative = t >= kOwners;
+    const uint32_t size = kFirst + (negative ? (t - kOwners) * kEach - kNear + f : kValues - 1 - t * kEach - f);
+    const double first = bf16_one((uint16_t)(size | (negative ? 0x8000 : 0)));
+    const double step = __builtin_bit_cast(float, ((size >> 7) - 7) << 23);  // (of the eight: 2^-7 of their power of two)
     double one = exponential((first - top) * per, s);
     const double ratio = exponential(-step * per, s);
 #pragma unroll
@@ -447,16 +477,9 @@ __device__ __forceinline__ void weigh(Shared& s, const uint32_t (&n)[kEach], dou
       if (both) w1 += k * weight_of(key, top, 1.0, s);
     }
   }
-#pragma unroll 1
-  for (int off = 1; off < kWave; off <<= 1) {
-    const uint32_t c2 = __shfl_up(c, off, kWave);
-    const double w2 = __shfl_up(w, off, kWave);
-    if (lane >= off) {
-      c += c2;
-      w = w2 + w;
-    }
-    if (both) w1 += __shfl_xor(w1, off, kWave);
-  }
+  c = sums_to<kWave>(c);
+  w = sums_to<kWave>(w);
+  if (both) w1 = sums_to<kWave>(w1);
   __syncthreads();  // (largest_counted()'s sums have been read)
   if (lane == 63) {
     s.sums[wave] = c;
@@ -464,22 +487,18 @@ __device__ __forceinline__ void weigh(Shared& s, const uint32_t (&n)[kEach], dou
     s.masses[1][wave] = w1;
   }
   __syncthreads();
-  uint32_t c0 = 0;
-  double w0 = 0.0, all1 = 0.0, all = 0.0;
-#pragma unroll 4
-  for (int i = 0; i < kWaves; ++i) {
-    if (i == wave) {
-      c0 += c;
-      w0 = all + w;
-    } else if (i < wave) {
-      c0 += s.sums[i];
-    }
-    all += s.masses[0][i];
-    all1 += s.masses[1][i];
+  // (lane i has the sums up to wave i)
+  const int i = lane & (kWaves - 1);
+  const uint32_t cs = sums_to<kWaves>(s.sums[i]);
+  const double ws = sums_to<kWaves>(s.masses[0][i]), ws1 = both ? sums_to<kWaves>(s.masses[1][i]) : ws;
+  const int before = __builtin_amdgcn_readfirstlane(wave) - 1;
+  if (t == 0) {
+    s.count_ends[0] = 0;
+    s.mass_ends[0] = 0.0;
   }
-  s.count_ends[t] = c0;
-  s.mass_ends[t] = w0;
-  *sum1 = both ? all1 : all;
+  s.count_ends[t + 1] = before < 0 ? c : __builtin_amdgcn_readlane(cs, before < 0 ? 0 : before) + c;
+  s.mass_ends[t + 1] = before < 0 ? w : lane_value(ws, before < 0 ? 0 : before) + w;
+  *sum1 = lane_value(ws1, kWaves - 1);
   __syncthreads();
 }
 
@@ -527,7 +546,7 @@ __device__ __forceinline__ Choice choose(const Entries& x, const Settings& q, bo
   }
   const double steps = floor((at - p.mass) / p.weight);
   const uint32_t which = !(steps > 0.0) ? 0 : steps < (double)here ? (uint32_t)steps : here - 1;
-  return Choice{p.key, n, which, ((double)value_of(p.key) - x.top) * x.per - log(sum)};
+  return Choice{p.key, n, which, ((double)value_of(p.key) - x.top) * x.per, sum};
 }
 
 // id of the entry `which` (in order of ids) of those of a value: their ids go into a list where the counters were
@@ -695,7 +714,7 @@ __device__ __attribute__((noinline)) void draw_by_passes(const SampleArgs a, int
   const Choice c = choose(passes, q, greedy);
   const double sum1 = !a.nll ? 1.0 : q.tau == 1.0 ? passes.sum : passes.sum_at(1.0);
   const int token = find_entry(row, c.key, c.which, s);
-  put(a, r, token, c.logprob, log(sum1) + (passes.top - (double)value_of(c.key)), c.kept, 0);
+  put(a, r, token, c.logit - log(c.sum), log(sum1) + (passes.top - (double)value_of(c.key)), c.kept, 0);
 }
 
 // (a workgroup has one row: in a loop over rows what only threadIdx decides would be kept in registers from one to the next)
@@ -781,7 +800,7 @@ __device__ __forceinline__ void count_entries(const Row& row, int longest, Share
 // Rows of calls that have few of them are counted in parts, by a workgroup each.  What a part leaves in the workspace:
 struct Part {
   uint32_t counts[kOthers];
-  uint32_t zeros, near, big, odd;
+  uint32_t zeros, near, big, odd;  // (sixteen bytes, aligned)
   uint32_t near_list[kNear];
 };
 static_assert(sizeof(Part) == kSamplePartBytes, "");
@@ -820,24 +839,37 @@ __global__ __launch_bounds__(kThreads, 8) void sample_count_kernel(SampleArgs a)
 
 // The counts of a row out of those of its parts, all threads.
 __device__ __forceinline__ void join_parts(const Part* parts, int n, uint32_t mask, Shared& s) {
-  for (int i = threadIdx.x; i < (int)kOthers / 4; i += kThreads) {
+  // (all requested together, of parts that are not there the last one's again: a round trip each would take longer than the counts)
+  const int t = threadIdx.x;
+  constexpr int kQuads = kOthers / 4, kMine = (kQuads + kThreads - 1) / kThreads;
+  uint4 rest[kSampleParts], v[kMine][kSampleParts];
+#pragma unroll
+  for (int p = 0; p < kSampleParts; ++p) {
+    const Part& part = parts[p < n ? p : n - 1];
+    rest[p] = *reinterpret_cast<const uint4*>(&part.zeros);
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) v[m][p] = reinterpret_cast<const uint4*>(part.counts)[t + m * kThreads < kQuads ? t + m * kThreads : t];
+  }
+#pragma unroll
+  for (int m = 0; m < kMine; ++m) {
     uint4 sum = make_uint4(0, 0, 0, 0);
-#pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-      const uint4 v = reinterpret_cast<const uint4*>(parts[p].counts)[i];
-      sum = make_uint4(sum.x + (v.x & mask), sum.y + (v.y & mask), sum.z + (v.z & mask), sum.w + (v.w & mask));
+#pragma unroll
+    for (int p = 0; p < kSampleParts; ++p) {
+      const uint32_t here = p < n ? mask : 0;
+      sum = make_uint4(sum.x + (v[m][p].x & here), sum.y + (v[m][p].y & here), sum.z + (v[m][p].z & here), sum.w + (v[m][p].w & here));
     }
-    reinterpret_cast<uint4*>(s.counts)[i] = sum;
+    if (t + m * kThreads < kQuads) reinterpret_cast<uint4*>(s.counts)[t + m * kThreads] = sum;
   }
   uint32_t zeros = 0, near = 0, big = 0, odd = 0;
-#pragma unroll 4
-  for (int p = 0; p < n; ++p) {
-    zeros += parts[p].zeros;
-    const uint32_t here = parts[p].near;
+#pragma unroll
+  for (int p = 0; p < kSampleParts; ++p) {
+    if (p >= n) break;
+    const uint32_t here = rest[p].y;
+    zeros += rest[p].x;
     if (near + here < kNear && threadIdx.x < here) s.near_list[near + threadIdx.x] = parts[p].near_list[threadIdx.x];
     near = near + here < kNear ? near + here : kNear;  // (no more than fit are looked at)
-    big += parts[p].big;
-    odd |= parts[p].odd;
+    big += rest[p].z;
+    odd |= rest[p].w;
   }
   if (threadIdx.x < kNear) {
     s.near_keys[threadIdx.x] = threadIdx.x ? kBelowNear : 0x8000;
@@ -865,14 +897,6 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   const float tau = a.taus ? a.taus[r] : a.tau, top_p = a.top_ps ? a.top_ps[r] : a.top_p, min_p = a.min_ps ? a.min_ps[r] : a.min_p;
   const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
   const float u = a.u[r];
-  if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
-      !(u >= 0.0f && u < 1.0f)) {
-    put(a, r, -1, nan, nan, 0, NPD_DEV_BAD_SAMPLING);
-    return;
-  }
-  const bool greedy = tau == 0.0f;
-  const double t = greedy ? 1.0 : (double)tau;
-  const Settings q = {t, 1.0 / t, top_p, min_p, u, (uint32_t)top_k};
   const Row row = {a.x + r * a.stride, a.V, row_split(a.x + r * a.stride, a.V, true)};
   const Part* parts = SPLIT ? reinterpret_cast<const Part*>(a.workspace) + r * a.parts : nullptr;
 
@@ -885,6 +909,15 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
     __syncthreads();
     count_entries(row, a.V, s);
   }
+  // (they were requested before the row)
+  if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
+      !(u >= 0.0f && u < 1.0f)) {
+    put(a, r, -1, nan, nan, 0, NPD_DEV_BAD_SAMPLING);
+    return;
+  }
+  const bool greedy = tau == 0.0f;
+  const double t = greedy ? 1.0 : (double)tau;
+  const Settings q = {t, 1.0 / t, top_p, min_p, u, (uint32_t)top_k};
   const uint32_t big = s.big;
   const bool odd = s.odd || s.near >= kNear;
   if (s.near && !odd) order_near(s);
@@ -896,15 +929,16 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   // Numbers below -256 have no weight that 64 bits would show beside the largest's (2^-90 times at most 2^26 of them) where that is
   // 64 temperatures above -256, and are none that a min-p would keep.
   const double room = counted_top + 256.0;
-  const bool apart = room >= 64.0 && room >= 64.0 * q.tau && (q.min_p == 0.0 || room > q.tau * (1.0 - log(q.min_p)));
-  if (odd || !top_key || (big && !apart)) {
+  const bool apart = !big || (room >= 64.0 && room >= 64.0 * q.tau && (q.min_p == 0.0 || room > q.tau * (1.0 - log(q.min_p))));
+  if (odd || !top_key || !apart) {
     draw_by_passes(a, r, row, q, greedy, s);
     return;
   }
   double sum1;  // of the weights at temperature 1
   weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
   if (threadIdx.x < kWave) {
-    const Counted counted{s, mask, top_key, s.count_ends[kThreads - 1], counted_top, q.per, s.mass_ends[kThreads - 1]};
+    const int end = (threadIdx.x + 1) * Counted::kPer;
+    const Counted counted{s, mask, top_key, s.count_ends[kThreads], counted_top, q.per, s.mass_ends[kThreads], s.count_ends[end], s.mass_ends[end]};
     Choice mine = choose(counted, q, greedy);
     if (mine.kept == counted.all && big && !greedy && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
       const uint32_t all = counted.all + big;
@@ -912,9 +946,10 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
     }
     if (threadIdx.x == 0) s.choice = mine;
   }
-  if (threadIdx.x == kWave) s.log1 = log(sum1);  // (beside the search)
+  if (threadIdx.x == kWave) s.logs[1] = log(sum1);  // (beside the search)
   __syncthreads();
   const Choice c = s.choice;
+  if (threadIdx.x == kWave) s.logs[0] = log(c.sum);  // (likewise: for the entry)
   // what there is about the value where it has a counter; of a row in parts the part that has the entry
   Row where = row;
   int first = 0;
@@ -940,7 +975,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   const Places places = places_of(where, longest);
   const bool once = places.there && (here & places.mask) == 1;
   const int token = first + (once ? find_place(where, c.key, here >> kCountBits, places.shift, s) : find_entry(where, c.key, which, s));
-  put(a, r, token, c.logprob, s.log1 + (counted_top - (double)value_of(c.key)), c.kept, 0);
+  put(a, r, token, c.logit - s.logs[0], s.logs[1] + (counted_top - (double)value_of(c.key)), c.kept, 0);
 }
 
 }  // namespace
