@@ -958,16 +958,23 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   if (bits >= kFirst) {
     if constexpr (SPLIT) {
       const uint32_t part_mask = places_of(row, longest).mask;
-      for (int p = 0; p < a.parts; ++p) {
-        here = parts[p].counts[i];
-        if (which < (here & part_mask)) {
-          const Span span = part_of(a.V, a.parts, p);
-          first = span.first;
-          where = row_part(row.p, span);
-          break;
+      uint32_t of[kSampleParts];  // (all requested together)
+#pragma unroll
+      for (int p = 0; p < kSampleParts; ++p) of[p] = parts[p < a.parts ? p : a.parts - 1].counts[i];
+      int at = -1;
+#pragma unroll
+      for (int p = 0; p < kSampleParts; ++p) {
+        if (at >= 0 || p >= a.parts) continue;
+        if (which < (of[p] & part_mask)) {
+          at = p;
+          here = of[p];
+        } else {
+          which -= of[p] & part_mask;
         }
-        which -= here & part_mask;
       }
+      const Span span = part_of(a.V, a.parts, at < 0 ? 0 : at);
+      first = span.first;
+      where = row_part(row.p, span);
     } else {
       here = s.counts[i];
     }
