@@ -509,9 +509,8 @@ struct Settings {
 };
 
 template <class Entries>
-__device__ __forceinline__ Choice choose(const Entries& x, const Settings& q, bool greedy) {
+__device__ __forceinline__ Choice choose(const Entries& x, const Settings& q) {
   uint32_t n = q.top_k > 0 && q.top_k < x.all ? q.top_k : x.all;
-  if (greedy) n = 1;
   Place end{};  // where the first n end
   double sum = x.sum;
   auto cut = [&]() {
@@ -711,7 +710,7 @@ __device__ __attribute__((noinline)) void draw_by_passes(const SampleArgs a, int
   }
   Passes passes{row, s, most, 0, value_of(most), 0.0, 0.0};
   passes.begin(q.per);
-  const Choice c = choose(passes, q, greedy);
+  const Choice c = greedy ? Choice{most, 1, 0, 0.0, 1.0} : choose(passes, q);
   const double sum1 = !a.nll ? 1.0 : q.tau == 1.0 ? passes.sum : passes.sum_at(1.0);
   const int token = find_entry(row, c.key, c.which, s);
   put(a, r, token, c.logit - log(c.sum), log(sum1) + (passes.top - (double)value_of(c.key)), c.kept, 0);
@@ -934,13 +933,15 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
     draw_by_passes(a, r, row, q, greedy, s);
     return;
   }
-  double sum1;  // of the weights at temperature 1
-  weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
-  if (threadIdx.x < kWave) {
+  double sum1 = 1.0;  // of the weights at temperature 1
+  if (!greedy || a.nll) weigh(s, n, counted_top, q.per, a.nll != nullptr, &sum1);
+  if (greedy) {
+    if (threadIdx.x == 0) s.choice = Choice{top_key, 1, 0, 0.0, 1.0};
+  } else if (threadIdx.x < kWave) {
     const int end = (threadIdx.x + 1) * Counted::kPer;
     const Counted counted{s, mask, top_key, s.count_ends[kThreads], counted_top, q.per, s.mass_ends[kThreads], s.count_ends[end], s.mass_ends[end]};
-    Choice mine = choose(counted, q, greedy);
-    if (mine.kept == counted.all && big && !greedy && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
+    Choice mine = choose(counted, q);
+    if (mine.kept == counted.all && big && q.min_p == 0.0 && q.top_p == 1.0) {  // nothing is cut off, or by top-k alone
       const uint32_t all = counted.all + big;
       mine.kept = q.top_k > 0 && q.top_k < all ? q.top_k : all;
     }
