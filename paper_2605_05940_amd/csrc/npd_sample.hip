@@ -85,17 +85,19 @@ struct Row {
 
 // eight(g, bits of eight entries) of the row's aligned groups, the next kAhead of them always requested, and one(id, bits) of the
 // entries around them.  (No load is behind a branch: the compiler would wait for all of them where paths meet.  Those behind the
-// row's end read its last group again.)
+// row's end read its last group again.)  begin() is done while the first are on their way.
 constexpr int kAhead = 6;
-template <class E, class F>
-__device__ __forceinline__ void each_group(const Row& r, E&& eight, F&& one) {
+template <class E, class F, class B>
+__device__ __forceinline__ void each_group(const Row& r, B&& begin, E&& eight, F&& one) {
   const int n = r.split.nvec, t = thread_of_phase();
+  if (n == 0) begin();
   if (n > 0) {
     const uint4* groups = reinterpret_cast<const uint4*>(r.p + r.split.head);
     auto load = [&](int g) { return groups[g < n ? g : n - 1]; };
     uint4 v[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) v[u] = load(t + u * kThreads);
+    begin();
     int g = 0;
 #pragma unroll 1
     for (; g + kAhead * kThreads <= n; g += kAhead * kThreads) {
@@ -568,7 +570,7 @@ __device__ __forceinline__ int find_entry(const Row& row, uint32_t key, uint32_t
   };
   const uint32_t bits2 = bits * 0x10001u, mask2 = mask * 0x10001u;
   each_group(
-      row,
+      row, [] {},
       [&](int g, const uint4& v) {
         const int id = row.split.head + 8 * g;
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -732,7 +734,8 @@ __device__ __forceinline__ void begin_counts(Shared& s) {
 constexpr unsigned short kTurnedFirst = 2 * kFirst, kTurnedForbidden = 0xff01 - kTurnedFirst;
 
 // Counts a row's entries; zero in the first of near_counts, what else is closer to zero than the counters' in near_list.
-__device__ __forceinline__ void count_entries(const Row& row, int longest, Shared& s) {
+template <class B>
+__device__ __forceinline__ void count_entries(const Row& row, int longest, Shared& s, B&& begin) {
   uint32_t big = 0, odd = 0;  // large negative numbers; entries that have no counter otherwise
   auto other = [&](uint32_t b) {
     const uint32_t size = b & 0x7fff;
@@ -754,6 +757,11 @@ __device__ __forceinline__ void count_entries(const Row& row, int longest, Share
   const Places places = places_of(row, longest);
   each_group(
       row,
+      [&] {
+        begin();
+        begin_counts(s);
+        __syncthreads();
+      },
       [&](int g, const uint4& v) {
         const uint32_t unit = 1u + (places.there ? (uint32_t)(g >> places.shift) << kCountBits : 0u);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -822,9 +830,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_count_kernel(SampleArgs a)
   __shared__ Shared s;
   const int64_t r = blockIdx.y;
   if (a.mask && !a.mask[r]) return;
-  begin_counts(s);
-  __syncthreads();
-  count_entries(row_part(a.x + r * a.stride, part_of(a.V, a.parts, blockIdx.x)), part_of(a.V, a.parts, 0).end, s);
+  count_entries(row_part(a.x + r * a.stride, part_of(a.V, a.parts, blockIdx.x)), part_of(a.V, a.parts, 0).end, s, [] {});
   Part& part = reinterpret_cast<Part*>(a.workspace)[r * a.parts + blockIdx.x];
   for (int i = threadIdx.x; i < (int)kOthers / 4; i += kThreads) reinterpret_cast<uint4*>(part.counts)[i] = reinterpret_cast<uint4*>(s.counts)[i];
   if (threadIdx.x < kNear) part.near_list[threadIdx.x] = s.near_list[threadIdx.x];
@@ -900,13 +906,11 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
   const Part* parts = SPLIT ? reinterpret_cast<const Part*>(a.workspace) + r * a.parts : nullptr;
 
   const int longest = SPLIT ? part_of(a.V, a.parts, 0).end : a.V;
-  begin_exponentials(s);
   if constexpr (SPLIT) {
+    begin_exponentials(s);
     join_parts(parts, a.parts, places_of(row, longest).mask, s);
   } else {
-    begin_counts(s);
-    __syncthreads();
-    count_entries(row, a.V, s);
+    count_entries(row, a.V, s, [&] { begin_exponentials(s); });
   }
   // (they were requested before the row)
   if (!(tau >= 0.0f && tau <= 3.4028234663852886e38f) || !(top_p >= 0.0f && top_p <= 1.0f) || !(min_p >= 0.0f && min_p <= 1.0f) || top_k < 0 ||
