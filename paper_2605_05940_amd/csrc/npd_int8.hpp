@@ -40,9 +40,14 @@ struct Int8Args {
 hipError_t launch_int8_few(const Int8Args& a, hipStream_t stream);
 // Any number of rows; rows of h and w begin on 16 bytes and their padding to a multiple of 16 may be read, of which h's is 0.
 hipError_t launch_int8_many(const Int8Args& a, hipStream_t stream);
-// rows of `to` are those of `from` and zeros up to to_width bytes, a multiple of 16
-hipError_t launch_int8_pack(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width, int64_t rows, int32_t cols,
-                            hipStream_t stream);
+// rows of `to` are those of `from` and zeros up to to_width bytes, a multiple of 16; two matrices of one width, either of no rows
+struct Int8Packed {
+  const int8_t* from;
+  int64_t stride;
+  int8_t* to;
+  int64_t rows;
+};
+hipError_t launch_int8_pack(const Int8Packed& first, const Int8Packed& second, int32_t to_width, int32_t cols, hipStream_t stream);
 
 // what npd_head_logits_int8 needs (npd_int8_api.hip)
 size_t int8_workspace_bytes(const npd_head_desc* desc);

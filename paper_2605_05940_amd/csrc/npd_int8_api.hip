@@ -112,17 +112,18 @@ npd_status npd_head_logits_int8(const npd_head_desc* desc, const int8_t* hidden,
   a.out = static_cast<uint16_t*>(logits);
   a.out_stride = d.logits_stride;
   if (p.few) return launch_int8_few(a, on) == hipSuccess ? NPD_OK : NPD_ERR_HIP;
-  if (p.pack_h) {
-    int8_t* to = reinterpret_cast<int8_t*>(ws + p.h);
-    if (launch_int8_pack(a.h, a.h_stride, to, p.padded, T, d.width, on) != hipSuccess) return NPD_ERR_HIP;
-    a.h = to;
-    a.h_stride = p.padded;
-  }
-  if (p.pack_w) {
-    int8_t* to = reinterpret_cast<int8_t*>(ws + p.w);
-    if (launch_int8_pack(a.w, a.w_stride, to, p.padded, d.vocab, d.width, on) != hipSuccess) return NPD_ERR_HIP;
-    a.w = to;
-    a.w_stride = p.padded;
+  if (p.pack_h || p.pack_w) {
+    const Int8Packed h = {a.h, a.h_stride, reinterpret_cast<int8_t*>(ws + p.h), p.pack_h ? T : 0};
+    const Int8Packed w = {a.w, a.w_stride, reinterpret_cast<int8_t*>(ws + p.w), p.pack_w ? d.vocab : 0};
+    if (launch_int8_pack(h, w, p.padded, d.width, on) != hipSuccess) return NPD_ERR_HIP;
+    if (p.pack_h) {
+      a.h = h.to;
+      a.h_stride = p.padded;
+    }
+    if (p.pack_w) {
+      a.w = w.to;
+      a.w_stride = p.padded;
+    }
   }
   return launch_int8_many(a, on) == hipSuccess ? NPD_OK : NPD_ERR_HIP;
 }

@@ -306,13 +306,32 @@ __global__ __launch_bounds__(kHeadThreads, 3) void int8_few_kernel(Int8Args a) {
   finish_columns<kPart>(a, &lds.x[0][0]);
 }
 
-constexpr int kPackThreads = 256;
-__global__ __launch_bounds__(kPackThreads) void int8_pack_kernel(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width,
-                                                                 int64_t rows, int32_t cols) {
-  // (a wave per row)
-  for (int64_t p = (int64_t)blockIdx.x * (kPackThreads / kWave) + (threadIdx.x >> 6); p < rows; p += (int64_t)gridDim.x * (kPackThreads / kWave))
-    for (int d = (threadIdx.x & 63) * 16; d < to_width; d += kWave * 16)
-      *reinterpret_cast<i32x4*>(to + p * to_width + d) = load16_of(from + p * from_stride, d, cols);
+// A wave has four rows, of either matrix, whose loads are requested together.  The last bytes of a row come with those before them, and
+// are moved to their place (byte by byte behind a branch they take as long as all others).  50,336 rows of 1,000 bytes 18.7 us (5.4
+// TB/s; a row at a time and two launches 24).
+constexpr int kPackThreads = 256, kPackRows = 4;
+__global__ __launch_bounds__(kPackThreads) void int8_pack_kernel(Int8Packed first, Int8Packed second, int32_t to_width, int32_t cols) {
+  const int64_t rows = first.rows + second.rows, step = (int64_t)gridDim.x * (kPackThreads / kWave) * kPackRows;
+  for (int64_t r = ((int64_t)blockIdx.x * (kPackThreads / kWave) + (threadIdx.x >> 6)) * kPackRows; r < rows; r += step)
+    for (int d = (threadIdx.x & 63) * 16; d < to_width; d += kWave * 16) {
+      const int at = d + 16 <= cols ? d : cols - 16, behind = d - at;  // (behind: bytes that others have, 16 and more of padding)
+      i32x4 v[kPackRows];
+      int8_t* to[kPackRows];
+#pragma unroll
+      for (int u = 0; u < kPackRows; ++u) {
+        const int64_t p = r + u < rows ? r + u : rows - 1;
+        const bool of_first = p < first.rows;
+        const int8_t* from = of_first ? first.from + p * first.stride : second.from + (p - first.rows) * second.stride;
+        to[u] = (of_first ? first.to + p * to_width : second.to + (p - first.rows) * to_width) + d;
+        v[u] = cols >= 16 ? load16(from + at) : load16_of(from, d, cols);  // uniform
+      }
+#pragma unroll
+      for (int u = 0; u < kPackRows; ++u) {
+        if (cols >= 16 && behind > 0)
+          v[u] = behind < 16 ? __builtin_bit_cast(i32x4, __builtin_bit_cast(unsigned __int128, v[u]) >> (8 * behind)) : i32x4{0, 0, 0, 0};
+        if (r + u < rows) *reinterpret_cast<i32x4*>(to[u]) = v[u];
+      }
+    }
 }
 
 template <int RT>
@@ -351,11 +370,11 @@ hipError_t launch_int8_few(const Int8Args& a, hipStream_t stream) {
   return launch_fragments<4>(a, stream);
 }
 
-hipError_t launch_int8_pack(const int8_t* from, int64_t from_stride, int8_t* to, int32_t to_width, int64_t rows, int32_t cols,
-                            hipStream_t stream) {
-  const int64_t blocks = (rows + kPackThreads / kWave - 1) / (kPackThreads / kWave);
-  return launch_kernel(int8_pack_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kPackThreads), 0, stream, from, from_stride, to,
-                       to_width, rows, cols);
+hipError_t launch_int8_pack(const Int8Packed& first, const Int8Packed& second, int32_t to_width, int32_t cols, hipStream_t stream) {
+  constexpr int kRows = kPackThreads / kWave * kPackRows;
+  const int64_t blocks = (first.rows + second.rows + kRows - 1) / kRows;
+  return launch_kernel(int8_pack_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kPackThreads), 0, stream, first, second,
+                       to_width, cols);
 }
 
 }  // namespace npd
