@@ -9,11 +9,12 @@
 // more of those, or an entry beyond 2^8 that may matter, is done by bisection over the values, with a pass over the row for each step.
 //
 // Counting bounds it: eleven vector instructions and two LDS additions for a pair of entries (262,144 take a compute unit 16 us, where
-// its share of the memory's rate would be 20), then some 10 us of dependent steps, most of them one wave's or between barriers.
-// Measured (MI355X, us): 256 rows of 151,936, top-k 50, top-p 0.9: 32.1 (read and counted 17, largest value 1.5, weights 4.7, search 3.5,
-// the token's id 1 to 8); one row of 262,144 in eight parts 21.5, whole 32; 2,048 rows of 151,936 greedy 160 (3.9 TB/s), untruncated 206:
-// where the token's value occurs more than once its row is read again.  4,096 rows of 1,000 take 112: rows that short are not what this
-// is made for.  Workgroups of 512 threads, three to a compute unit, are 8 to 13 % faster for those, and 16 % slower for 48 rows of 50,003.
+// its share of the memory's rate would be 20), then some 6 us of dependent steps, most of them one wave's or between barriers.
+// Measured (MI355X, us): 256 rows of 151,936, top-k 50, top-p 0.9: 26.7 (read and counted 11.3, largest value 1, weights 2.8, search 2.2,
+// the token's id .5 to 5); one row of 262,144 in eight parts 17.6, whole 34; 2,048 rows of 151,936 greedy 147 (4.2 TB/s), untruncated 191:
+// where the token's value occurs more than once its row is read again.  4,096 rows of 1,000 take 67: rows that short are not what this
+// is made for.  (With longer steps, 112 then, workgroups of 512 threads, three to a compute unit, were 8 to 13 % faster for those, and 16 %
+// slower for 48 rows of 50,003.)
 #include <stddef.h>
 
 #include "../../include/npd.h"
@@ -993,9 +994,10 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
 }  // namespace
 
 // As many parts as give every compute unit one and leave each 32,768 entries, and at least three: a second launch and the joining of the
-// counts have to be earned.  Measured (MI355X, us, whole / in parts, untruncated): 1 row of 65,536 17.5 / 18.7 (4 parts), of 100,000 19.8 / 19.9
-// (4), of 128,256 21.9 / 20.0 (4), of 151,936 24 / 20.6 (4), 22.0 (8), of 262,144 32 / 22.3 (8), of 600,000 60 / 26.2 (8), 28.5 (4); 32 rows of
-// 50,048 18 / 22 (3), of 151,936 28 / 24.1 (4), 26.9 (8), of 262,144 39 / 26.9 (8).
+// counts have to be earned.  Measured (MI355X, us, whole / in parts, untruncated): 1 row of 100,000 16.1 / 16.4 (3 parts), of 128,256 18.2 / 17.7
+// (3), of 151,936 17.8 / 16.3 (4), of 262,144 34 / 18.5 (8), of 600,000 51 / 18.6 (8); 32 rows of 100,000 19.0 / 19.4 (3), of 151,936 24.9 / 21.1
+// (4), of 262,144 37 / 22.1 (8); 64 rows of 128,256 23.1 / 23.0 (3), of 151,936 26.1 / 23.2 (4).  With top-k 50 and top-p 0.9, where few rows are
+// read again, 64 rows of 100,000 18.9 / 21.9, of 151,936 22.5 / 23.6, of 262,144 30.6 / 25.2.
 int sample_parts(int64_t T, int32_t V) {
   const int64_t most = 256 / T < kSampleParts ? 256 / T : kSampleParts, some = V / 32768, parts = most < some ? most : some;
   return parts < 3 ? 1 : (int)parts;
