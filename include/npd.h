@@ -535,8 +535,9 @@ typedef struct {
  *   y     bf16 [T, y_stride], required; what lies between D and the stride is left as it was
  *   mean  fp32 [T] or NULL (with NPD_NORM_RMS: NULL)      rstd  fp32 [T] or NULL
  *
- * Statistics are fp32 (sums of squares beyond that range, of values of 1e17 and more, give rstd 0).  A row of equal values has
- * that mean exactly and gives the bias; with eps = 0 it has no rstd (inf) and gives NaN.  NaN or infinities stay in their row.
+ * Statistics are fp32, of rows of any finite values (also where their sums or squares lie beyond fp32 or below it; an rstd that does
+ * is written as inf, and y is right all the same).  A row of equal values has that mean exactly and gives the bias; with eps = 0 it
+ * has no rstd (inf) and gives NaN.  NaN or infinities stay in their row.
  */
 npd_status npd_layer_norm(const npd_norm_desc* desc, const void* x, const void* weight, const void* bias, void* y,
                           float* mean, float* rstd, void* stream);

@@ -5,6 +5,8 @@
 // Bytes bound it.  Measured (MI355X, 32,768 x 2,048): forward 48.4 us (5.5 TB/s), backward with both parameters' gradients 82.8 (4.9 TB/s;
 // torch's copy of 4 GiB reaches 4.7), of which joining the 512 pieces of those is 4.  With what is unpacked kept in registers, and so one
 // or two waves per SIMD, 56.8 and 110.  One row of 2,048 3.6 us.
+#include <float.h>
+
 #include "../../include/npd.h"
 #include "npd_head_gemm.hpp"
 #include "npd_norm.hpp"
@@ -13,6 +15,7 @@ namespace npd {
 namespace {
 
 constexpr int kNormThreads = 256;  // of a workgroup with rows of a wave each
+constexpr int kNormMostRows = 64;  // one after the other of norm_kernel's threads
 
 template <int TH>
 constexpr int norm_block() { return TH < kNormThreads ? kNormThreads : TH; }
@@ -38,6 +41,26 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* smem) {
       v[n] = t;
     }
   }
+}
+
+// the largest of the numbers, of up to 24 bits, of a row's TH threads
+template <int TH>
+__device__ __forceinline__ uint32_t row_most(uint32_t v, float* smem) {
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) {
+    const uint32_t o = __shfl_xor(v, off, kWave);
+    v = v > o ? v : o;
+  }
+  if constexpr (TH > kWave) {
+    __syncthreads();  // (likewise)
+    if ((threadIdx.x & 63) == 0) smem[threadIdx.x >> 6] = (float)v;
+    __syncthreads();
+    for (int w = 0; w < TH / kWave; ++w) {
+      const uint32_t o = (uint32_t)smem[w];
+      v = v > o ? v : o;
+    }
+  }
+  return v;
 }
 
 // Values [d, d + 8) of a row, 0 behind its end.  WHOLE: rows are whole groups of eight (what ends of groups take otherwise, in code and
@@ -72,22 +95,77 @@ __device__ __forceinline__ void stay_packed(uint4 (&w)[G]) {
   for (int u = 0; u < G; ++u) asm volatile("" : "+v"(w[u].x), "+v"(w[u].y), "+v"(w[u].z), "+v"(w[u].w));
 }
 
+// A row whose sums or squares fp32 does not hold, done again: read for each of its sums and for y, a value at a time (no model has such
+// rows; 32,768 of them of 2,048 take 305 us, others 44).  With its largest value's power of two taken out, which is exact, nothing leaves
+// fp32, and the variance is put together in 64 bits.  A row that is not finite stays as it came out.  (Threads have the values that they
+// have in norm_kernel: what was written there is written again by the same thread.)
+template <int TH, int G>
+__device__ __forceinline__ void norm_wide_row(const NormArgs& a, int64_t p, float* smem) {
+  int thread = threadIdx.x;
+  asm volatile("" : "+v"(thread));  // (nothing that this needs is kept in registers over the other rows)
+  const uint16_t* row = a.x + p * a.x_stride;
+  const auto each = [&](auto&& f) {
+#pragma unroll 1
+    for (int i = 0; i < 8 * G; ++i) {
+      const int d = (thread % TH) * 8 + 8 * TH * (i >> 3) + (i & 7);
+      if (d < a.D) f(d, bf16_one(row[d]));
+    }
+  };
+  uint32_t most = 0;
+  each([&](int, float v) {
+    const uint32_t size = __builtin_bit_cast(uint32_t, v) << 1 >> 17;
+    most = most > size ? most : size;
+  });
+  most = row_most<TH>(most, smem);
+  if (most >= 0x7f80) return;  // uniform over the row
+  const int e = __builtin_amdgcn_frexp_expf(bf16_one((uint16_t)most)), exponent = e < -100 ? -100 : e > 126 ? 126 : e;
+  const float by = __builtin_ldexpf(1.0f, -exponent);
+  float mean = 0.0f, s[1] = {0.0f};  // of the row times `by`
+  if (!a.rms) {
+    each([&](int, float v) { s[0] += v * by; });
+    row_sums<TH, 1>(s, smem);
+    mean = s[0] / (float)a.D;
+  }
+  s[0] = 0.0f;
+  each([&](int, float v) {
+    const float d = __builtin_fmaf(v, by, -mean);
+    s[0] = __builtin_fmaf(d, d, s[0]);
+  });
+  row_sums<TH, 1>(s, smem);
+  const double r = 1.0 / __builtin_sqrt(__builtin_ldexp((double)s[0] / a.D, 2 * exponent) + (double)a.eps);
+  const float rstd = (float)(s[0] > 0.0f ? __builtin_ldexp(r, exponent) : r);  // (of equal values: any finite number would do)
+  if (threadIdx.x % TH == 0) {
+    if (a.mean) a.mean[p] = __builtin_ldexpf(mean, exponent);
+    if (a.rstd) a.rstd[p] = (float)r;
+  }
+  uint16_t* out = a.y + p * a.y_stride;
+  each([&](int d, float v) {
+    const float w = a.w ? bf16_one(a.w[d]) : 1.0f, b = a.b ? bf16_one(a.b[d]) : 0.0f;
+    out[d] = one_bf16(__builtin_fmaf(__builtin_fmaf(v, by, -mean) * rstd, w, b));
+  });
+}
+
 template <int TH, int G, bool WHOLE>
 __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
   __shared__ float smem[norm_block<TH>() / kWave];
   constexpr int kRows = norm_block<TH>() / TH;  // a workgroup's at a time
   const int at = (threadIdx.x % TH) * 8;        // + 8 TH u
-  uint4 w[G], b[G];
+  // (of the widest rows the bias is read where it is added: there are no registers for it, 1,024 x 65,536 69 us, with it kept 90)
+  constexpr bool kHoldBias = G < 8;
+  uint4 w[G], b[kHoldBias ? G : 1];
+  const auto bias = [&](int u) { return a.b ? read8<WHOLE>(a.b, at + 8 * TH * u, a.D) : make_uint4(0, 0, 0, 0); };
 #pragma unroll
   for (int u = 0; u < G; ++u) {
     w[u] = a.w ? read8<WHOLE>(a.w, at + 8 * TH * u, a.D) : make_uint4(kOnes, kOnes, kOnes, kOnes);
-    b[u] = a.b ? read8<WHOLE>(a.b, at + 8 * TH * u, a.D) : make_uint4(0, 0, 0, 0);
+    if constexpr (kHoldBias) b[u] = bias(u);
   }
   const float per = 1.0f / (float)a.D;
+  uint64_t wide = 0;  // which of the rows so far are to be done again (kNormMostRows at most)
+  int n = 0;
   for (int64_t p = (int64_t)blockIdx.x * kRows + threadIdx.x / TH; p < a.T; p += (int64_t)gridDim.x * kRows) {
     const uint16_t* row = a.x + p * a.x_stride;
     stay_packed(w);
-    stay_packed(b);
+    if constexpr (kHoldBias) stay_packed(b);
     uint4 x[G];
 #pragma unroll
     for (int u = 0; u < G; ++u) x[u] = read8<WHOLE>(row, at + 8 * TH * u, a.D);
@@ -118,6 +196,9 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
     row_sums<TH, 1>(s, smem);
     stay_packed(x);
     const float rstd = 1.0f / __builtin_sqrtf(__builtin_fmaf(s[0], per, a.eps));
+    // (Sums and squares beyond fp32 are not finite.  Squares below it are off by 2^-150 each, nothing beside a variance of 2^-100.)
+    if (__ballot(!(rstd >= 0x1p-64f && rstd <= 0x1p50f))) wide |= (uint64_t)1 << n;  // (a row's threads have the same)
+    ++n;
     if (threadIdx.x % TH == 0) {
       if (a.mean) a.mean[p] = mean;
       if (a.rstd) a.rstd[p] = rstd;
@@ -128,12 +209,18 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
       float v[8], wv[8], bv[8];
       unpack8(x[u], v);
       unpack8(w[u], wv);
-      unpack8(b[u], bv);
+      unpack8(kHoldBias ? b[kHoldBias ? u : 0] : bias(u), bv);
 #pragma unroll
       for (int t = 0; t < 8; ++t) v[t] = __builtin_fmaf((v[t] - mean) * rstd, wv[t], bv[t]);
       store8_of<WHOLE>(out, at + 8 * TH * u, a.D, v);
     }
   }
+  // (Behind the loop, where they need none of its registers, and with the kernel's one argument read again: in the loop 32,768 x 2,047
+  // takes 61.7 us, so 56.7.)
+  const NormArgs* again = (const NormArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(again));
+  for (; wide; wide &= wide - 1)
+    norm_wide_row<TH, G>(*again, ((int64_t)blockIdx.x + (int64_t)__builtin_ctzll(wide) * gridDim.x) * kRows + threadIdx.x / TH, smem);
 }
 
 // HELD: the workgroup's sums over its rows for the parameters' gradients stay in registers, and go to its piece at the end.
@@ -299,8 +386,8 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormGradArgs a)
 template <int TH, int G>
 hipError_t launch_rows(const NormArgs& a, hipStream_t stream) {
   constexpr int kRows = norm_block<TH>() / TH;
-  const int64_t blocks = (a.T + kRows - 1) / kRows;
-  return launch_kernel(a.D % 8 == 0 ? norm_kernel<TH, G, true> : norm_kernel<TH, G, false>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)),
+  const int64_t blocks = (a.T + kRows - 1) / kRows, least = (blocks + kNormMostRows - 1) / kNormMostRows, most = least > 65536 ? least : 65536;
+  return launch_kernel(a.D % 8 == 0 ? norm_kernel<TH, G, true> : norm_kernel<TH, G, false>, dim3((unsigned)(blocks < most ? blocks : most)),
                        dim3(norm_block<TH>()), 0, stream, a);
 }
 
