@@ -241,7 +241,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
     uint4 g[G], x[G];
 #pragma unroll
     for (int u = 0; u < G; ++u) {
-      g[u] = read8<WHOLE>(grow, at + 8 * TH * u, a.D);  // (0 behind the end: no part in any sum)
+      g[u] = read8<WHOLE>(grow, at + 8 * TH * u, a.D);
       x[u] = read8<WHOLE>(xrow, at + 8 * TH * u, a.D);
     }
     const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
@@ -254,7 +254,9 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
       unpack8(w[u], wv);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const float n = (xv[t] - mean) * rstd, q = gv[t] * wv[t];
+        // (behind the end g is 0, but the mean times rstd may be beyond fp32)
+        const bool inside = (WHOLE ? at + 8 * TH * u : at + 8 * TH * u + t) < a.D;
+        const float n = inside ? (xv[t] - mean) * rstd : 0.0f, q = gv[t] * wv[t];
         s[0] = __builtin_fmaf(q, n, s[0]);
         s[1] += q;
         if constexpr (HELD) {
