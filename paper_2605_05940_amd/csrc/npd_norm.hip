@@ -223,6 +223,17 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_kernel(NormArgs a) {
     norm_wide_row<TH, G>(*again, ((int64_t)blockIdx.x + (int64_t)__builtin_ctzll(wide) * gridDim.x) * kRows + threadIdx.x / TH, smem);
 }
 
+// (x - mean) rstd of a row, whose difference is halved first where it could be beyond fp32
+struct RowMean {
+  float by, mean_by, rstd_by;  // rstd = by rstd_by
+  __device__ __forceinline__ float normed(float x) const { return __builtin_fmaf(x, by, -mean_by) * rstd_by; }
+};
+__device__ __forceinline__ RowMean row_mean(const NormGradArgs& a, int64_t p) {
+  const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
+  const bool large = __builtin_fabsf(mean) >= 0x1p119f;  // (bf16 ends 2^120 below 2^128, fp32 2^104)
+  return large ? RowMean{0.5f, 0.5f * mean, 2.0f * rstd} : RowMean{1.0f, mean, rstd};
+}
+
 // HELD: the workgroup's sums over its rows for the parameters' gradients stay in registers, and go to its piece at the end.
 template <int TH, int G, bool HELD, bool WHOLE>
 __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArgs a) {
@@ -244,7 +255,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
       g[u] = read8<WHOLE>(grow, at + 8 * TH * u, a.D);
       x[u] = read8<WHOLE>(xrow, at + 8 * TH * u, a.D);
     }
-    const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
+    const RowMean row = row_mean(a, p);
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int u = 0; u < G; ++u) {
@@ -256,7 +267,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
       for (int t = 0; t < 8; ++t) {
         // (behind the end g is 0, but the mean times rstd may be beyond fp32)
         const bool inside = (WHOLE ? at + 8 * TH * u : at + 8 * TH * u + t) < a.D;
-        const float n = inside ? (xv[t] - mean) * rstd : 0.0f, q = gv[t] * wv[t];
+        const float n = inside ? row.normed(xv[t]) : 0.0f, q = gv[t] * wv[t];
         s[0] = __builtin_fmaf(q, n, s[0]);
         s[1] += q;
         if constexpr (HELD) {
@@ -270,7 +281,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
     stay_packed(g);
     stay_packed(x);
     stay_packed(w);
-    const float along = s[0] * per, flat = a.rms ? 0.0f : s[1] * per;
+    const float along = s[0] * per, flat = a.rms ? 0.0f : s[1] * per, rstd = row.by * row.rstd_by;
     uint16_t* out = a.dx + p * a.dx_stride;
 #pragma unroll
     for (int u = 0; u < G; ++u) {
@@ -280,8 +291,7 @@ __global__ __launch_bounds__(norm_block<TH>()) void norm_grad_kernel(NormGradArg
       unpack8(w[u], wv);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const float n = (xv[t] - mean) * rstd;
-        gv[t] = __builtin_fmaf(-n, along, gv[t] * wv[t] - flat) * rstd;
+        gv[t] = __builtin_fmaf(-row.normed(xv[t]), along, gv[t] * wv[t] - flat) * rstd;
       }
       store8_of<WHOLE>(out, at + 8 * TH * u, a.D, gv);
     }
@@ -334,10 +344,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_columns_kernel(NormGradArgs
     float g[8], x[8];
     unpack8(load8_of(a.g + p * a.g_stride, d, a.D), g);
     unpack8(load8_of(a.x + p * a.x_stride, d, a.D), x);
-    const float mean = a.rms ? 0.0f : a.mean[p], rstd = a.rstd[p];
+    const RowMean row = row_mean(a, p);
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      dw[t] = __builtin_fmaf(g[t], (x[t] - mean) * rstd, dw[t]);
+      dw[t] = __builtin_fmaf(g[t], row.normed(x[t]), dw[t]);
       db[t] += g[t];
     }
   }

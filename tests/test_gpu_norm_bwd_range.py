@@ -30,3 +30,28 @@ def test_large_means_beside_a_small_eps(D):
     for eps in (2.0 ** -17, 2.0 ** -60):
         rstd = torch.full((T,), eps ** -0.5, device=DEV)
         check_backward(gy, x, w, x[:, 0].float().contiguous(), rstd, False)
+
+
+@pytest.mark.parametrize("D", WIDTHS)
+def test_differences_beyond_fp32(D):
+    """The largest number but for one of the other sign, with the statistics that the forward pass leaves."""
+    x, w, b, gy = inputs(4, D)
+    x.fill_(LARGEST)
+    x[1:3] *= -1
+    x[:2, D // 2] *= -1
+    x[3, 0] = 2.0 ** 119
+    got = run_forward(x, w, b, 2.0 ** -20, False)
+    rstd = got["rstd"].clone()
+    rstd[2] = 2.0 ** 10
+    check_backward(gy, x, w, got["mean"], rstd, False)
+
+
+@pytest.mark.parametrize("e", [-100, -60, 0, 60, 110, 118, 119, 120, 126])
+@pytest.mark.parametrize("D", [100, 1004, 20000])
+def test_means_of_every_size(D, e):
+    x, w, b, gy = inputs(6, D)
+    x.copy_(((1 + 0.1 * x.double().clamp(-4, 4)) * 2.0 ** e).clamp(-LARGEST, LARGEST))
+    got = run_forward(x, w, b, 0.0, False)
+    # (the gradients of a row as large as its rstd is small, so that neither leaves the numbers there are)
+    gy.mul_(2.0 ** (e // 2))
+    check_backward(gy, x, w, got["mean"], got["rstd"], False)
