@@ -56,6 +56,10 @@ __global__ __launch_bounds__(kHeadThreads, 1) void int8_tiles_kernel(Int8Args a)
     }
 #pragma unroll
     for (int c = 0; c < kR; ++c) of_rows[wave][c * kWave + lane] = hs[c];
+    // (Lanes read what others of their wave wrote.  A wave's LDS instructions are done in their order; that this is their order in the code
+    // is said here, and takes no instruction.)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 
     const SoftCap soft(CAP ? a.cap : 1.0f);
 #pragma unroll

@@ -34,3 +34,32 @@ def test_the_products_keep_their_distances(tmp_path):
             kernels += checked > 0
             assert not bad, (name, bad[0])
     assert kernels == 8
+
+
+def exchanges(instructions):
+    """Of a kernel's LDS instructions and barriers in their order: what comes before each that writes LDS."""
+    those = [i[0] for i in instructions if i[0].startswith("ds_") or i[0] == "s_barrier"]
+    return [those[n - 1] if n else None for n, op in enumerate(those) if op.startswith("ds_write")]
+
+
+@pytest.mark.skipif(OBJDUMP is None, reason="no llvm-objdump")
+def test_the_tiles_factors_are_written_before_they_are_read(tmp_path):
+    """A wave's factors lie in LDS, where lanes read what others wrote.  Nothing reads LDS between the barrier behind a tile's last step and the
+    last of these writes, which follow each other: the reads are all behind them."""
+    assert exchanges([(op,) for op in ("ds_read_b128", "s_barrier", "ds_write_b32", "ds_read_b32", "ds_write_b32")]) == ["s_barrier", "ds_read_b32"]
+    binding.load()
+    kernels = 0
+    for n, code in enumerate(device_code(binding.LIB_PATH)):
+        if b"int8_tiles_kernel" not in code:
+            continue
+        path = tmp_path / f"{n}.o"
+        path.write_bytes(code)
+        listing = subprocess.run([OBJDUMP, "-d", "--mcpu=gfx950", str(path)], capture_output=True, text=True, check=True).stdout
+        for name, instructions in parse(listing).items():
+            if "int8_tiles_kernel" not in name or len(instructions) < 100:
+                continue
+            before = exchanges(instructions)
+            kernels += 1
+            assert before and before[0] == "s_barrier", name
+            assert all(op.startswith("ds_write") for op in before[1:]), (name, before)
+    assert kernels == 8
