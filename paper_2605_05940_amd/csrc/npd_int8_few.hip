@@ -314,7 +314,7 @@ __global__ __launch_bounds__(kPackThreads) void int8_pack_kernel(Int8Packed firs
   const int64_t rows = first.rows + second.rows, step = (int64_t)gridDim.x * (kPackThreads / kWave) * kPackRows;
   for (int64_t r = ((int64_t)blockIdx.x * (kPackThreads / kWave) + (threadIdx.x >> 6)) * kPackRows; r < rows; r += step)
     for (int d = (threadIdx.x & 63) * 16; d < to_width; d += kWave * 16) {
-      const int at = d + 16 <= cols ? d : cols - 16, behind = d - at;  // (behind: bytes that others have, 16 and more of padding)
+      const int at = d + 16 <= cols ? d : cols - 16, behind = d - at;  // (behind: bytes that another lane has, 15 at most)
       i32x4 v[kPackRows];
       int8_t* to[kPackRows];
 #pragma unroll
@@ -327,8 +327,7 @@ __global__ __launch_bounds__(kPackThreads) void int8_pack_kernel(Int8Packed firs
       }
 #pragma unroll
       for (int u = 0; u < kPackRows; ++u) {
-        if (cols >= 16 && behind > 0)
-          v[u] = behind < 16 ? __builtin_bit_cast(i32x4, __builtin_bit_cast(unsigned __int128, v[u]) >> (8 * behind)) : i32x4{0, 0, 0, 0};
+        if (cols >= 16 && behind > 0) v[u] = __builtin_bit_cast(i32x4, __builtin_bit_cast(unsigned __int128, v[u]) >> (8 * behind));
         if (r + u < rows) *reinterpret_cast<i32x4*>(to[u]) = v[u];
       }
     }
