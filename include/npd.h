@@ -588,7 +588,8 @@ npd_status npd_quantize_rows(int64_t n_rows, int32_t width, int64_t x_stride, in
  *   hidden        int8 [T, hidden_stride], hidden_scale  fp32 [T], weight  int8 [V, weight_stride], weight_scale  fp32 [V], required
  *   bias          bf16 [V] or NULL         logits  bf16 [T, logits_stride], required
  *   workspace     >= npd_head_workspace_bytes(desc, NPD_HEAD_LOGITS_INT8) bytes.  Widths and strides that are multiples of 16 need
- *                 none; others are copied in calls of more than 64 positions, so weights are best laid out with such rows
+ *                 none.  In calls of more than 64 positions both matrices are copied where the width is none, wherever their rows
+ *                 begin, and a matrix alone where its stride is none; so rows are best laid out, and given, with zeros up to the next one
  */
 npd_status npd_head_logits_int8(const npd_head_desc* desc, const int8_t* hidden, const float* hidden_scale,
                                 const int8_t* weight, const float* weight_scale, const void* bias, void* logits,

@@ -704,8 +704,9 @@ def _given_or_own(workspace: Optional[torch.Tensor], bytes_of):
 
 def npd_quantize_rows(x: torch.Tensor, *, q_out: torch.Tensor, scale_out: torch.Tensor) -> None:
     """Enqueue ``scale_out = max|x| / 127`` and ``q_out = round(x / scale_out)`` of every row of a bf16 matrix, as 8-bit integers
-    (see ``npd_quantize_rows`` in npd.h).  A ``q_out`` whose rows begin on multiples of 16 (a view of a wider tensor where the
-    width is none) is read as it is by ``npd_head_logits_int8``."""
+    (see ``npd_quantize_rows`` in npd.h).  ``npd_head_logits_int8`` copies rows of a width or stride that is no multiple of 16, in
+    calls of more than 64 positions.  It reads them as they are if they are laid out in rows of the next multiple, zeros behind the
+    width (``q_out`` is the view without these), and it is given those whole rows: zeros add nothing to a sum."""
     if _host is not None:
         st = _host.quantize_rows(x, q_out, scale_out)
         if st >= 0:

@@ -40,3 +40,25 @@ def test_ends_of_rows(D):
     out = torch.empty((T, V), dtype=torch.bfloat16, device=DEV)
     npd.npd_head_logits_int8(h, torch.ones(T, device=DEV), w, torch.ones(V, device=DEV), logits_out=out)
     assert torch.equal(out, torch.full_like(out, D - 8 if D > 1 else 1))
+
+
+@pytest.mark.parametrize("T", [40, 70, 300])
+def test_rows_laid_out_with_zeros_are_read_as_they_are(T):
+    """What npd_quantize_rows' documentation says: rows of the next multiple of 16, zeros behind the width, need no copy and have the same
+    logits.  Rows that only begin there are copied."""
+    V, D, S = 1200, 1000, 1008
+    g = torch.Generator(device=DEV).manual_seed(T)
+    rows, scales = [], []
+    for n in (T, V):
+        whole, scale = torch.zeros((n, S), dtype=torch.int8, device=DEV), torch.empty(n, device=DEV)
+        npd.npd_quantize_rows(torch.randn((n, D), device=DEV, generator=g).to(torch.bfloat16), q_out=whole[:, :D], scale_out=scale)
+        assert not bool(whole[:, D:].any())
+        rows.append(whole)
+        scales.append(scale)
+    assert npd.npd_head_workspace_bytes(binding.NPD_HEAD_LOGITS_INT8, T, V, S) == 0
+    copied = npd.npd_head_workspace_bytes(binding.NPD_HEAD_LOGITS_INT8, T, V, D, hidden_stride=S, weight_stride=S)
+    assert copied == (0 if T <= 64 else -(-T * S // 256) * 256 + -(-V * S // 256) * 256)
+    a, b = torch.empty((2, T, V), dtype=torch.bfloat16, device=DEV)
+    npd.npd_head_logits_int8(rows[0], scales[0], rows[1], scales[1], logits_out=a, workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
+    npd.npd_head_logits_int8(rows[0][:, :D], scales[0], rows[1][:, :D], scales[1], logits_out=b)
+    assert torch.equal(a, b)
