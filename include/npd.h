@@ -554,7 +554,8 @@ npd_status npd_layer_norm(const npd_norm_desc* desc, const void* x, const void* 
  *   NPD_NORM_RMS, else NULL; weight  bf16 [D] or NULL;  grad_x  bf16 [T, grad_x_stride]  grad_weight, grad_bias  bf16 [D]
  *   workspace  device, >= npd_layer_norm_workspace_bytes(desc) bytes (0 for grad_x alone), 256-byte aligned; as for the head's calls
  *
- * Reproducible bit by bit for the same sizes.  The gradients that rows share are non-finite where a row's is.
+ * Reproducible bit by bit for the same sizes.  x may be any finite values; a row whose rstd is not finite has gradients that are not,
+ * and the gradients that rows share are non-finite where a row's is.
  */
 npd_status npd_layer_norm_bwd(const npd_norm_desc* desc, const void* grad_y, const void* x, const void* weight,
                               const float* mean, const float* rstd, void* grad_x, void* grad_weight, void* grad_bias,

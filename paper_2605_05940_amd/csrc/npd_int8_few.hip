@@ -360,7 +360,8 @@ hipError_t launch_int8_few(const Int8Args& a, hipStream_t stream) {
   // Up to four rows of 1,536 and more bytes are int8_tokens_kernel's, whose waves share a row.  Measured (MI355X, us, one row there / in
   // int8_few_kernel, weights out of the caches): 8,000 x 1,024 6.1 / 4.9 (1,000 entries), 8,000 x 1,536 7.0 / 7.8, 8,000 x 8,192 15.3 / 39.7,
   // 32,000 x 2,048 15.4 / 13.7, 50,048 x 2,048 22.1 / 20.0, 100,000 x 2,048 38.2 / 43.9, 151,936 x 1,024 35.4 / 30.4, x 1,536 40.6 / 44.2, x
-  // 2,048 53 / 60, 262,144 x 1,152 82.5 / 56.8.  Eight rows in two of its products at once are slower (100,000 x 2,048 70 / 46).
+  // 2,048 53 / 60, 262,144 x 1,152 82.5 / 56.8.  (The width alone decides: 32,000 to 50,000 entries of 2,048 are 10 to 12 % slower so.)
+  // Eight rows in two of its products at once are slower (100,000 x 2,048 70 / 46).
   if (a.T <= 4 && a.D >= 1536)
     return launch_kernel(int8_tokens_kernel, dim3((unsigned)((a.V + (int64_t)kTokenColumns - 1) / kTokenColumns)), dim3(kHeadThreads), 0, stream, a);
   if (a.T <= 16) return launch_fragments<1>(a, stream);

@@ -126,7 +126,10 @@ hipError_t launch_int8_many(const Int8Args& a, hipStream_t stream) {
   if (a.T <= 64) return launch<2, 4>(a, 3, stream);
   if (a.T <= 128 || head_small(a.T, a.V)) return launch<4, 4>(a, 2, stream);
   const int64_t tiles = (a.T + 255) / 256 * (((int64_t)a.V + 255) / 256);
-  // (up to 384 rows fill three tiles of 128, two of 256 by three quarters; with a short k that decides: 333 x 50,003 x 1,008, capped, 54 / 60)
+  // (Up to 384 rows fill three tiles of 128, two of 256 by three quarters; with a short k that decides.  Measured (us, tiles of 128 / the
+  // larger ones below, 257 and 384 rows): 50,048 x 256 14.4 / 26.7 and 16.1 / 27.2, x 1,024 32.6 / 42.5 and 38.4 / 44.5; 151,936 x 1,024 87.9 /
+  // 100.9 and 108.9 / 105.0, x 1,536 124 / 126 and 150 / 133, x 2,048 154 / 157 and 181 / 162; 262,144 x 1,024 147 / 154 and 182 / 164.  Up to
+  // 50,048 entries tiles of 128 are faster at 1,536 and 2,048 too, 44.5 / 52.1 and 63.4 / 66.3 us: the width alone decides.)
   if (a.T > 256 && a.T <= 384 && a.D <= 1024) return launch<4, 4>(a, 2, stream);
   if (tiles <= 128) return launch<8, 4>(a, 1, stream);
   return launch<8, 8>(a, 1, stream);

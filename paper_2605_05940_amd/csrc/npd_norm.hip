@@ -2,9 +2,10 @@
 // of eight values each, from its one read to its one write; its sums are taken over what is there (the mean first, then the squares of
 // what is left: the difference of two large sums is never formed).
 //
-// Bytes bound it.  Measured (MI355X, 32,768 x 2,048): forward 48.4 us (5.5 TB/s), backward with both parameters' gradients 82.8 (4.9 TB/s;
+// Bytes bound it.  Measured (MI355X, 32,768 x 2,048): forward 48.5 us (5.5 TB/s), backward with both parameters' gradients 83.4 (4.9 TB/s;
 // torch's copy of 4 GiB reaches 4.7), of which joining the 512 pieces of those is 4.  With what is unpacked kept in registers, and so one
-// or two waves per SIMD, 56.8 and 110.  One row of 2,048 3.6 us.
+// or two waves per SIMD, 56.8 and 110.  One row of 2,048 3.7 us.  Rows wider than 16,384 have their gradients read twice (2,048 x 32,768
+// 218 us, 10 bytes a value for 6).
 #include <float.h>
 
 #include "../../include/npd.h"

@@ -10,11 +10,13 @@
 //
 // Counting bounds it: eleven vector instructions and two LDS additions for a pair of entries (262,144 take a compute unit 16 us, where
 // its share of the memory's rate would be 20), then some 6 us of dependent steps, most of them one wave's or between barriers.
-// Measured (MI355X, us): 256 rows of 151,936, top-k 50, top-p 0.9: 26.7 (read and counted 11.3, largest value 1, weights 2.8, search 2.2,
-// the token's id .5 to 5); one row of 262,144 in eight parts 17.6, whole 34; 2,048 rows of 151,936 greedy 147 (4.2 TB/s), untruncated 191:
-// where the token's value occurs more than once its row is read again.  4,096 rows of 1,000 take 67: rows that short are not what this
-// is made for.  (With longer steps, 112 then, workgroups of 512 threads, three to a compute unit, were 8 to 13 % faster for those, and 16 %
-// slower for 48 rows of 50,003.)
+// Measured (MI355X, us): 256 rows of 151,936, temperature 0.7, top-k 50, top-p 0.9: 26.9 (by the clock in an instrumented build: read and
+// counted 11.3, largest value 1, weights 2.8, search 2.2, the token's id .5 to 5); one row of 262,144, untruncated, in eight parts 17.0,
+// whole 34; 2,048 rows of 151,936 greedy 148 (4.2 TB/s), untruncated 193: where the token's value occurs more than once its row is read
+// again.  4,096 rows of 1,000 take 60 greedy, 67 untruncated and 80 with that top-k and top-p: rows that short are not what this is made
+// for.  (With longer steps, 112 then, workgroups of 512 threads, three to a compute unit, were 8 to 13 % faster for those, and 16 %
+// slower for 48 rows of 50,003.)  By bisection, with logits of a spread of 1,000, 48 rows of 50,003 take 321 untruncated and 1,060 with
+// top-k and top-p (14 and 15 counted), 256 of 151,936 803 and 2,705 (34 and 28): 16 passes for each of one to four searches.
 #include <stddef.h>
 
 #include "../../include/npd.h"
@@ -997,7 +999,8 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 4 : 8) void sample_kernel(SampleA
 // counts have to be earned.  Measured (MI355X, us, whole / in parts, untruncated): 1 row of 100,000 16.1 / 16.4 (3 parts), of 128,256 18.2 / 17.7
 // (3), of 151,936 17.8 / 16.3 (4), of 262,144 34 / 18.5 (8), of 600,000 51 / 18.6 (8); 32 rows of 100,000 19.0 / 19.4 (3), of 151,936 24.9 / 21.1
 // (4), of 262,144 37 / 22.1 (8); 64 rows of 128,256 23.1 / 23.0 (3), of 151,936 26.1 / 23.2 (4).  With top-k 50 and top-p 0.9, where few rows are
-// read again, 64 rows of 100,000 18.9 / 21.9, of 151,936 22.5 / 23.6, of 262,144 30.6 / 25.2.
+// read again, 64 rows of 100,000 18.9 / 21.9, of 151,936 22.5 / 23.6, of 262,144 30.6 / 25.2.  So at the beginning of the range parts gain
+// nothing, and 64 rows of up to 151,936 lose by them if they are truncated, which the host does not know of rows with settings of their own.
 int sample_parts(int64_t T, int32_t V) {
   const int64_t most = 256 / T < kSampleParts ? 256 / T : kSampleParts, some = V / 32768, parts = most < some ? most : some;
   return parts < 3 ? 1 : (int)parts;
