@@ -97,9 +97,10 @@ __device__ __forceinline__ void stay_packed(uint4 (&w)[G]) {
 }
 
 // A row whose sums or squares fp32 does not hold, done again: read for each of its sums and for y, a value at a time (no model has such
-// rows; 32,768 of them of 2,048 take 305 us, others 44).  With its largest value's power of two taken out, which is exact, nothing leaves
-// fp32, and the variance is put together in 64 bits.  A row that is not finite stays as it came out.  (Threads have the values that they
-// have in norm_kernel: what was written there is written again by the same thread.)
+// rows; 32,768 of them of 2,048 take 305 us, others 44).  With its largest value's power of two taken out nothing that shows leaves fp32
+// (what is less than 2^-126 of that value is rounded to 2^-149 of it; the rest is exact), and the variance is put together in 64 bits.  A
+// row that is not finite stays as it came out.  (Threads have the values that they have in norm_kernel: what was written there is
+// written again by the same thread.)
 template <int TH, int G>
 __device__ __forceinline__ void norm_wide_row(const NormArgs& a, int64_t p, float* smem) {
   int thread = threadIdx.x;
